@@ -312,15 +312,16 @@ def _adamw_plain(s):
 
 def _adamw_own(s):
     from paper_2301_06284_amd import rgnn
-    if "views" not in s:      # a program keeps its tensors' lists
+    if "tensors" not in s:      # a program keeps its tensors' list
         cut = lambda b: [b[o:o + n] for o, n in s["at"]]  # noqa: E731
         cut_top = lambda b: [b[o // QBLOCK:-(-(o + n) // QBLOCK)] for o, n in s["at"]]  # noqa: E731
-        s["views"] = dict(params=cut(s["p"]), grads=cut(s["grad"]), m=cut(s["m"]), v=cut(s["v"]))
+        views = dict(params=cut(s["p"]), grads=cut(s["grad"]), m=cut(s["m"]), v=cut(s["v"]))
         if s["case"]["bits"] == 8:
-            s["views"].update(m_scale=cut_top(s["ms"]), v_scale=cut_top(s["vs"]))
+            views.update(m_scale=cut_top(s["ms"]), v_scale=cut_top(s["vs"]))
         if "copy" in s:
-            s["views"].update(copies=cut(s["copy"]))
-    rgnn.adamw_step(**s["views"], step=s["step"], lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, weight_decay=DECAY)
+            views.update(copies=cut(s["copy"]))
+        s["tensors"] = rgnn.AdamwTensors(**views)
+    rgnn.adamw_step(s["tensors"], step=s["step"], lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, weight_decay=DECAY)
 
 
 def _adamw(s):
