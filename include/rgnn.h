@@ -1,6 +1,7 @@
 /*
- * rgnn.h -- C ABI of librgnn.so: RGCN, RGAT and HGT layers and the RGAT
- * backward pass on one MI355X (gfx950), in fp32.
+ * rgnn.h -- C ABI of librgnn.so: RGCN, RGAT and HGT layers and their backward
+ * passes on one MI355X (gfx950), in fp32, and the typed linear for training and
+ * serving (fp32, 16 and 8 bits) with the AdamW step.
  *
  * The layers follow the definitions of Hector (ASPLOS '24, arXiv 2301.06284):
  *   RGCN  -- the RGCN equation of Section "RGNN Formulation and Operators";
@@ -17,7 +18,7 @@
  *     and maps a row of d_in features to d_out outputs (the typed-linear formula
  *     Y[i,0,j] = sum_k X[i,0,k] W[T[i],k,j] of Section "Inefficiency in Existing
  *     Computation Stack").
- *   - All tensors are dense, row-major, fp32, on the device the graph was
+ *   - All tensors of the layers are dense, row-major, fp32, on the device the graph was
  *     created on.  Pointers named h, W, out, grad_* and ws are DEVICE pointers
  *     owned by the caller; the library never frees them.
  *   - Outputs and gradients are overwritten, never accumulated.
@@ -342,6 +343,136 @@ rgnn_status rgnn_segment_gemm(const float *X, int64_t ldx, const int32_t *gather
                               int32_t K, int32_t Nc, float *Y, int64_t ldy,
                               const int32_t *scatter, void *ws, size_t ws_bytes, void *stream);
 rgnn_status rgnn_segment_gemm_workspace_size(int64_t M, int32_t num_types, size_t *bytes);
+
+/* ------------------------------------------------------------------ typed linear
+ *
+ * The typed linear for training and serving: segment MM with its gradients, in 16
+ * bits and in 8, over type offsets that lie on the DEVICE (a router or a sampler
+ * makes them there, and the host never waits for them), for any widths.
+ *
+ * What these calls share, besides the conventions above:
+ *   - type_ptr: DEVICE int64 [num_types + 1], ascending; type t owns the positions
+ *     [type_ptr[t], type_ptr[t+1]).  M is how many positions the index arrays and the
+ *     rows hold, a capacity: positions outside [type_ptr[0], type_ptr[num_types]) belong
+ *     to no type, and nothing of theirs is read or written.  Offsets are kept inside [0, M]
+ *     by the kernels; offsets that descend give wrong rows, and no access out of range.
+ *   - gather / scatter: DEVICE int32 [M] or NULL for the identity (then the matrix
+ *     needs M rows).  A gathered index outside the matrix's rows (-1, say) reads a row of
+ *     zeros, a scattered one writes nothing.  Gathered rows may repeat; scattered
+ *     rows that repeat race.
+ *   - ldx, ldy, lddy: elements from one row to the next.  Weights are dense.
+ *   - Types of the elements (rgnn_dtype): X, W and dY alike RGNN_F32, RGNN_BF16 or
+ *     RGNN_F16; outputs of the same type, or RGNN_F32.  Sums are kept in fp32 and rounded
+ *     once, to nearest.  fp32 operands are multiplied by the fp32 matrix cores, so
+ *     infinities and NaN go where the definition takes them.
+ *   - 1 <= K, N <= 2^24; M < 2^31 - 1; num_types <= 65535.  RGNN_ERANGE beyond.
+ *   - Results are reproducible: no atomics, sums in a fixed order.
+ *   - Fastest where the base addresses and the rows (ldx, ldy, K, N times the element's
+ *     size) are multiples of 16 bytes; right for any. */
+typedef enum {
+    RGNN_F32 = 0,
+    RGNN_BF16 = 1,
+    RGNN_F16 = 2,
+    RGNN_F8_E4M3 = 3      /* 1 sign, 4 exponent, 3 mantissa bits, largest 448, no infinities */
+} rgnn_dtype;
+
+/* Y[scatter[i]] = X[gather[i]] W[t(i)] for every position i that a type owns.
+ *   X [x_rows, K], W [num_types, K, N], Y [y_rows, N].
+ *   trans_w = 1: W is stored [num_types, N, K] and used transposed: with dY as X,
+ *   the same weights as in the forward (K and N exchanged) and gather and scatter
+ *   exchanged, the call is the input gradient dX = dY W^T (of repeated rows: one row
+ *   for each position). */
+rgnn_status rgnn_typed_linear(int32_t dtype, const void *X, int64_t x_rows, int64_t ldx,
+                              const int32_t *gather, const int64_t *type_ptr, int32_t num_types,
+                              int64_t M, const void *W, int32_t K, int32_t N, int32_t trans_w,
+                              int32_t y_dtype, void *Y, int64_t y_rows, int64_t ldy,
+                              const int32_t *scatter, void *stream);
+
+/* The weight gradient: dW[t] = sum over the positions i of type t of
+ * X[gather[i]]^T dY[dy_gather[i]]; zero for a type without positions.
+ *   X [x_rows, K], dY [dy_rows, N], dW [num_types, K, N]; dy_gather is the forward's
+ *   scatter.  ws: rgnn_typed_linear_wgrad_workspace_size() bytes. */
+rgnn_status rgnn_typed_linear_wgrad(int32_t dtype, const void *X, int64_t x_rows, int64_t ldx,
+                                    const int32_t *gather, const void *dY, int64_t dy_rows,
+                                    int64_t lddy, const int32_t *dy_gather,
+                                    const int64_t *type_ptr, int32_t num_types, int64_t M,
+                                    int32_t K, int32_t N, int32_t dw_dtype, void *dW, void *ws,
+                                    size_t ws_bytes, void *stream);
+rgnn_status rgnn_typed_linear_wgrad_workspace_size(int32_t dtype, int64_t M, int32_t num_types,
+                                                   int32_t K, int32_t N, size_t *bytes);
+
+/* 8-bit rows and weights with a scale for each block of 128.  A block's scale is the
+ * least power of two s >= 2^-126 with max |x| <= 448 s, kept as the byte log2(s) + 127; its codes
+ * are x / s (exact) rounded to the nearest e4m3 value, ties to even.  A block that holds
+ * an infinity or a NaN has scale byte 255 and NaN codes.
+ *   Kp = K rounded up to 128, Ks = 4 * ceil(K / 512) (whole 32-bit words of scales).
+ *   rows:    X [rows, K] -> codes [rows, Kp], scales [rows, Ks]; blocks of 1 x 128.
+ *   weights: W [num_types, K, N] -> codes [num_types, N, Kp] (each output's k side by
+ *            side), scales [num_types, ceil(N / 128), Ks]; blocks of 128 x 128.
+ *   Codes behind K are 0, scale bytes behind the last block 127.  dtype of X and W:
+ *   RGNN_F32, RGNN_BF16 or RGNN_F16.  codes on a 16-byte address, scales on a 4-byte one. */
+rgnn_status rgnn_fp8_quantize_rows(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t K,
+                                   void *codes, uint8_t *scales, void *stream);
+rgnn_status rgnn_fp8_quantize_weights(int32_t dtype, const void *W, int32_t num_types, int32_t K,
+                                      int32_t N, void *codes, uint8_t *scales, void *stream);
+
+/* rgnn_typed_linear on such rows and weights: X codes [x_rows, Kp] and scales
+ * [x_rows, Ks], W codes [num_types, N, Kp] and scales [num_types, ceil(N/128), Ks], both on
+ * 16-byte addresses; Y RGNN_F32, RGNN_BF16 or RGNN_F16.  The products of codes and scales are
+ * formed by the 8-bit matrix cores, which add
+ * products in groups of eight aligned to the group's largest and drop what lies below 2^-13
+ * of its power of two (measured), and keep the sums of the groups in fp32: about 1e-5 of
+ * the sum of magnitudes, far below what the codes' 2^-4 leave. */
+rgnn_status rgnn_typed_linear_fp8(const void *X, const uint8_t *x_scales, int64_t x_rows,
+                                  const int32_t *gather, const int64_t *type_ptr, int32_t num_types,
+                                  int64_t M, const void *W, const uint8_t *w_scales, int32_t K,
+                                  int32_t N, int32_t y_dtype, void *Y, int64_t y_rows, int64_t ldy,
+                                  const int32_t *scatter, void *stream);
+
+/* ------------------------------------------------------------------ AdamW
+ *
+ * One AdamW step of many tensors at once, for the gradients of the backward calls.
+ * Per element, with g = grad * grad_scale, t the step's number from 1:
+ *   m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, whatever the types; a 16-bit parameter is rounded to nearest, and `copy` takes
+ * the new parameter in another type (the working copy of fp32 parameters).
+ *
+ * States in 32 bits: m, v fp32 [n].  In 8 bits: m int8 [n], v uint8 [n] in blocks of 256
+ * elements from the tensor's start with one fp32 number each, m_scale, v_scale
+ * [ceil(n / 256)], the block's largest |m| and v ("top"):
+ *   m = top sgn(c) (c / 127)^2,  c = +-round(127 sqrt(|m| / top))
+ *   v = top (c / 255)^4,         c = round(255 (v / top)^(1/4)), at least 1 where v > 0
+ * The powers spend the codes on small values: a code's v spans 4.2e9, and none
+ * that is not zero becomes zero (its update would be divided by eps).  The step itself
+ * uses m and v before they are rounded.  Zero codes and scales are the start state.
+ * Gradients and states must be finite (an infinity or a NaN spoils its block). */
+typedef struct {
+    void *param;             /* [n]                                             */
+    const void *grad;        /* [n]                                             */
+    void *m, *v;             /* [n] fp32, or int8 and uint8                     */
+    float *m_scale, *v_scale;/* [ceil(n / 256)] with 8-bit states, else NULL    */
+    void *copy;              /* [n] or NULL                                     */
+    int64_t n;
+    int32_t param_dtype, grad_dtype, copy_dtype;   /* RGNN_F32, RGNN_BF16 or RGNN_F16 */
+    int32_t state_bits;      /* 32 or 8                                         */
+} rgnn_adamw_tensor_t;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+} rgnn_adamw_t;
+
+/* One step of the tensors (HOST array, read during the call only).  Tensors may lie
+ * anywhere and be of any length (0 is skipped); no two may overlap, and one named twice
+ * is refused (RGNN_EINVAL).
+ *   step: t, from 1.  step_dev: NULL, or DEVICE int64 [1] that holds t and is read
+ *   when the kernels run, so that a captured graph counts on; `step` is then unused.
+ *   grad_scale: NULL, or DEVICE fp32 [1], a factor on every gradient (clipping, loss
+ *   scaling).
+ * Needs no workspace.  Fastest on addresses of 16 bytes; right for any that the types allow. */
+rgnn_status rgnn_adamw_step(const rgnn_adamw_tensor_t *tensors, int32_t num_tensors,
+                            const rgnn_adamw_t *hyper, int64_t step, const int64_t *step_dev,
+                            const float *grad_scale, void *stream);
 
 /* ------------------------------------------------------------------ profiling */
 

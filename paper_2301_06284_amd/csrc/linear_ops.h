@@ -1,0 +1,193 @@
+// linear_ops.h -- what the typed linear's kernels share: element types and their
+// matrix instructions, the search for a workgroup's tile in offsets that lie on the
+// device, and the launchers' arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "rgnn_internal.h"
+
+namespace rgnn {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// ---------------------------------------------------------------- arguments
+
+struct LinearArgs {
+    int dtype = 0;                       // rgnn_dtype of X and W (fp8: RGNN_F8_E4M3)
+    int y_dtype = 0;
+    const void *X = nullptr;   int64_t x_rows = 0, ldx = 0;
+    const int32_t *gather = nullptr;
+    const int64_t *type_ptr = nullptr;   // device [T+1]
+    int32_t T = 0;
+    int64_t M = 0;
+    const void *W = nullptr;
+    int32_t K = 0, N = 0;
+    int trans_w = 0;                     // W stored [T, N, K]
+    void *Y = nullptr;         int64_t y_rows = 0, ldy = 0;
+    const int32_t *scatter = nullptr;
+    // fp8: scale bytes of X [x_rows, ks] and of W [T, ceil(N/128), ks]
+    const uint8_t *x_scale = nullptr, *w_scale = nullptr;
+};
+
+struct WgradArgs {
+    int dtype = 0, dw_dtype = 0;
+    const void *X = nullptr;   int64_t x_rows = 0, ldx = 0;
+    const int32_t *gather = nullptr;     // rows of X
+    const void *dY = nullptr;  int64_t dy_rows = 0, lddy = 0;
+    const int32_t *dy_gather = nullptr;  // rows of dY (the forward's scatter)
+    const int64_t *type_ptr = nullptr;
+    int32_t T = 0;
+    int64_t M = 0;
+    int32_t K = 0, N = 0;
+    void *dW = nullptr;
+    void *ws = nullptr;
+};
+
+size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
+rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s);
+rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s);
+
+rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s);
+rgnn_status launch_fp8_rows(int dtype, const void *X, int64_t rows, int64_t ldx, int K, void *codes, uint8_t *scales,
+                            hipStream_t s);
+rgnn_status launch_fp8_weights(int dtype, const void *W, int T, int K, int N, void *codes, uint8_t *scales, hipStream_t s);
+rgnn_status launch_adamw(const rgnn_adamw_tensor_t *t, int32_t count, const rgnn_adamw_t &h, int64_t step,
+                         const int64_t *step_dev, const float *grad_scale, hipStream_t s);
+
+// Width of the codes of K elements, and bytes of their scales (whole words).
+constexpr int32_t fp8_width(int32_t K) { return (K + 127) / 128 * 128; }
+constexpr int32_t fp8_scales(int32_t K) { return (K + 511) / 512 * 4; }
+
+constexpr int dtype_bytes(int d) { return d == RGNN_F32 ? 4 : d == RGNN_F8_E4M3 ? 1 : 2; }
+
+// Row tiles of `rows` rows that M rows of T types can make, at most: every type that
+// has rows can leave one tile partly filled.
+inline int64_t row_tiles_bound(int64_t M, int64_t T, int64_t rows)
+{
+    const int64_t nz = M < T ? M : T;
+    return (M + nz * (rows - 1)) / rows;
+}
+
+#ifdef __HIPCC__
+
+// ---------------------------------------------------------------- elements
+
+struct F32 { typedef float elem; };
+struct BF16 { typedef __bf16 elem; };
+struct F16 { typedef _Float16 elem; };
+
+// D[n][m] += sum_k a[n][k] b[m][k] over 16 bytes of k a lane: lane l holds row l % 16
+// of both, 16-byte chunk l / 16 of the step's k.  The order of k within a step is the
+// same for both operands, so any one will do: fp32 takes the chunk's element i of the
+// four lane groups in instruction i.  The result's lane l holds m = l % 16 and the
+// four n = 4 (l / 16) + i.
+template <class T>
+__device__ __forceinline__ f32x4 mma16(i32x4 a, i32x4 b, f32x4 c);
+template <>
+__device__ __forceinline__ f32x4 mma16<BF16>(i32x4 a, i32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f32x4 mma16<F16>(i32x4 a, i32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ f32x4 mma16<F32>(i32x4 a, i32x4 b, f32x4 c)
+{
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+    return c;
+}
+
+// ---------------------------------------------------------------- tiles
+
+// Rows [begin, end) of type t, with offsets that the host has not seen kept inside
+// [0, M): a table that is not monotone gives wrong rows, and no access out of range.
+__device__ __forceinline__ void type_rows(const int64_t *ptr, int t, int64_t M, int64_t &begin, int64_t &end)
+{
+    const int64_t p = ptr[t], q = ptr[t + 1];
+    begin = p < 0 ? 0 : p > M ? M : p;
+    end = q < begin ? begin : q > M ? M : q;
+}
+
+// A value that is the same in every lane, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+    return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+
+struct Piece {          // a workgroup's share: number `index` of type `type`'s pieces
+    int type;
+    int64_t begin, end;   // the type's rows
+    int64_t index, count; // piece and number of pieces of the type
+    int64_t before;       // what `weight` counted in the types before it
+};
+
+// The type that owns piece number `want`, where type t with c rows makes count(c)
+// pieces.  Every wave of a workgroup searches alike, 256 types a turn: one load of
+// the offsets and a prefix sum over the lanes, no LDS and no barrier.  weight(c) is a
+// second count summed over the types before the owner.  False where there are fewer pieces.
+template <class Count, class Weight>
+__device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int T, int64_t M, int64_t want,
+                                           Count count, Weight weight, Piece &out)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t before = 0, wbefore = 0;
+    for (int t0 = 0; t0 < T; t0 += 256) {
+        int64_t b[4], e[4], c[4], w[4], cs = 0, ws = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + lane * 4 + i;
+            b[i] = e[i] = c[i] = w[i] = 0;
+            if (t < T) {
+                type_rows(ptr, t, M, b[i], e[i]);
+                c[i] = count(e[i] - b[i]);
+                w[i] = weight(e[i] - b[i]);
+            }
+            cs += c[i];
+            ws += w[i];
+        }
+        int64_t ci = cs, wi = ws;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t x = __shfl_up(ci, d), y = __shfl_up(wi, d);
+            if (lane >= d) { ci += x; wi += y; }
+        }
+        const int64_t total = __shfl(ci, 63);
+        if (want < before + total) {
+            const uint64_t over = __ballot(before + ci > want);
+            const int owner = __builtin_ctzll(over);
+            int64_t at = before + ci - cs, wat = wbefore + wi - ws;   // before this lane's first type
+            int k = 0;
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (k == i && at + c[i] <= want) { at += c[i]; wat += w[i]; k = i + 1; }
+            const int64_t bb = k == 0 ? b[0] : k == 1 ? b[1] : k == 2 ? b[2] : b[3];
+            const int64_t ee = k == 0 ? e[0] : k == 1 ? e[1] : k == 2 ? e[2] : e[3];
+            const int64_t cc = k == 0 ? c[0] : k == 1 ? c[1] : k == 2 ? c[2] : c[3];
+            out.type = (int)uniform(__shfl(t0 + lane * 4 + k, owner));
+            out.begin = uniform(__shfl(bb, owner));
+            out.end = uniform(__shfl(ee, owner));
+            out.count = uniform(__shfl(cc, owner));
+            out.index = want - uniform(__shfl(at, owner));
+            out.before = uniform(__shfl(wat, owner));
+            return true;
+        }
+        before += total;
+        wbefore += __shfl(wi, 63);
+    }
+    return false;
+}
+
+#endif  // __HIPCC__
+
+}  // namespace rgnn

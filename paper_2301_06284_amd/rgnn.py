@@ -24,6 +24,7 @@ LAYER_RGCN_BACKWARD, LAYER_HGT_BACKWARD = 5, 6
 SOFTMAX_PER_DST, SOFTMAX_PER_DST_REL = 0, 1
 FLAG_RELU, FLAG_RESIDUAL, FLAG_A_LINEAR = 1, 2, 4
 GRAPH_HOST_ONLY, GRAPH_NO_COMPACT = 1, 2
+F32, BF16, F16, F8_E4M3 = 0, 1, 2, 3
 
 INDEX_KINDS = {
     "dst_rowptr": 0, "in_src": 1, "in_rel": 2, "in_eid": 3, "seg_ptr": 4, "seg_rel": 5,
@@ -36,7 +37,9 @@ EXPORTED = [
     "rgnn_graph_export", "rgnn_workspace_size", "rgnn_select_plan", "rgcn_forward",
     "rgat_forward", "rgat_forward_noalloc", "hgt_forward", "rgat_backward", "rgcn_backward", "hgt_backward",
     "rgnn_segment_gemm",
-    "rgnn_segment_gemm_workspace_size", "rgnn_profile_enable", "rgnn_profile_count",
+    "rgnn_segment_gemm_workspace_size", "rgnn_typed_linear", "rgnn_typed_linear_wgrad",
+    "rgnn_typed_linear_wgrad_workspace_size", "rgnn_fp8_quantize_rows", "rgnn_fp8_quantize_weights",
+    "rgnn_typed_linear_fp8", "rgnn_adamw_step", "rgnn_profile_enable", "rgnn_profile_count",
     "rgnn_profile_read", "rgnn_profile_reset", "rgnn_last_error", "rgnn_version",
 ]
 
@@ -55,6 +58,18 @@ class GraphInfo(ctypes.Structure):
                 ("num_vsegs", ctypes.c_int64), ("num_items", ctypes.c_int64),
                 ("num_split_dst", ctypes.c_int64), ("chunk_edges", ctypes.c_int32),
                 ("device", ctypes.c_int32)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("copy_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32)]
+
+
+class AdamwHyper(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")]
 
 
 def _load():
@@ -82,6 +97,14 @@ def _load():
                          vp, vp, vp, vp, sz, vp],
         "rgnn_segment_gemm": [vp, i64, vp, vp, i32, vp, i32, i32, vp, i64, vp, vp, sz, vp],
         "rgnn_segment_gemm_workspace_size": [i64, i32, P(sz)],
+        "rgnn_typed_linear": [i32, vp, i64, i64, vp, vp, i32, i64, vp, i32, i32, i32, i32, vp, i64, i64, vp, vp],
+        "rgnn_typed_linear_wgrad": [i32, vp, i64, i64, vp, vp, i64, i64, vp, vp, i32, i64, i32, i32, i32, vp, vp,
+                                    sz, vp],
+        "rgnn_typed_linear_wgrad_workspace_size": [i32, i64, i32, i32, i32, P(sz)],
+        "rgnn_fp8_quantize_rows": [i32, vp, i64, i64, i32, vp, vp, vp],
+        "rgnn_fp8_quantize_weights": [i32, vp, i32, i32, i32, vp, vp, vp],
+        "rgnn_typed_linear_fp8": [vp, vp, i64, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, i64, i64, vp, vp],
+        "rgnn_adamw_step": [P(AdamwTensor), i32, P(AdamwHyper), i64, vp, vp, vp],
         "rgnn_profile_enable": [i32],
         "rgnn_profile_count": [P(i32)],
         "rgnn_profile_read": [i32, ctypes.c_char_p, sz, P(i64), P(ctypes.c_double)],
@@ -296,6 +319,231 @@ def segment_gemm(X, gather, type_ptr, W, Y, scatter, ws, K, Nc, stream=None):
                                   _ptr(W), K, Nc, _ptr(Y), Y.shape[1], _ptr(scatter), _ptr(ws),
                                   0 if ws is None else ws.numel() * ws.element_size(),
                                   _stream(stream)))
+
+
+# ---------------------------------------------------------------- typed linear, AdamW
+#
+# These calls check their tensors here: type, shape, device and strides, since a wrong
+# one would read out of range.  Matrices may have any row stride (their columns lie
+# side by side); everything else is contiguous.
+
+_DTYPES: dict = {}
+
+
+def _dtype(t) -> int:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"tensors must be fp32, bf16 or fp16, not {t.dtype}")
+    return d
+
+
+def _need(ok, why: str):
+    if not ok:
+        raise ValueError(why)
+
+
+def _same_device(first, *others):
+    import torch
+    _need(first.is_cuda, "tensors must be on a GPU")
+    _need(first.get_device() == torch.cuda.current_device(),
+          f"tensors are on device {first.get_device()}, the current one is {torch.cuda.current_device()}")
+    for t in others:
+        _need(t is None or t.device == first.device, "tensors must be on one device")
+
+
+def _matrix(t, name: str, cols: int):
+    """(pointer, rows, leading dimension) of a matrix with `cols` columns."""
+    _need(t.dim() == 2 and t.shape[1] == cols, f"{name} must have {cols} columns")
+    rows, ld = t.shape[0], t.stride(0)
+    if rows <= 1:
+        ld = max(ld, cols)
+    _need((cols <= 1 or t.stride(1) == 1) and ld >= cols, f"{name}'s columns must lie side by side, its rows apart")
+    return t.data_ptr(), rows, ld
+
+
+def _indices(type_ptr, types: int, *index):
+    """Checks the offsets and index arrays; the number of positions, or None."""
+    import torch
+    _need(type_ptr.dtype == torch.int64 and type_ptr.dim() == 1 and type_ptr.is_contiguous() and
+          type_ptr.shape[0] == types + 1, "type_ptr must be int64 [types + 1]")
+    M = None
+    for i in index:
+        if i is None:
+            continue
+        _need(i.dtype == torch.int32 and i.dim() == 1 and i.is_contiguous(), "gather and scatter must be int32 [M]")
+        _need(M is None or i.shape[0] == M, "gather and scatter must have one length")
+        M = i.shape[0]
+    return M
+
+
+def typed_linear(X, type_ptr, W, Y, gather=None, scatter=None, trans_w=False, stream=None):
+    """Y[scatter[i]] = X[gather[i]] W[t(i)] over the positions of device offsets
+    type_ptr [types + 1] (trans_w: W [types, N, K] used transposed).  X, W, Y fp32, bf16
+    or fp16; Y of that type or fp32."""
+    _same_device(X, type_ptr, W, Y, gather, scatter)
+    _need(W.dim() == 3 and W.is_contiguous() and W.dtype == X.dtype, "W must be contiguous [types, ., .] of X's type")
+    T, K, N = W.shape
+    if trans_w:
+        K, N = N, K
+    xp, xr, ldx = _matrix(X, "X", K)
+    yp, yr, ldy = _matrix(Y, "Y", N)
+    M = _indices(type_ptr, T, gather, scatter)
+    if M is None:
+        M = xr
+    _check(_lib.rgnn_typed_linear(_dtype(X), xp, xr, ldx, _ptr(gather), type_ptr.data_ptr(), T, M, W.data_ptr(), K, N,
+                                  1 if trans_w else 0, _dtype(Y), yp, yr, ldy, _ptr(scatter), _stream(stream)))
+
+
+def typed_linear_wgrad_workspace_size(dtype, M: int, num_types: int, K: int, N: int) -> int:
+    """dtype: torch.float32, torch.bfloat16 or torch.float16."""
+    import torch
+    n = ctypes.c_size_t()
+    _check(_lib.rgnn_typed_linear_wgrad_workspace_size(_dtype(torch.empty(0, dtype=dtype)), M, num_types, K, N,
+                                                       ctypes.byref(n)))
+    return n.value
+
+
+def typed_linear_wgrad(X, dY, type_ptr, dW, ws, gather=None, dy_gather=None, stream=None):
+    """dW[t] = sum over the positions i of type t of X[gather[i]]^T dY[dy_gather[i]]."""
+    _same_device(X, dY, type_ptr, dW, ws, gather, dy_gather)
+    _need(dY.dtype == X.dtype, "dY must be of X's type")
+    _need(dW.dim() == 3 and dW.is_contiguous(), "dW must be contiguous [types, K, N]")
+    T, K, N = dW.shape
+    xp, xr, ldx = _matrix(X, "X", K)
+    dp, dr, ldd = _matrix(dY, "dY", N)
+    M = _indices(type_ptr, T, gather, dy_gather)
+    if M is None:
+        M = xr
+    _check(_lib.rgnn_typed_linear_wgrad(_dtype(X), xp, xr, ldx, _ptr(gather), dp, dr, ldd, _ptr(dy_gather),
+                                        type_ptr.data_ptr(), T, M, K, N, _dtype(dW), dW.data_ptr(), _ptr(ws),
+                                        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def fp8_widths(K: int):
+    """(columns of the codes, bytes of the scales) of K elements."""
+    return -(-K // 128) * 128, -(-K // 512) * 4
+
+
+def _fp8_out(codes, scales, lead, blocks, K, device):
+    import torch
+    Kp, Ks = fp8_widths(K)
+    if codes is None:
+        codes = torch.empty(*lead, Kp, dtype=torch.float8_e4m3fn, device=device)
+    if scales is None:
+        scales = torch.empty(*blocks, Ks, dtype=torch.uint8, device=device)
+    _fp8_check(codes, scales, lead, blocks, K)
+    return codes, scales
+
+
+def _fp8_check(codes, scales, lead, blocks, K):
+    import torch
+    Kp, Ks = fp8_widths(K)
+    _need(codes.dtype == torch.float8_e4m3fn and tuple(codes.shape) == (*lead, Kp) and codes.is_contiguous(),
+          f"codes must be contiguous float8_e4m3fn {(*lead, Kp)}")
+    _need(scales.dtype == torch.uint8 and tuple(scales.shape) == (*blocks, Ks) and scales.is_contiguous(),
+          f"scales must be contiguous uint8 {(*blocks, Ks)}")
+
+
+def fp8_quantize_rows(X, codes=None, scales=None, stream=None):
+    """X [rows, K] -> (codes float8_e4m3fn [rows, Kp], scales uint8 [rows, Ks]), a
+    power-of-two scale for each 128 columns of a row."""
+    _need(X.dim() == 2, "X must be a matrix")
+    xp, rows, ldx = _matrix(X, "X", X.shape[1])
+    codes, scales = _fp8_out(codes, scales, (rows,), (rows,), X.shape[1], X.device)
+    _same_device(X, codes, scales)
+    _check(_lib.rgnn_fp8_quantize_rows(_dtype(X), xp, rows, ldx, X.shape[1], codes.data_ptr(), scales.data_ptr(),
+                                       _stream(stream)))
+    return codes, scales
+
+
+def fp8_quantize_weights(W, codes=None, scales=None, stream=None):
+    """W [types, K, N] -> (codes float8_e4m3fn [types, N, Kp], scales uint8
+    [types, ceil(N / 128), Ks]), a power-of-two scale for each 128 x 128 block."""
+    _need(W.dim() == 3 and W.is_contiguous(), "W must be contiguous [types, K, N]")
+    T, K, N = W.shape
+    codes, scales = _fp8_out(codes, scales, (T, N), (T, -(-N // 128)), K, W.device)
+    _same_device(W, codes, scales)
+    _check(_lib.rgnn_fp8_quantize_weights(_dtype(W), W.data_ptr(), T, K, N, codes.data_ptr(), scales.data_ptr(),
+                                          _stream(stream)))
+    return codes, scales
+
+
+def typed_linear_fp8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatter=None, stream=None):
+    """typed_linear on the codes and scales of fp8_quantize_rows and
+    fp8_quantize_weights; Y fp32, bf16 or fp16."""
+    _same_device(X, x_scales, type_ptr, W, w_scales, Y, gather, scatter)
+    _need(W.dim() == 3 and X.dim() == 2, "X must be [rows, Kp], W [types, N, Kp]")
+    T, N, K = W.shape
+    _fp8_check(X, x_scales, (X.shape[0],), (X.shape[0],), K)
+    _fp8_check(W, w_scales, (T, N), (T, -(-N // 128)), K)
+    yp, yr, ldy = _matrix(Y, "Y", N)
+    M = _indices(type_ptr, T, gather, scatter)
+    if M is None:
+        M = X.shape[0]
+    _check(_lib.rgnn_typed_linear_fp8(X.data_ptr(), x_scales.data_ptr(), X.shape[0], _ptr(gather), type_ptr.data_ptr(),
+                                      T, M, W.data_ptr(), w_scales.data_ptr(), K, N, _dtype(Y), yp, yr, ldy,
+                                      _ptr(scatter), _stream(stream)))
+
+
+class AdamwTensors:
+    """The tensors of adamw_step, checked once and kept: lists of parameters,
+    gradients (the buffers that the backward calls write) and states m, v, fp32, or int8
+    and uint8 with m_scale, v_scale (fp32, one for each 256 elements); copies: None, or a
+    tensor or None for each parameter, which takes the new value in its own type."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
+        import torch
+        n = len(params)
+        m_scale, v_scale, copies = (x if x is not None else [None] * n for x in (m_scale, v_scale, copies))
+        lists = (params, grads, m, v, m_scale, v_scale, copies)
+        _need(all(len(x) == n for x in lists), "lists must have one length")
+        self._kept = [list(x) for x in lists]
+        self._array = (AdamwTensor * max(n, 1))()
+        self._n = n
+        self.device = params[0].device if n else None
+        for k, (p, g, a, b, sa, sb, c) in enumerate(zip(*lists)):
+            size, eight = p.numel(), a.dtype == torch.int8
+            _need(all(t is None or (t.is_contiguous() and t.device == self.device) for t in (p, g, a, b, sa, sb, c)),
+                  f"tensor {k}: tensors must be contiguous and on one device")
+            _need(p.is_cuda, "tensors must be on a GPU")
+            _need(all(t is None or t.numel() == size for t in (g, a, b, c)), f"tensor {k}: lengths differ")
+            if eight:
+                blocks = -(-size // 256)
+                _need(b.dtype == torch.uint8 and all(t is not None and t.dtype == torch.float32 and
+                                                     t.numel() == blocks for t in (sa, sb)),
+                      f"tensor {k}: 8-bit states are int8 and uint8 with fp32 scales [{blocks}]")
+            else:
+                _need(a.dtype == b.dtype == torch.float32 and sa is None and sb is None,
+                      f"tensor {k}: states are fp32 without scales, or int8 and uint8 with them")
+            at = self._array[k]
+            at.param, at.grad, at.m, at.v, at.n = p.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(), size
+            at.m_scale, at.v_scale, at.copy = (None if t is None else t.data_ptr() for t in (sa, sb, c))
+            at.param_dtype, at.grad_dtype, at.copy_dtype = _dtype(p), _dtype(g), F32 if c is None else _dtype(c)
+            at.state_bits = 8 if eight else 32
+
+
+def adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+               grad_scale=None, stream=None):
+    """One AdamW step.  step: the step's number from 1, or a device int64 [1] that
+    holds it; grad_scale: None or a device fp32 [1]."""
+    import torch
+    if tensors.device is not None:
+        _need(tensors.device.index == torch.cuda.current_device(), "tensors are not on the current device")
+    step_dev = None
+    if isinstance(step, torch.Tensor):
+        _need(step.dtype == torch.int64 and step.numel() == 1 and step.device == tensors.device,
+              "step must be a number or a device int64 [1]")
+        step, step_dev = 0, step.data_ptr()
+    if grad_scale is not None:
+        _need(grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == tensors.device,
+              "grad_scale must be a device fp32 [1]")
+        grad_scale = grad_scale.data_ptr()
+    hyper = AdamwHyper(lr, beta1, beta2, eps, weight_decay)
+    _check(_lib.rgnn_adamw_step(tensors._array, tensors._n, ctypes.byref(hyper), step, step_dev, grad_scale,
+                                _stream(stream)))
 
 
 def profile_enable(on: bool):
