@@ -50,6 +50,7 @@ struct WgradArgs {
 
 size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s);
+rgnn_status launch_linear_any(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s);
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s);
@@ -111,9 +112,8 @@ __device__ __forceinline__ f32x4 mma16<F32>(i32x4 a, i32x4 b, f32x4 c)
 
 // Rows [begin, end) of type t, with offsets that the host has not seen kept inside
 // [0, M): a table that is not monotone gives wrong rows, and no access out of range.
-__device__ __forceinline__ void type_rows(const int64_t *ptr, int t, int64_t M, int64_t &begin, int64_t &end)
+__device__ __forceinline__ void type_rows(int64_t p, int64_t q, int64_t M, int64_t &begin, int64_t &end)
 {
-    const int64_t p = ptr[t], q = ptr[t + 1];
     begin = p < 0 ? 0 : p > M ? M : p;
     end = q < begin ? begin : q > M ? M : q;
 }
@@ -144,15 +144,15 @@ __device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int 
     int64_t before = 0, wbefore = 0;
     for (int t0 = 0; t0 < T; t0 += 256) {
         int64_t b[4], e[4], c[4], w[4], cs = 0, ws = 0;
+        int64_t at[5];       // loads that depend on nothing, all at once
+#pragma unroll
+        for (int i = 0; i < 5; ++i) at[i] = ptr[min(t0 + lane * 4 + i, T)];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = t0 + lane * 4 + i;
-            b[i] = e[i] = c[i] = w[i] = 0;
-            if (t < T) {
-                type_rows(ptr, t, M, b[i], e[i]);
-                c[i] = count(e[i] - b[i]);
-                w[i] = weight(e[i] - b[i]);
-            }
+            const bool own = t0 + lane * 4 + i < T;
+            type_rows(at[i], at[i + 1], M, b[i], e[i]);
+            c[i] = own ? count(e[i] - b[i]) : 0;
+            w[i] = own ? weight(e[i] - b[i]) : 0;
             cs += c[i];
             ws += w[i];
         }
@@ -166,11 +166,11 @@ __device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int 
         if (want < before + total) {
             const uint64_t over = __ballot(before + ci > want);
             const int owner = __builtin_ctzll(over);
-            int64_t at = before + ci - cs, wat = wbefore + wi - ws;   // before this lane's first type
+            int64_t pat = before + ci - cs, wat = wbefore + wi - ws;   // before this lane's first type
             int k = 0;
 #pragma unroll
             for (int i = 0; i < 3; ++i)
-                if (k == i && at + c[i] <= want) { at += c[i]; wat += w[i]; k = i + 1; }
+                if (k == i && pat + c[i] <= want) { pat += c[i]; wat += w[i]; k = i + 1; }
             const int64_t bb = k == 0 ? b[0] : k == 1 ? b[1] : k == 2 ? b[2] : b[3];
             const int64_t ee = k == 0 ? e[0] : k == 1 ? e[1] : k == 2 ? e[2] : e[3];
             const int64_t cc = k == 0 ? c[0] : k == 1 ? c[1] : k == 2 ? c[2] : c[3];
@@ -178,7 +178,7 @@ __device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int 
             out.begin = uniform(__shfl(bb, owner));
             out.end = uniform(__shfl(ee, owner));
             out.count = uniform(__shfl(cc, owner));
-            out.index = want - uniform(__shfl(at, owner));
+            out.index = want - uniform(__shfl(pat, owner));
             out.before = uniform(__shfl(wat, owner));
             return true;
         }

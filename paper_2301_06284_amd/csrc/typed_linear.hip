@@ -1,6 +1,25 @@
 // typed_linear.hip -- the typed linear over ragged segments whose offsets lie on the
-// device: Y[scatter[i]] = X[gather[i]] W[t(i)], its weights as stored or transposed
-// (the input gradient), and the weight gradient dW[t] = X_t^T dY_t.
+// device: Y[scatter[i]] = X[gather[i]] W[t(i)], weights as stored or transposed (the
+// input gradient), and its 8-bit form.  The tiles of linear_any.hip take what does not
+// fill vectors of 16 bytes.
+//
+// A workgroup takes BM x BN outputs of one type and walks k in steps of 128 bytes of a row
+// (32 fp32, 64 16-bit or 128 8-bit values), which makes one kernel of all types: the same
+// rows in LDS, the same loads, and 16-byte chunks that feed the matrix cores in an order of
+// k that is the same for both operands.  Steps go straight from memory to LDS (16 bytes a
+// lane, no registers), the next one while this one is multiplied.
+//
+//   Rows of k (X, and W where its k lie side by side): LDS rows of 128 bytes; chunk c of
+//     row r lies at position c ^ ((r >> 1) & 7), so that the 16 rows that a fragment reads
+//     at one chunk lie in 16 different places of the 64 banks.  The loads write LDS in lane
+//     order, so it is their source address that is permuted.
+//   Rows of n (W as stored): LDS rows of BN values for each k.  16-bit fragments are read
+//     with the transposing LDS read: lane 4 r + c of 16 brings row k = r, columns 4 c, and
+//     lane n gets the four k of its column.  Units of 32 bytes are permuted by k so that the
+//     eight rows of half a wave lie in different banks.
+//
+// The product is formed as D[n][m], so that a lane holds four outputs side by side of one
+// row, and rows are written as whole 32-byte pieces.
 #include <algorithm>
 
 #include "linear_ops.h"
@@ -9,335 +28,389 @@ namespace rgnn {
 
 namespace {
 
-// ---------------------------------------------------------------- any sizes
-//
-// The form without any demand on sizes, strides and alignment: 64 x 64 outputs a
-// workgroup of four waves (32 x 32 each), both operands taken element by element into
-// LDS rows of 64 bytes of k, zero outside the matrix, and multiplied by the matrix
-// cores from there.  Bound by the element loads.
-
-constexpr int kAny = 64;         // outputs of a tile, each way
-constexpr int kAnyRow = 80;      // bytes of an LDS row: 64 of k and 16 against bank conflicts
-
-enum AnyOp { kForward, kTransposed, kWgrad };
-
-struct AnyArgs {
-    const void *A, *B;           // X (or X of the weight gradient); W or dY
-    int64_t a_rows, lda, b_rows, ldb;
-    const int32_t *a_index, *b_index;   // gather of X; of dY (weight gradient)
-    const int64_t *ptr;
-    int T;
-    int64_t M;
-    int K, N;                    // of the weights as the call names them
-    void *out;                   // Y or dW
-    int64_t out_rows, ldo;
-    const int32_t *scatter;
-    int out_f32;
-    int64_t chunk;               // weight gradient: rows of a piece
-    float *partial;              // and the sums of types with several pieces [slots, K, N]
-    int64_t slots;
-};
-
-template <class E>
-__device__ __forceinline__ void store_out(void *out, int64_t at, float v, int f32)
-{
-    if (f32) ((float *)out)[at] = v;
-    else ((E *)out)[at] = (E)v;
-}
-
-template <class T, int OP>
-__global__ __launch_bounds__(256, 2) void linear_any_kernel(AnyArgs a)
-{
-    typedef typename T::elem E;
-    constexpr int KE = 64 / sizeof(E);               // k of a step
-    constexpr int RE = kAnyRow / sizeof(E);
-    __shared__ __attribute__((aligned(16))) E sa[kAny * RE], sb[kAny * RE];
-    const E *A = (const E *)a.A, *B = (const E *)a.B;
-    const int ni = OP == kWgrad ? (a.K + kAny - 1) / kAny : 1;
-    const int nj = (a.N + kAny - 1) / kAny;
-    Piece p;
-    const int64_t chunk = a.chunk;
-    const int64_t per = (int64_t)ni * nj;
-    const bool any = OP == kWgrad
-        ? find_piece(a.ptr, a.T, a.M, blockIdx.x,
-                     [=](int64_t c) { return (c <= chunk ? 1 : (c + chunk - 1) / chunk) * per; },
-                     [=](int64_t c) { return c <= chunk ? 0 : (c + chunk - 1) / chunk; }, p)
-        : find_piece(a.ptr, a.T, a.M, blockIdx.x,
-                     [=](int64_t c) { return (c + kAny - 1) / kAny * nj; }, [](int64_t) { return 0; }, p);
-    if (!any) return;
-    const int64_t part = p.index / per;              // row tile, or piece of the contraction
-    const int64_t rest = p.index % per;
-    const int j0 = (int)(rest % nj) * kAny;
-    const int64_t i0 = OP == kWgrad ? rest / nj * kAny : p.begin + part * kAny;
-    const int64_t i1 = OP == kWgrad ? a.K : p.end;
-    const int64_t k0 = OP == kWgrad ? p.begin + part * chunk : 0;
-    const int64_t k1 = OP == kWgrad ? (k0 + chunk < p.end ? k0 + chunk : p.end) : a.K;
-    const E *W = B + (OP == kWgrad ? 0 : (int64_t)p.type * a.K * a.N);
-
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    f32x4 acc[2][2] = {};
-    for (int64_t ks = k0; ks < k1; ks += KE) {
-        // A: row i, k (forward: k along the lanes; weight gradient: i)
-        for (int x = tid; x < kAny * KE; x += 256) {
-            const int i = OP == kWgrad ? x % kAny : x / KE, k = OP == kWgrad ? x / kAny : x % KE;
-            E v = (E)0.0f;
-            if (i0 + i < i1 && ks + k < k1) {
-                int64_t row = OP == kWgrad ? ks + k : i0 + i;
-                const int64_t col = OP == kWgrad ? i0 + i : ks + k;
-                if (a.a_index) row = a.a_index[row];
-                if (row >= 0 && row < a.a_rows) v = A[row * a.lda + col];
-            }
-            sa[i * RE + k] = v;
-        }
-        for (int x = tid; x < kAny * KE; x += 256) {
-            const int j = OP == kTransposed ? x / KE : x % kAny, k = OP == kTransposed ? x % KE : x / kAny;
-            E v = (E)0.0f;
-            if (j0 + j < a.N && ks + k < k1) {
-                if (OP == kForward) v = W[(ks + k) * a.N + j0 + j];
-                else if (OP == kTransposed) v = W[(int64_t)(j0 + j) * a.K + ks + k];
-                else {
-                    int64_t row = ks + k;
-                    if (a.b_index) row = a.b_index[row];
-                    if (row >= 0 && row < a.b_rows) v = B[row * a.ldb + j0 + j];
-                }
-            }
-            sb[j * RE + k] = v;
-        }
-        __syncthreads();
-        const int r = lane & 15, c = lane >> 4;
-        i32x4 fa[2], fb[2];
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            fa[f] = *(const i32x4 *)((const char *)sa + ((wave >> 1) * 32 + f * 16 + r) * kAnyRow + c * 16);
-            fb[f] = *(const i32x4 *)((const char *)sb + ((wave & 1) * 32 + f * 16 + r) * kAnyRow + c * 16);
-        }
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) acc[f][h] = mma16<T>(fb[h], fa[f], acc[f][h]);
-        __syncthreads();
-    }
-    const bool split = OP == kWgrad && p.end - p.begin > chunk;
-    const int64_t slot = p.before + part;
-    if (split && slot >= a.slots) return;            // only where the offsets are not monotone
-#pragma unroll
-    for (int f = 0; f < 2; ++f) {
-        const int64_t i = i0 + (wave >> 1) * 32 + f * 16 + (lane & 15);
-        if (i >= i1) continue;
-        int64_t row = i;
-        if (OP != kWgrad) {
-            if (a.scatter) row = a.scatter[i];
-            if (row < 0 || row >= a.out_rows) continue;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int j = j0 + (wave & 1) * 32 + h * 16 + (lane >> 4) * 4 + q;
-                if (j >= a.N) continue;
-                if (OP != kWgrad) store_out<E>(a.out, row * a.ldo + j, acc[f][h][q], a.out_f32);
-                else if (split) a.partial[(slot * a.K + i) * a.N + j] = acc[f][h][q];
-                else store_out<E>(a.out, ((int64_t)p.type * a.K + i) * a.N + j, acc[f][h][q], a.out_f32);
-            }
-    }
-}
-
-// dW[t] of the types with several pieces: their sums in ascending order.
-template <class E>
-__global__ __launch_bounds__(256) void wgrad_join_kernel(const int64_t *ptr, int T, int64_t M, int64_t chunk,
-                                                         int64_t KN, const float *partial, int64_t slots,
-                                                         void *dW, int out_f32)
-{
-    Piece p;
-    if (!find_piece(ptr, T, M, blockIdx.y, [](int64_t) { return 1; },
-                    [=](int64_t c) { return c <= chunk ? 0 : (c + chunk - 1) / chunk; }, p))
-        return;
-    const int64_t n = (p.end - p.begin + chunk - 1) / chunk;
-    if (n <= 1 || p.before + n > slots) return;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < KN; i += (int64_t)gridDim.x * 256) {
-        const float *x = partial + p.before * KN + i;
-        float s = 0.0f;
-        for (int64_t c = 0; c < n; ++c) s += x[c * KN];
-        store_out<E>(dW, (int64_t)p.type * KN + i, s, out_f32);
-    }
-}
-
-// The 8-bit form: 64 x 64 outputs a workgroup, steps of 128 k, one scale block.  The
-// matrix instruction takes a scale byte for each lane's row; lane l brings the 16-byte
-// chunks l / 16 and l / 16 + 4 of its row, the same k for both operands.
-struct Fp8Args {
-    const uint8_t *X, *xs, *W, *ws;
-    int64_t x_rows;
+struct TileArgs {
+    const char *X;
+    int64_t x_rows, ldx;         // bytes of a row
     const int32_t *gather;
     const int64_t *ptr;
     int T;
     int64_t M;
-    int Kp, ks, N;
-    void *Y;
-    int64_t y_rows, ldy;
+    const char *W;
+    int64_t w_type, w_row;       // bytes of one type's weights, of one row of them
+    int K, N;
+    char *Y;
+    int64_t y_rows, ldy;         // ldy in elements
     const int32_t *scatter;
+    int y_f32, y_f16, y_vec;     // fp32 outputs; of 8-bit products fp16 ones; whole vectors of four are aligned
+    int window;                  // workgroups dealt to the XCDs at a time, over 8
+    const uint8_t *xs, *ws;      // fp8: scale bytes
+    int ks, nb;                  // bytes of a row's scales; 128-blocks of n
 };
 
-template <class E>
-__global__ __launch_bounds__(256, 2) void linear_fp8_kernel(Fp8Args a)
+__device__ const i32x4 kZeros = {0, 0, 0, 0};
+
+typedef const __attribute__((address_space(1))) uint32_t *global_ptr;
+typedef __attribute__((address_space(3))) uint32_t *lds_ptr;
+
+// 16 bytes of every lane's address to LDS, lane after lane from `lds` on
+__device__ __forceinline__ void load_lds(const char *from, char *lds)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t sa[64 * 144], sb[64 * 144];
-    const int nj = (a.N + 63) / 64;
+    __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)lds, 16, 0, 0);
+}
+
+// Every wave's loads into LDS have arrived and every wave is done with the step before.  The
+// barrier alone waits for LDS instructions only: loads into LDS count as loads.
+__device__ __forceinline__ void step_barrier()
+{
+    __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0)
+    __syncthreads();
+}
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
+__device__ __forceinline__ uint64_t read_turned(const char *lds)
+{
+    return __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)lds));
+}
+
+// How the 32-byte units (16-bit) or 64-byte units (fp32) of row k are permuted.
+template <class T, int BN>
+__device__ __forceinline__ int unit_turn(int k)
+{
+    if (sizeof(typename T::elem) == 4) return (k >> 2) & 3;
+    return BN >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);
+}
+
+struct F8 { typedef uint8_t elem; };
+
+// Order of a type's tiles: groups of 8 row tiles, in a group all row tiles of one column
+// tile after another, so that the tiles at work together share rows and weights in L2.
+__device__ __forceinline__ void tile_place(int q, int mt, int nt, int &m, int &n)
+{
+    const int group = q / (8 * nt), rest = q - group * 8 * nt;
+    const int gm = min(8, mt - group * 8);
+    n = rest / gm;
+    m = group * 8 + rest - n * gm;
+}
+
+// Four outputs side by side, or the first `n` of them.
+template <class O>
+__device__ __forceinline__ void write4(O *y, f32x4 v, bool whole, int n)
+{
+    O o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] = (O)v[q];
+    if (whole) {
+        if constexpr (sizeof(O) == 2) *(uint2 *)y = *(const uint2 *)o;
+        else *(i32x4 *)y = *(const i32x4 *)o;
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < n) y[q] = o[q];
+    }
+}
+
+template <class T, int BM, int BN, int WM, int WN, bool TRANS>
+__global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a)
+{
+    typedef typename T::elem E;
+    constexpr bool FP8 = sizeof(E) == 1;
+    constexpr int NW = WM * WN, KE = 128 / sizeof(E);
+    constexpr int FM = BM / WM / 16, FN = BN / WN / 16;     // fragments of a wave
+    constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;       // KB that a wave loads each step
+    static_assert(NA * 8 * NW == BM && NB * 8 * NW == BN, "whole loads");
+    __shared__ __attribute__((aligned(1024))) char sa0[BM * 128], sb0[BN * 128], sa1[BM * 128], sb1[BN * 128];
+
+    // deal the workgroups so that each XCD (which takes every eighth) has neighbouring tiles
+    const uint32_t span = a.window * 8, in = blockIdx.x % span;
+    const int64_t want = blockIdx.x - in + (in & 7) * a.window + (in >> 3);
+    const int nt = (a.N + BN - 1) / BN;
     Piece p;
-    if (!find_piece(a.ptr, a.T, a.M, blockIdx.x, [=](int64_t c) { return (c + 63) / 64 * nj; }, [](int64_t) { return 0; }, p))
+    if (!find_piece(a.ptr, a.T, a.M, want, [=](int64_t c) { return (c + BM - 1) / BM * nt; }, [](int64_t) { return 0; }, p))
         return;
-    const int64_t i0 = p.begin + p.index / nj * 64;
-    const int j0 = (int)(p.index % nj) * 64;
-    const uint8_t *W = a.W + (int64_t)p.type * a.N * a.Kp;
-    const int nb = (a.N + 127) / 128;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, c = lane >> 4;
-    auto row_of = [&](int64_t i) -> int64_t {
-        if (i >= p.end) return -1;
+    int mi, ni;
+    tile_place((int)p.index, (int)((p.end - p.begin + BM - 1) / BM), nt, mi, ni);
+    const int64_t i0 = p.begin + (int64_t)mi * BM;
+    const int j0 = ni * BN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, g = lane >> 4;
+
+    // ---- where this lane's loads come from
+    const char *zeros = (const char *)&kZeros;
+    const char *ap[NA], *bp[NB];
+    uint32_t aok = 0;                               // bit x: row x is one of X
+    int ac, bc;                                     // chunk of k (bytes / 16) of the loads of rows of k
+    {
+        const int pos = lane & 7, sub = lane >> 3;
+        ac = pos ^ ((((wave & 1) << 2) | (sub >> 1)) & 7);
+        bc = ac;
+        static_assert(NW % 2 == 0 || NW == 1, "slab parity is the wave's");
+    }
+#pragma unroll
+    for (int x = 0; x < NA; ++x) {
+        int64_t i = i0 + (x * NW + wave) * 8 + (lane >> 3);
+        if (i >= p.end) i = p.end - 1;              // its outputs are not written
         const int64_t row = a.gather ? a.gather[i] : i;
-        return row < a.x_rows ? row : -1;
+        const bool ok = row >= 0 && row < a.x_rows;
+        ap[x] = ok ? a.X + row * a.ldx + ac * 16 : zeros;
+        aok |= (ok ? 1u : 0u) << x;
+    }
+    const char *W = a.W + (int64_t)p.type * a.w_type;
+    int bk[NB];                                     // rows of n: the k of the load
+    const int64_t binc = TRANS ? 128 : KE * a.w_row;
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+        if (TRANS) {
+            const int j = min(j0 + (x * NW + wave) * 8 + (lane >> 3), a.N - 1);
+            bp[x] = W + (int64_t)j * a.w_row + bc * 16;
+            bk[x] = 0;
+        } else {
+            constexpr int CH = BN * sizeof(E) / 16;  // chunks of a row
+            const int at = (x * NW + wave) * 64 + lane;
+            const int k = at / CH, pos = at % CH;
+            constexpr int UC = sizeof(E) == 4 ? 4 : 2;   // chunks of a unit
+            const int c = (pos / UC ^ unit_turn<T, BN>(k)) * UC + pos % UC;
+            const int j = j0 + c * (16 / (int)sizeof(E));
+            bk[x] = k;
+            bp[x] = W + k * a.w_row + (j < a.N ? j : 0) * (int64_t)sizeof(E);
+        }
+    }
+    const int kbytes = a.K * (int)sizeof(E);
+    const int steps = (kbytes + 127) / 128;
+    // fp8: a word of scale bytes is four steps.  Those of the rows go through LDS, one row a
+    // lane; those of the weights are one for a wave, whose columns lie in one block of 128.
+    constexpr bool SCALES = FP8;
+    __shared__ __attribute__((aligned(256))) char sx0[SCALES ? BM * 4 : 4], sx1[SCALES ? BM * 4 : 4];
+    const char *xp = zeros;
+    int xinc = 0, sx[SCALES ? FM : 1], sw = 0;
+    const uint8_t *wp = nullptr;
+    if constexpr (SCALES) {
+        static_assert(BM / 64 <= NW && FN * 16 <= 128 && 128 % (FN * 16) == 0, "scales");
+        if (wave < BM / 64) {
+            int64_t i = i0 + wave * 64 + lane;
+            if (i >= p.end) i = p.end - 1;
+            const int64_t row = a.gather ? a.gather[i] : i;
+            if (row >= 0 && row < a.x_rows) { xp = (const char *)a.xs + row * a.ks; xinc = 4; }
+        }
+        const int jb = min(j0 + wave % WN * FN * 16, a.N - 1) / 128;
+        wp = a.ws + ((int64_t)p.type * a.nb + jb) * a.ks;
+    }
+    auto load = [&](char *sa, char *sb, int step) {
+        if constexpr (SCALES) {
+            if ((step & 3) == 0 && wave < BM / 64) {
+                char *to = step & 4 ? sx1 : sx0;
+                __builtin_amdgcn_global_load_lds((global_ptr)xp, (lds_ptr)(to + wave * 256), 4, 0, 0);
+                xp += xinc;
+            }
+        }
+        const bool tail = (step + 1) * 128 > kbytes;
+#pragma unroll
+        for (int x = 0; x < NA; ++x) {
+            const char *src = tail && step * 128 + ac * 16 >= kbytes ? zeros : ap[x];
+            load_lds(src, sa + (x * NW + wave) * 1024);
+            ap[x] += (aok >> x & 1) << 7;
+        }
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+            const bool out = TRANS ? step * 128 + bc * 16 >= kbytes : step * KE + bk[x] >= a.K;
+            load_lds(tail && out ? zeros : bp[x], sb + (x * NW + wave) * 1024);
+            bp[x] += binc;
+        }
     };
-    int64_t arow[2], xrow[2];
-    for (int f = 0; f < 2; ++f) {
-        arow[f] = row_of(i0 + (tid >> 3) + 32 * f);
-        xrow[f] = row_of(i0 + (wave >> 1) * 32 + f * 16 + r);
-    }
-    f32x4 acc[2][2] = {};
-    for (int k = 0; k < a.Kp; k += 128) {
-        for (int f = 0; f < 2; ++f) {
-            const int j = j0 + (tid >> 3) + 32 * f;
-            const i32x4 zero = {0, 0, 0, 0};
-            *(i32x4 *)(sa + ((tid >> 3) + 32 * f) * 144 + (tid & 7) * 16) =
-                arow[f] >= 0 ? *(const i32x4 *)(a.X + arow[f] * a.Kp + k + (tid & 7) * 16) : zero;
-            *(i32x4 *)(sb + ((tid >> 3) + 32 * f) * 144 + (tid & 7) * 16) =
-                j < a.N ? *(const i32x4 *)(W + (int64_t)j * a.Kp + k + (tid & 7) * 16) : zero;
+
+    // ---- where its fragments lie
+    const int wm = wave / WN, wn = wave % WN;
+    const int turn = (r16 >> 1) & 7;
+    int aoff[2], boff[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) aoff[q] = (wm * FM * 16 + r16) * 128 + (((g + 4 * q) ^ turn) * 16);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) boff[q] = (wn * FN * 16 + r16) * 128 + (((g + 4 * q) ^ turn) * 16);
+    int uoff[FN];                                   // rows of n
+    if (!TRANS) {
+        if (sizeof(E) == 2) {
+            const int r = (lane & 15) >> 2, c = lane & 3, k = g * 8 + r;
+#pragma unroll
+            for (int f = 0; f < FN; ++f) uoff[f] = k * BN * 2 + ((wn * FN + f) ^ unit_turn<T, BN>(k)) * 32 + c * 8;
+        } else {
+#pragma unroll
+            for (int f = 0; f < FN; ++f) uoff[f] = g * 4 * BN * 4 + ((wn * FN + f) ^ g) * 64 + r16 * 4;
         }
-        __syncthreads();
-        const int b = k / 128;
-        for (int f = 0; f < 2; ++f) {
-            const int sx = xrow[f] >= 0 ? a.xs[xrow[f] * a.ks + b] : 127;
-            const uint8_t *ra = sa + ((wave >> 1) * 32 + f * 16 + r) * 144 + c * 16;
-            const i32x4 a0 = *(const i32x4 *)ra, a1 = *(const i32x4 *)(ra + 64);
-            const i32x8 fa = {a0[0], a0[1], a0[2], a0[3], a1[0], a1[1], a1[2], a1[3]};
-            for (int h = 0; h < 2; ++h) {
-                const int j = j0 + (wave & 1) * 32 + h * 16;
-                const int sw = j < a.N ? a.ws[((int64_t)p.type * nb + j / 128) * a.ks + b] : 127;
-                const uint8_t *rb = sb + ((wave & 1) * 32 + h * 16 + r) * 144 + c * 16;
-                const i32x4 b0 = *(const i32x4 *)rb, b1 = *(const i32x4 *)(rb + 64);
-                const i32x8 fb = {b0[0], b0[1], b0[2], b0[3], b1[0], b1[1], b1[2], b1[3]};
-                acc[f][h] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa, acc[f][h], 0, 0, 0, sw, 0, sx);
+    }
+    f32x4 acc[FM][FN] = {};
+
+    // before the next loads are issued: a read of LDS that they might write would wait for them
+    auto scales = [&](int step) {
+        if constexpr (SCALES) {
+            if ((step & 3) == 0) {
+                const char *from = (step & 4 ? sx1 : sx0) + (wm * FM * 16 + r16) * 4;
+#pragma unroll
+                for (int f = 0; f < FM; ++f) sx[f] = *(const int *)(from + f * 64);
+                sw = *(const int *)(wp + step);
             }
         }
-        __syncthreads();
+    };
+    auto multiply = [&](const char *sa, const char *sb) {
+        if constexpr (FP8) {
+            i32x8 fb[FN];
+#pragma unroll
+            for (int f = 0; f < FN; ++f) {
+                const i32x4 x = *(const i32x4 *)(sb + boff[0] + f * 2048), y = *(const i32x4 *)(sb + boff[1] + f * 2048);
+                fb[f] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+#pragma unroll
+            for (int m = 0; m < FM; ++m) {
+                const i32x4 x = *(const i32x4 *)(sa + aoff[0] + m * 2048), y = *(const i32x4 *)(sa + aoff[1] + m * 2048);
+                const i32x8 fa = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int f = 0; f < FN; ++f)
+                    acc[m][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[f], fa, acc[m][f], 0, 0, 0, sw, 0, sx[m]);
+            }
+#pragma unroll
+            for (int f = 0; f < FM; ++f) sx[f] = (int)((uint32_t)sx[f] >> 8);
+            sw = (int)((uint32_t)sw >> 8);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                __builtin_amdgcn_sched_barrier(0);
+                i32x4 fb[FN], fa[FM];
+#pragma unroll
+                for (int f = 0; f < FN; ++f) {
+                    if constexpr (TRANS) fb[f] = *(const i32x4 *)(sb + boff[q] + f * 2048);
+                    else if constexpr (sizeof(E) == 2) {
+                        const uint64_t x = read_turned(sb + uoff[f] + q * 32 * BN * 2);
+                        const uint64_t y = read_turned(sb + uoff[f] + (q * 32 + 4) * BN * 2);
+                        fb[f] = i32x4{(int)x, (int)(x >> 32), (int)y, (int)(y >> 32)};
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) fb[f][i] = *(const int *)(sb + uoff[f] + (q * 16 + i) * BN * 4);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < FM; ++m) fa[m] = *(const i32x4 *)(sa + aoff[q] + m * 2048);
+#pragma unroll
+                for (int m = 0; m < FM; ++m)
+#pragma unroll
+                    for (int f = 0; f < FN; ++f) acc[m][f] = mma16<T>(fb[f], fa[m], acc[m][f]);
+            }
+        }
+    };
+
+    load(sa0, sb0, 0);
+    int step = 0;
+    for (; step + 2 <= steps; step += 2) {
+        step_barrier();
+        scales(step);
+        load(sa1, sb1, step + 1);
+        multiply(sa0, sb0);
+        step_barrier();
+        if (step + 2 < steps) load(sa0, sb0, step + 2);
+        multiply(sa1, sb1);
     }
-    for (int f = 0; f < 2; ++f) {
-        const int64_t i = i0 + (wave >> 1) * 32 + f * 16 + r;
-        if (i >= p.end) continue;
-        const int64_t row = a.scatter ? a.scatter[i] : i;
+    if (step < steps) {
+        step_barrier();
+        scales(step);
+        multiply(sa0, sb0);
+    }
+
+    // ---- write
+#pragma unroll
+    for (int m = 0; m < FM; ++m) {
+        const int64_t i = i0 + (wm * FM + m) * 16 + r16;
+        int64_t row = -1;
+        if (i < p.end) row = a.scatter ? a.scatter[i] : i;
         if (row < 0 || row >= a.y_rows) continue;
-        for (int h = 0; h < 2; ++h)
-            for (int q = 0; q < 4; ++q) {
-                const int j = j0 + (wave & 1) * 32 + h * 16 + c * 4 + q;
-                if (j < a.N) ((E *)a.Y)[row * a.ldy + j] = (E)acc[f][h][q];
-            }
+#pragma unroll
+        for (int f = 0; f < FN; ++f) {
+            const int j = j0 + (wn * FN + f) * 16 + g * 4;
+            if (j >= a.N) continue;
+            const int64_t at = row * a.ldy + j;
+            const bool whole = a.y_vec && j + 4 <= a.N;
+            if (sizeof(E) == 4 || a.y_f32) write4((float *)a.Y + at, acc[m][f], whole, a.N - j);
+            else if (FP8 && a.y_f16) write4((_Float16 *)a.Y + at, acc[m][f], whole, a.N - j);
+            else write4((typename std::conditional<FP8, __bf16, E>::type *)a.Y + at, acc[m][f], whole, a.N - j);
+        }
     }
 }
 
-template <int OP>
-bool launch_any(int dtype, const AnyArgs &k, int64_t grid, hipStream_t s)
+template <class T, int BM, int BN, int WM, int WN, bool TRANS>
+rgnn_status launch_tile(TileArgs k, hipStream_t s)
 {
-    switch (dtype) {
-    case RGNN_F32: hipLaunchKernelGGL((linear_any_kernel<F32, OP>), dim3((uint32_t)grid), dim3(256), 0, s, k); return true;
-    case RGNN_BF16: hipLaunchKernelGGL((linear_any_kernel<BF16, OP>), dim3((uint32_t)grid), dim3(256), 0, s, k); return true;
-    case RGNN_F16: hipLaunchKernelGGL((linear_any_kernel<F16, OP>), dim3((uint32_t)grid), dim3(256), 0, s, k); return true;
+    const int64_t tiles = row_tiles_bound(k.M, k.T, BM) * ((k.N + BN - 1) / BN);
+    // XCD windows of up to 32 tiles each, an eighth of the work at most
+    int window = 32;
+    while (window > 1 && (int64_t)window * 8 * 4 > tiles) window /= 2;
+    k.window = window;
+    const int64_t grid = (tiles + window * 8 - 1) / (window * 8) * (window * 8);
+    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
+    hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
+    return RGNN_OK;
+}
+
+template <class T, bool TRANS>
+rgnn_status launch_shape(const TileArgs &k, hipStream_t s)
+{
+    const int64_t rows = k.M / std::min<int64_t>(std::max<int64_t>(k.M, 1), k.T);   // of a type, on average
+    if constexpr (sizeof(typename T::elem) == 4) return launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
+    else {
+        if (k.N <= 64) return launch_tile<T, 256, 64, 4, 1, TRANS>(k, s);
+        if (rows <= 64) return launch_tile<T, 64, 128, 1, 4, TRANS>(k, s);
+        if (rows <= 192 || k.N <= 128) return launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
+        return launch_tile<T, 256, 256, 2, 4, TRANS>(k, s);
     }
-    return false;
 }
 
-// Pieces of the weight gradient's contraction: about kPiecesWanted over all output tiles,
-// of at least kLeastPiece rows, which amortise the piece's sums written and read back.
-constexpr int64_t kPiecesWanted = 1024, kLeastPiece = 1024;
-
-int64_t wgrad_tiles(int32_t K, int32_t N) { return (int64_t)((K + kAny - 1) / kAny) * ((N + kAny - 1) / kAny); }
-
-int64_t wgrad_chunk(int64_t M, int32_t K, int32_t N)
+TileArgs tile_args(const LinearArgs &a)
 {
-    return std::max<int64_t>(kLeastPiece, (M * wgrad_tiles(K, N) + kPiecesWanted - 1) / kPiecesWanted);
-}
-
-// Pieces of types with more rows than a piece, at most: there ceil(c / chunk) <= 2 c / chunk,
-// so 2 M / chunk over all.  Written so that it never falls as M grows.
-int64_t wgrad_slots(int64_t M, int32_t K, int32_t N)
-{
-    return std::min(2 * M / kLeastPiece, 2 * kPiecesWanted / wgrad_tiles(K, N));
+    const int el = dtype_bytes(a.dtype), yel = dtype_bytes(a.y_dtype);
+    TileArgs k{};
+    k.X = (const char *)a.X; k.x_rows = a.x_rows; k.ldx = a.ldx * el; k.gather = a.gather;
+    k.ptr = a.type_ptr; k.T = a.T; k.M = a.M;
+    k.W = (const char *)a.W; k.K = a.K; k.N = a.N;
+    k.w_row = (int64_t)(a.trans_w ? a.K : a.N) * el;
+    k.w_type = (int64_t)a.K * a.N * el;
+    k.Y = (char *)a.Y; k.y_rows = a.y_rows; k.ldy = a.ldy; k.scatter = a.scatter;
+    k.y_f32 = a.y_dtype == RGNN_F32;
+    k.y_vec = (uintptr_t)a.Y % (4 * yel) == 0 && a.ldy % 4 == 0;
+    return k;
 }
 
 }  // namespace
 
-size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
-{
-    return (size_t)wgrad_slots(M, K, N) * K * N * sizeof(float);
-}
-
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s)
 {
-    AnyArgs k{};
-    k.A = a.X; k.a_rows = a.x_rows; k.lda = a.ldx; k.a_index = a.gather;
-    k.B = a.W;
-    k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
-    k.out = a.Y; k.out_rows = a.y_rows; k.ldo = a.ldy; k.scatter = a.scatter;
-    k.out_f32 = a.y_dtype == RGNN_F32;
-    const int64_t grid = row_tiles_bound(a.M, a.T, kAny) * ((a.N + kAny - 1) / kAny);
-    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
+    const int el = dtype_bytes(a.dtype);
+    const bool whole = (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.W % 16 == 0 && a.ldx * el % 16 == 0 &&
+                       (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
+    if (!whole) return launch_linear_any(a, s);
+    const TileArgs k = tile_args(a);
+    rgnn_status st;
     {
-        LaunchScope ls("typed_linear_any", s);
-        if (!(a.trans_w ? launch_any<kTransposed>(a.dtype, k, grid, s) : launch_any<kForward>(a.dtype, k, grid, s)))
-            return fail(RGNN_EUNSUPPORTED, "typed linear: unsupported type");
+        LaunchScope ls("typed_linear", s);
+        if (a.dtype == RGNN_F32) st = a.trans_w ? launch_shape<F32, true>(k, s) : launch_shape<F32, false>(k, s);
+        else if (a.dtype == RGNN_BF16) st = a.trans_w ? launch_shape<BF16, true>(k, s) : launch_shape<BF16, false>(k, s);
+        else st = a.trans_w ? launch_shape<F16, true>(k, s) : launch_shape<F16, false>(k, s);
     }
+    if (st != RGNN_OK) return st;
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_linear launch");
 }
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s)
 {
-    Fp8Args k{(const uint8_t *)a.X, a.x_scale, (const uint8_t *)a.W, a.w_scale, a.x_rows, a.gather, a.type_ptr, a.T, a.M,
-              fp8_width(a.K), fp8_scales(a.K), a.N, a.Y, a.y_rows, a.ldy, a.scatter};
-    const int64_t grid = row_tiles_bound(a.M, a.T, 64) * ((a.N + 63) / 64);
-    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
+    TileArgs k = tile_args(a);
+    k.K = fp8_width(a.K);
+    k.w_row = k.K; k.w_type = (int64_t)k.K * a.N;
+    k.xs = a.x_scale; k.ws = a.w_scale; k.ks = fp8_scales(a.K); k.nb = (a.N + 127) / 128;
+    k.y_f16 = a.y_dtype == RGNN_F16;
+    rgnn_status st;
     {
         LaunchScope ls("typed_linear_fp8", s);
-        if (a.y_dtype == RGNN_F32) hipLaunchKernelGGL((linear_fp8_kernel<float>), dim3((uint32_t)grid), dim3(256), 0, s, k);
-        else if (a.y_dtype == RGNN_BF16) hipLaunchKernelGGL((linear_fp8_kernel<__bf16>), dim3((uint32_t)grid), dim3(256), 0, s, k);
-        else hipLaunchKernelGGL((linear_fp8_kernel<_Float16>), dim3((uint32_t)grid), dim3(256), 0, s, k);
+        st = launch_shape<F8, true>(k, s);
     }
+    if (st != RGNN_OK) return st;
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_linear_fp8 launch");
-}
-
-rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
-{
-    const int64_t chunk = wgrad_chunk(a.M, a.K, a.N), slots = wgrad_slots(a.M, a.K, a.N);
-    AnyArgs k{};
-    k.A = a.X; k.a_rows = a.x_rows; k.lda = a.ldx; k.a_index = a.gather;
-    k.B = a.dY; k.b_rows = a.dy_rows; k.ldb = a.lddy; k.b_index = a.dy_gather;
-    k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
-    k.out = a.dW; k.out_f32 = a.dw_dtype == RGNN_F32;
-    k.chunk = chunk; k.partial = (float *)a.ws; k.slots = slots;
-    const int64_t grid = (a.T + slots) * wgrad_tiles(a.K, a.N);
-    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    {
-        LaunchScope ls("typed_wgrad_any", s);
-        if (!launch_any<kWgrad>(a.dtype, k, grid, s)) return fail(RGNN_EUNSUPPORTED, "weight gradient: unsupported type");
-    }
-    if (slots > 0) {
-        const int64_t kn = (int64_t)a.K * a.N;
-        const dim3 g((uint32_t)std::min<int64_t>((kn + 255) / 256, 4096), (uint32_t)a.T);
-        LaunchScope ls("typed_wgrad_join", s);
-        if (a.dtype == RGNN_BF16) hipLaunchKernelGGL((wgrad_join_kernel<__bf16>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, chunk, kn, k.partial, slots, a.dW, k.out_f32);
-        else if (a.dtype == RGNN_F16) hipLaunchKernelGGL((wgrad_join_kernel<_Float16>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, chunk, kn, k.partial, slots, a.dW, k.out_f32);
-        else hipLaunchKernelGGL((wgrad_join_kernel<float>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, chunk, kn, k.partial, slots, a.dW, k.out_f32);
-    }
-    hipError_t e = hipGetLastError();
-    return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_wgrad launch");
 }
 
 }  // namespace rgnn
