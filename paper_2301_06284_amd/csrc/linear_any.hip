@@ -141,26 +141,6 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(AnyArgs a)
     }
 }
 
-// dW[t] of the types with several pieces: their sums in ascending order.
-template <class E>
-__global__ __launch_bounds__(256) void wgrad_join_kernel(const int64_t *ptr, int T, int64_t M, int64_t chunk,
-                                                         int64_t KN, const float *partial, int64_t slots,
-                                                         void *dW, int out_f32)
-{
-    Piece p;
-    if (!find_piece(ptr, T, M, blockIdx.y, [](int64_t) { return 1; },
-                    [=](int64_t c) { return c <= chunk ? 0 : (c + chunk - 1) / chunk; }, p))
-        return;
-    const int64_t n = (p.end - p.begin + chunk - 1) / chunk;
-    if (n <= 1 || p.before + n > slots) return;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < KN; i += (int64_t)gridDim.x * 256) {
-        const float *x = partial + p.before * KN + i;
-        float s = 0.0f;
-        for (int64_t c = 0; c < n; ++c) s += x[c * KN];
-        store_out<E>(dW, (int64_t)p.type * KN + i, s, out_f32);
-    }
-}
-
 template <int OP>
 bool launch_any(int dtype, const AnyArgs &k, int64_t grid, hipStream_t s)
 {
@@ -172,30 +152,7 @@ bool launch_any(int dtype, const AnyArgs &k, int64_t grid, hipStream_t s)
     return false;
 }
 
-// Pieces of the weight gradient's contraction: about kPiecesWanted over all output tiles,
-// of at least kLeastPiece rows, which amortise the piece's sums written and read back.
-constexpr int64_t kPiecesWanted = 1024, kLeastPiece = 1024;
-
-int64_t wgrad_tiles(int32_t K, int32_t N) { return (int64_t)((K + kAny - 1) / kAny) * ((N + kAny - 1) / kAny); }
-
-int64_t wgrad_chunk(int64_t M, int32_t K, int32_t N)
-{
-    return std::max<int64_t>(kLeastPiece, (M * wgrad_tiles(K, N) + kPiecesWanted - 1) / kPiecesWanted);
-}
-
-// Pieces of types with more rows than a piece, at most: there ceil(c / chunk) <= 2 c / chunk,
-// so 2 M / chunk over all.  Written so that it never falls as M grows.
-int64_t wgrad_slots(int64_t M, int32_t K, int32_t N)
-{
-    return std::min(2 * M / kLeastPiece, 2 * kPiecesWanted / wgrad_tiles(K, N));
-}
-
 }  // namespace
-
-size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
-{
-    return (size_t)wgrad_slots(M, K, N) * K * N * sizeof(float);
-}
 
 rgnn_status launch_linear_any(const LinearArgs &a, hipStream_t s)
 {
@@ -216,28 +173,20 @@ rgnn_status launch_linear_any(const LinearArgs &a, hipStream_t s)
     return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_linear launch");
 }
 
-rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
+rgnn_status launch_wgrad_any(const WgradArgs &a, const WgradPlan &plan, hipStream_t s)
 {
-    const int64_t chunk = wgrad_chunk(a.M, a.K, a.N), slots = wgrad_slots(a.M, a.K, a.N);
     AnyArgs k{};
     k.A = a.X; k.a_rows = a.x_rows; k.lda = a.ldx; k.a_index = a.gather;
     k.B = a.dY; k.b_rows = a.dy_rows; k.ldb = a.lddy; k.b_index = a.dy_gather;
     k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
     k.out = a.dW; k.out_f32 = a.dw_dtype == RGNN_F32;
-    k.chunk = chunk; k.partial = (float *)a.ws; k.slots = slots;
-    const int64_t grid = (a.T + slots) * wgrad_tiles(a.K, a.N);
+    k.chunk = plan.chunk; k.partial = (float *)a.ws; k.slots = plan.slots;
+    const int64_t tiles = (int64_t)((a.K + kAny - 1) / kAny) * ((a.N + kAny - 1) / kAny);
+    const int64_t grid = (a.T + plan.slots) * tiles;
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
     {
         LaunchScope ls("typed_wgrad_any", s);
         if (!launch_any<kWgrad>(a.dtype, k, grid, s)) return fail(RGNN_EUNSUPPORTED, "weight gradient: unsupported type");
-    }
-    if (slots > 0) {
-        const int64_t kn = (int64_t)a.K * a.N;
-        const dim3 g((uint32_t)std::min<int64_t>((kn + 255) / 256, 4096), (uint32_t)a.T);
-        LaunchScope ls("typed_wgrad_join", s);
-        if (a.dtype == RGNN_BF16) hipLaunchKernelGGL((wgrad_join_kernel<__bf16>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, chunk, kn, k.partial, slots, a.dW, k.out_f32);
-        else if (a.dtype == RGNN_F16) hipLaunchKernelGGL((wgrad_join_kernel<_Float16>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, chunk, kn, k.partial, slots, a.dW, k.out_f32);
-        else hipLaunchKernelGGL((wgrad_join_kernel<float>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, chunk, kn, k.partial, slots, a.dW, k.out_f32);
     }
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_wgrad launch");

@@ -48,6 +48,14 @@ struct WgradArgs {
     void *ws = nullptr;
 };
 
+// How the weight gradient's contraction is cut: pieces of `chunk` rows of a type, and how many
+// pieces the types with more rows than one have, at most (their sums go through the workspace).
+struct WgradPlan {
+    int bk = 0, bn = 0;          // the tile
+    int64_t chunk = 0, slots = 0;
+};
+WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
+rgnn_status launch_wgrad_any(const WgradArgs &a, const WgradPlan &plan, hipStream_t s);
 size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_linear_any(const LinearArgs &a, hipStream_t s);

@@ -22,7 +22,7 @@
 // row, and rows are written as whole 32-byte pieces.
 #include <algorithm>
 
-#include "linear_ops.h"
+#include "linear_tiles.h"
 
 namespace rgnn {
 
@@ -47,68 +47,7 @@ struct TileArgs {
     int ks, nb;                  // bytes of a row's scales; 128-blocks of n
 };
 
-__device__ const i32x4 kZeros = {0, 0, 0, 0};
-
-typedef const __attribute__((address_space(1))) uint32_t *global_ptr;
-typedef __attribute__((address_space(3))) uint32_t *lds_ptr;
-
-// 16 bytes of every lane's address to LDS, lane after lane from `lds` on
-__device__ __forceinline__ void load_lds(const char *from, char *lds)
-{
-    __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)lds, 16, 0, 0);
-}
-
-// Every wave's loads into LDS have arrived and every wave is done with the step before.  The
-// barrier alone waits for LDS instructions only: loads into LDS count as loads.
-__device__ __forceinline__ void step_barrier()
-{
-    __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0)
-    __syncthreads();
-}
-
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
-__device__ __forceinline__ uint64_t read_turned(const char *lds)
-{
-    return __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)lds));
-}
-
-// How the 32-byte units (16-bit) or 64-byte units (fp32) of row k are permuted.
-template <class T, int BN>
-__device__ __forceinline__ int unit_turn(int k)
-{
-    if (sizeof(typename T::elem) == 4) return (k >> 2) & 3;
-    return BN >= 128 ? (k & 3) | ((k >> 1) & 4) : ((k >> 1) & 1) | ((k >> 2) & 2);
-}
-
 struct F8 { typedef uint8_t elem; };
-
-// Order of a type's tiles: groups of 8 row tiles, in a group all row tiles of one column
-// tile after another, so that the tiles at work together share rows and weights in L2.
-__device__ __forceinline__ void tile_place(int q, int mt, int nt, int &m, int &n)
-{
-    const int group = q / (8 * nt), rest = q - group * 8 * nt;
-    const int gm = min(8, mt - group * 8);
-    n = rest / gm;
-    m = group * 8 + rest - n * gm;
-}
-
-// Four outputs side by side, or the first `n` of them.
-template <class O>
-__device__ __forceinline__ void write4(O *y, f32x4 v, bool whole, int n)
-{
-    O o[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) o[q] = (O)v[q];
-    if (whole) {
-        if constexpr (sizeof(O) == 2) *(uint2 *)y = *(const uint2 *)o;
-        else *(i32x4 *)y = *(const i32x4 *)o;
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < n) y[q] = o[q];
-    }
-}
 
 template <class T, int BM, int BN, int WM, int WN, bool TRANS>
 __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a)
@@ -121,9 +60,7 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     static_assert(NA * 8 * NW == BM && NB * 8 * NW == BN, "whole loads");
     __shared__ __attribute__((aligned(1024))) char sa0[BM * 128], sb0[BN * 128], sa1[BM * 128], sb1[BN * 128];
 
-    // deal the workgroups so that each XCD (which takes every eighth) has neighbouring tiles
-    const uint32_t span = a.window * 8, in = blockIdx.x % span;
-    const int64_t want = blockIdx.x - in + (in & 7) * a.window + (in >> 3);
+    const int64_t want = xcd_tile(a.window);
     const int nt = (a.N + BN - 1) / BN;
     Piece p;
     if (!find_piece(a.ptr, a.T, a.M, want, [=](int64_t c) { return (c + BM - 1) / BM * nt; }, [](int64_t) { return 0; }, p))
@@ -337,11 +274,8 @@ template <class T, int BM, int BN, int WM, int WN, bool TRANS>
 rgnn_status launch_tile(TileArgs k, hipStream_t s)
 {
     const int64_t tiles = row_tiles_bound(k.M, k.T, BM) * ((k.N + BN - 1) / BN);
-    // XCD windows of up to 32 tiles each, an eighth of the work at most
-    int window = 32;
-    while (window > 1 && (int64_t)window * 8 * 4 > tiles) window /= 2;
-    k.window = window;
-    const int64_t grid = (tiles + window * 8 - 1) / (window * 8) * (window * 8);
+    k.window = xcd_window(tiles);
+    const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
     hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
     return RGNN_OK;

@@ -1,0 +1,326 @@
+// typed_wgrad.hip -- the weight gradient of the typed linear over ragged segments,
+// dW[t] = sum over the positions i of type t of X[gather[i]]^T dY[dy_gather[i]].
+//
+// A workgroup takes BK x BN values of one type's gradient and walks the type's positions in
+// steps of 64 (fp32: 32), a row of X and of dY each, straight from memory to LDS, the next
+// step while this one is multiplied.  Both operands have the contraction across the rows,
+// so 16-bit fragments are read with the transposing LDS read (the layout of "rows of n" in
+// typed_linear.hip).
+//
+// A type with more positions than a piece (WgradPlan) is cut into pieces whose sums, in
+// fp32, go through the workspace and are added in ascending order by a second kernel: no
+// atomics, the same result every time.
+#include <algorithm>
+
+#include "linear_tiles.h"
+
+namespace rgnn {
+
+namespace {
+
+struct WgradK {
+    const char *X, *dY;
+    int64_t x_rows, ldx, dy_rows, lddy;   // ld in bytes
+    const int32_t *gather, *dy_gather;
+    const int64_t *ptr;
+    int T;
+    int64_t M;
+    int K, N;
+    void *dW;
+    int f32, vec;                // fp32 gradients; whole vectors of four are aligned
+    int64_t chunk, slots;
+    float *partial;
+    int window;
+};
+
+__host__ __device__ constexpr int64_t pieces_of(int64_t rows, int64_t chunk) { return rows <= chunk ? 1 : (rows + chunk - 1) / chunk; }
+__host__ __device__ constexpr int64_t slots_of(int64_t rows, int64_t chunk) { return rows <= chunk ? 0 : (rows + chunk - 1) / chunk; }
+
+// One operand's loads: rows of the contraction, B columns from c0 on.
+template <class T, int B, int NW>
+struct Side {
+    typedef typename T::elem E;
+    static constexpr int KE = 128 / sizeof(E), L = B / 8 / NW, CH = B * sizeof(E) / 16, UC = sizeof(E) == 4 ? 4 : 2;
+    static_assert(L * 8 * NW == B, "whole loads");
+    const char *base;
+    const int32_t *index;
+    int64_t rows, ld, pos, end;  // pos: the position of this lane's first load of the next step
+    int col[L];                  // bytes
+    int next[L];                 // indices of the next step's rows
+    int wave;
+
+    __device__ __forceinline__ static int row_of(int x, int wave, int lane) { return ((x * NW + wave) * 64 + lane) / CH; }
+
+    __device__ __forceinline__ void init(const char *m, const int32_t *idx, int64_t m_rows, int64_t m_ld, int64_t p0, int64_t p1, int c0,
+                                         int width, int w, int lane)
+    {
+        base = m; index = idx; rows = m_rows; ld = m_ld; pos = p0; end = p1; wave = w;
+#pragma unroll
+        for (int x = 0; x < L; ++x) {
+            const int at = (x * NW + w) * 64 + lane, k = at / CH, p = at % CH;
+            const int c = ((p / UC) ^ unit_turn<T, B>(k)) * UC + p % UC;
+            const int j = c0 + c * (16 / (int)sizeof(E));
+            col[x] = (j < width ? j : 0) * (int)sizeof(E);
+        }
+        fetch(lane);
+    }
+    __device__ __forceinline__ void fetch(int lane)
+    {
+        if (!index) return;
+#pragma unroll
+        for (int x = 0; x < L; ++x) {
+            const int64_t i = pos + row_of(x, wave, lane);
+            next[x] = i < end ? index[i] : -1;
+        }
+    }
+    __device__ __forceinline__ void load(char *lds, int lane)
+    {
+#pragma unroll
+        for (int x = 0; x < L; ++x) {
+            const int64_t i = pos + row_of(x, wave, lane);
+            const int64_t row = index ? (int64_t)next[x] : i;
+            const bool ok = i < end && row >= 0 && row < rows;
+            load_lds(ok ? base + row * ld + col[x] : (const char *)&kZeros, lds + (x * NW + wave) * 1024);
+        }
+        pos += KE;
+        fetch(lane);
+    }
+};
+
+template <class T, int BK, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
+{
+    typedef typename T::elem E;
+    constexpr int NW = WM * WN, KE = 128 / sizeof(E);
+    constexpr int FM = BK / WM / 16, FN = BN / WN / 16;
+    __shared__ __attribute__((aligned(1024))) char sx0[BK * 128], sy0[BN * 128], sx1[BK * 128], sy1[BN * 128];
+
+    const int nk = (a.K + BK - 1) / BK, nn = (a.N + BN - 1) / BN, per = nk * nn;
+    const int64_t chunk = a.chunk;
+    Piece p;
+    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return pieces_of(c, chunk) * per; },
+                    [=](int64_t c) { return slots_of(c, chunk); }, p))
+        return;
+    const int part = (int)(p.index / per);
+    int ki, ni;
+    tile_place((int)(p.index - (int64_t)part * per), nk, nn, ki, ni);
+    const int64_t p0 = p.begin + part * chunk;
+    const int64_t p1 = p0 + chunk < p.end ? p0 + chunk : p.end;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, g = lane >> 4, wm = wave / WN, wn = wave % WN;
+
+    Side<T, BK, NW> x;
+    Side<T, BN, NW> y;
+    x.init(a.X, a.gather, a.x_rows, a.ldx, p0, p1, ki * BK, a.K, wave, lane);
+    y.init(a.dY, a.dy_gather, a.dy_rows, a.lddy, p0, p1, ni * BN, a.N, wave, lane);
+
+    // fragment f lies at (units before the wave's) + (f ^ turn): the turn sits in the address
+    // bits of the units, so an exclusive or with f's bits moves from fragment to fragment
+    constexpr int UB = sizeof(E) == 2 ? 32 : 64;
+    const int kr = sizeof(E) == 2 ? g * 8 + (r16 >> 2) : g * 4, in = sizeof(E) == 2 ? (r16 & 3) * 8 : r16 * 4;
+    static_assert((FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0, "powers of two");
+    int xat = (kr * BK * (int)sizeof(E) + in) | ((wm * FM) ^ unit_turn<T, BK>(kr)) * UB;
+    int yat = (kr * BN * (int)sizeof(E) + in) | ((wn * FN) ^ unit_turn<T, BN>(kr)) * UB;
+    f32x4 acc[FM][FN] = {};
+    auto fragment = [&](const char *lds, int off, int q, int width) -> i32x4 {
+        if constexpr (sizeof(E) == 2) {
+            const uint64_t u = read_turned(lds + off + q * 32 * width * 2), v = read_turned(lds + off + (q * 32 + 4) * width * 2);
+            return i32x4{(int)u, (int)(u >> 32), (int)v, (int)(v >> 32)};
+        } else {
+            i32x4 r;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = *(const int *)(lds + off + (q * 16 + i) * width * 4);
+            return r;
+        }
+    };
+    auto multiply = [&](const char *sx, const char *sy) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" : "+v"(xat), "+v"(yat));   // the fragments' addresses are made here, not kept in registers
+            i32x4 fx[FM], fy[FN];
+#pragma unroll
+            for (int f = 0; f < FN; ++f) fy[f] = fragment(sy, yat ^ f * UB, q, BN);
+#pragma unroll
+            for (int f = 0; f < FM; ++f) fx[f] = fragment(sx, xat ^ f * UB, q, BK);
+#pragma unroll
+            for (int m = 0; m < FM; ++m)
+#pragma unroll
+                for (int f = 0; f < FN; ++f) acc[m][f] = mma16<T>(fy[f], fx[m], acc[m][f]);
+        }
+    };
+
+    const int steps = (int)((p1 - p0 + KE - 1) / KE);
+    if (steps > 0) {
+        x.load(sx0, lane);
+        y.load(sy0, lane);
+    }
+    int step = 0;
+    for (; step + 2 <= steps; step += 2) {
+        step_barrier();
+        x.load(sx1, lane);
+        y.load(sy1, lane);
+        multiply(sx0, sy0);
+        step_barrier();
+        if (step + 2 < steps) {
+            x.load(sx0, lane);
+            y.load(sy0, lane);
+        }
+        multiply(sx1, sy1);
+    }
+    if (step < steps) {
+        step_barrier();
+        multiply(sx0, sy0);
+    }
+
+    const bool split = p.end - p.begin > chunk;
+    const int64_t slot = p.before + part;
+    if (split && slot >= a.slots) return;            // only where the offsets are not monotone
+    const int64_t at0 = (split ? slot : (int64_t)p.type) * a.K;
+#pragma unroll
+    for (int m = 0; m < FM; ++m) {
+        const int k = ki * BK + (wm * FM + m) * 16 + r16;
+        if (k >= a.K) continue;
+#pragma unroll
+        for (int f = 0; f < FN; ++f) {
+            const int n = ni * BN + (wn * FN + f) * 16 + g * 4;
+            if (n >= a.N) continue;
+            const int64_t at = (at0 + k) * a.N + n;
+            const bool whole = a.vec && n + 4 <= a.N;
+            if (split) write4(a.partial + at, acc[m][f], whole, a.N - n);
+            else if (sizeof(E) == 4 || a.f32) write4((float *)a.dW + at, acc[m][f], whole, a.N - n);
+            else write4((E *)a.dW + at, acc[m][f], whole, a.N - n);
+        }
+    }
+}
+
+// dW[t] of the types with several pieces.  A workgroup takes 64 V values of one type's gradient
+// at a time and adds a quarter of the pieces in each wave, then the quarters.
+template <class E, int V>
+__global__ __launch_bounds__(256) void wgrad_join_kernel(const int64_t *ptr, int T, int64_t M, int64_t chunk, int64_t KN,
+                                                         const float *partial, int64_t slots, void *dW, int out_f32)
+{
+    typedef float vec __attribute__((ext_vector_type(V)));
+    __shared__ vec sums[4][64];
+    Piece p;
+    if (!find_piece(ptr, T, M, blockIdx.y, [](int64_t) { return 1; }, [=](int64_t c) { return slots_of(c, chunk); }, p)) return;
+    const int64_t n = slots_of(p.end - p.begin, chunk);
+    if (n == 0 || p.before + n > slots) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t quarter = (n + 3) / 4, c0 = min(wave * quarter, n), c1 = min(c0 + quarter, n);
+    for (int64_t i0 = blockIdx.x * (int64_t)(64 * V); i0 < KN; i0 += (int64_t)gridDim.x * (64 * V)) {
+        const int64_t i = i0 + lane * V;
+        vec s = 0.0f;
+        if (i < KN) {
+            const float *x = partial + p.before * KN + i;
+#pragma unroll 4
+            for (int64_t c = c0; c < c1; ++c) s += *(const vec *)(x + c * KN);
+        }
+        sums[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && i < KN) {
+            s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            const int64_t at = p.type * KN + i;
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                if (out_f32) ((float *)dW)[at + q] = s[q];
+                else ((E *)dW)[at + q] = (E)s[q];
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <class E>
+void launch_join(const WgradArgs &a, const WgradPlan &plan, hipStream_t s)
+{
+    const int64_t kn = (int64_t)a.K * a.N;
+    const int v = kn % 4 == 0 ? 4 : 1;
+    // a workgroup looks for its type first: few of them for many types
+    const int64_t most = std::max<int64_t>(1, 4096 / a.T);
+    const dim3 g((uint32_t)std::min((kn + 64 * v - 1) / (64 * v), most), (uint32_t)a.T);
+    const int f32 = a.dw_dtype == RGNN_F32;
+    const float *part = (const float *)a.ws;
+    LaunchScope ls("typed_wgrad_join", s);
+    if (v == 4) hipLaunchKernelGGL((wgrad_join_kernel<E, 4>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, plan.chunk, kn, part, plan.slots, a.dW, f32);
+    else hipLaunchKernelGGL((wgrad_join_kernel<E, 1>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, plan.chunk, kn, part, plan.slots, a.dW, f32);
+}
+
+template <class T, int BK, int BN, int WM, int WN>
+rgnn_status launch_tile(WgradK k, hipStream_t s)
+{
+    const int64_t tiles = (k.T + k.slots) * ((k.K + BK - 1) / BK) * ((k.N + BN - 1) / BN);
+    k.window = xcd_window(tiles);
+    const int64_t grid = xcd_grid(tiles, k.window);
+    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
+    hipLaunchKernelGGL((typed_wgrad_kernel<T, BK, BN, WM, WN>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
+    return RGNN_OK;
+}
+
+template <class T>
+rgnn_status launch_shape(const WgradK &k, const WgradPlan &p, hipStream_t s)
+{
+    if constexpr (sizeof(typename T::elem) == 2)
+        if (p.bk == 256) return launch_tile<T, 256, 256, 2, 4>(k, s);
+    if (p.bk == 128 && p.bn == 128) return launch_tile<T, 128, 128, 2, 2>(k, s);
+    if (p.bk == 128) return launch_tile<T, 128, 64, 2, 2>(k, s);
+    if (p.bn == 128) return launch_tile<T, 64, 128, 2, 2>(k, s);
+    return launch_tile<T, 64, 64, 2, 2>(k, s);
+}
+
+}  // namespace
+
+WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
+{
+    WgradPlan p;
+    p.bk = K <= 64 ? 64 : 128;
+    p.bn = N <= 64 ? 64 : 128;
+    auto tiles = [&]() { return (int64_t)((K + p.bk - 1) / p.bk) * ((N + p.bn - 1) / p.bn); };
+    // the widest tile where its tiles alone fill the chip
+    if (dtype != RGNN_F32 && K > 128 && N > 128 && (int64_t)((K + 255) / 256) * ((N + 255) / 256) * T >= 256) p.bk = p.bn = 256;
+    // pieces: enough workgroups over all tiles, and rows enough to pay for a piece's sums,
+    // which are written and read back in fp32
+    const int64_t want = p.bk == 256 ? 512 : 2048, least = p.bk == 256 ? 4096 : 1024;
+    p.chunk = std::max<int64_t>(least, (M * tiles() + want - 1) / want);
+    p.chunk = (p.chunk + 63) / 64 * 64;
+    // ceil(c / chunk) <= 2 c / chunk where c > chunk; written so that it never falls as M grows
+    p.slots = std::min(2 * M / least, 2 * want / tiles());
+    return p;
+}
+
+size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
+{
+    return (size_t)wgrad_plan(dtype, M, T, K, N).slots * K * N * sizeof(float);
+}
+
+rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
+{
+    const WgradPlan plan = wgrad_plan(a.dtype, a.M, a.T, a.K, a.N);
+    const int el = dtype_bytes(a.dtype);
+    const bool whole = (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.dY % 16 == 0 && a.ldx * el % 16 == 0 && a.lddy * el % 16 == 0 &&
+                       (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
+    rgnn_status st;
+    if (!whole) {
+        st = launch_wgrad_any(a, plan, s);
+    } else {
+        WgradK k{};
+        k.X = (const char *)a.X; k.x_rows = a.x_rows; k.ldx = a.ldx * el; k.gather = a.gather;
+        k.dY = (const char *)a.dY; k.dy_rows = a.dy_rows; k.lddy = a.lddy * el; k.dy_gather = a.dy_gather;
+        k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
+        k.dW = a.dW; k.f32 = a.dw_dtype == RGNN_F32;
+        k.vec = (uintptr_t)a.dW % 16 == 0;           // N is a multiple of 4
+        k.chunk = plan.chunk; k.slots = plan.slots; k.partial = (float *)a.ws;
+        LaunchScope ls("typed_wgrad", s);
+        st = a.dtype == RGNN_F32 ? launch_shape<F32>(k, plan, s) : a.dtype == RGNN_BF16 ? launch_shape<BF16>(k, plan, s) : launch_shape<F16>(k, plan, s);
+    }
+    if (st != RGNN_OK) return st;
+    if (plan.slots > 0) {
+        if (a.dtype == RGNN_F32) launch_join<float>(a, plan, s);
+        else if (a.dtype == RGNN_BF16) launch_join<__bf16>(a, plan, s);
+        else launch_join<_Float16>(a, plan, s);
+    }
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_wgrad launch");
+}
+
+}  // namespace rgnn
