@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256, 2) void linear_any_kernel(AnyArgs a)
                      [=](int64_t c) { return (c <= chunk ? 1 : (c + chunk - 1) / chunk) * per; },
                      [=](int64_t c) { return c <= chunk ? 0 : (c + chunk - 1) / chunk; }, p)
         : find_piece(a.ptr, a.T, a.M, blockIdx.x,
-                     [=](int64_t c) { return (c + kAny - 1) / kAny * nj; }, [](int64_t) { return 0; }, p);
+                     [=](int64_t c) { return (c + kAny - 1) / kAny * nj; }, NoWeight(), p);
     if (!any) return;
     const int64_t part = p.index / per;              // row tile, or piece of the contraction
     const int64_t rest = p.index % per;

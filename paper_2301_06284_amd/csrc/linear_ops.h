@@ -5,6 +5,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "rgnn_internal.h"
 
 namespace rgnn {
@@ -126,32 +128,44 @@ __device__ __forceinline__ void type_rows(int64_t p, int64_t q, int64_t M, int64
     end = q < begin ? begin : q > M ? M : q;
 }
 
-// A value that is the same in every lane, in scalar registers.
-__device__ __forceinline__ int64_t uniform(int64_t x)
-{
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), hi = __builtin_amdgcn_readfirstlane((int)(x >> 32));
-    return (int64_t)(((uint64_t)hi << 32) | lo);
-}
-
 struct Piece {          // a workgroup's share: number `index` of type `type`'s pieces
     int type;
     int64_t begin, end;   // the type's rows
-    int64_t index, count; // piece and number of pieces of the type
-    int64_t before;       // what `weight` counted in the types before it
+    int index;            // which of the type's pieces
+    int before;           // what `weight` counted in the types before it
 };
 
-// The type that owns piece number `want`, where type t with c rows makes count(c)
-// pieces.  Every wave of a workgroup searches alike, 256 types a turn: one load of
-// the offsets and a prefix sum over the lanes, no LDS and no barrier.  weight(c) is a
-// second count summed over the types before the owner.  False where there are fewer pieces.
+// Sum over the lanes up to this one, on DPP (no LDS): within rows of 16, then across rows.
+__device__ __forceinline__ int wave_prefix_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);   // row_shr:2
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);   // row_shr:4
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);   // row_shr:8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast:15 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
+    return x;
+}
+
+struct NoWeight {
+    __device__ __forceinline__ int operator()(int64_t) const { return 0; }
+};
+
+// The type that owns piece number `want`, where a type with c rows makes count(c) pieces (fewer
+// than 2^31 over all types: the host checks the grid).  Every wave of a workgroup searches
+// alike, 256 types a turn: one load of the offsets and a prefix sum over the lanes, no LDS and no
+// barrier.  weight(c) is a second count summed over the types before the owner.  False where
+// there are fewer pieces.
 template <class Count, class Weight>
-__device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int T, int64_t M, int64_t want,
+__device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int T, int64_t M, int want,
                                            Count count, Weight weight, Piece &out)
 {
+    constexpr bool WEIGHT = !std::is_same<Weight, NoWeight>::value;
     const int lane = threadIdx.x & 63;
-    int64_t before = 0, wbefore = 0;
+    int before = 0, wbefore = 0;
     for (int t0 = 0; t0 < T; t0 += 256) {
-        int64_t b[4], e[4], c[4], w[4], cs = 0, ws = 0;
+        int64_t b[4], e[4];
+        int c[4], w[4], cs = 0, ws = 0;
         int64_t at[5];       // loads that depend on nothing, all at once
 #pragma unroll
         for (int i = 0; i < 5; ++i) at[i] = ptr[min(t0 + lane * 4 + i, T)];
@@ -159,39 +173,36 @@ __device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int 
         for (int i = 0; i < 4; ++i) {
             const bool own = t0 + lane * 4 + i < T;
             type_rows(at[i], at[i + 1], M, b[i], e[i]);
-            c[i] = own ? count(e[i] - b[i]) : 0;
-            w[i] = own ? weight(e[i] - b[i]) : 0;
+            c[i] = own ? (int)count(e[i] - b[i]) : 0;
+            w[i] = own ? (int)weight(e[i] - b[i]) : 0;
             cs += c[i];
             ws += w[i];
         }
-        int64_t ci = cs, wi = ws;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t x = __shfl_up(ci, d), y = __shfl_up(wi, d);
-            if (lane >= d) { ci += x; wi += y; }
-        }
-        const int64_t total = __shfl(ci, 63);
+        const int ci = wave_prefix_sum(cs), wi = WEIGHT ? wave_prefix_sum(ws) : 0;
+        const int total = __builtin_amdgcn_readlane(ci, 63);
         if (want < before + total) {
             const uint64_t over = __ballot(before + ci > want);
             const int owner = __builtin_ctzll(over);
-            int64_t pat = before + ci - cs, wat = wbefore + wi - ws;   // before this lane's first type
+            int pat = before + ci - cs, wat = wbefore + wi - ws;   // before this lane's first type
             int k = 0;
 #pragma unroll
             for (int i = 0; i < 3; ++i)
                 if (k == i && pat + c[i] <= want) { pat += c[i]; wat += w[i]; k = i + 1; }
             const int64_t bb = k == 0 ? b[0] : k == 1 ? b[1] : k == 2 ? b[2] : b[3];
             const int64_t ee = k == 0 ? e[0] : k == 1 ? e[1] : k == 2 ? e[2] : e[3];
-            const int64_t cc = k == 0 ? c[0] : k == 1 ? c[1] : k == 2 ? c[2] : c[3];
-            out.type = (int)uniform(__shfl(t0 + lane * 4 + k, owner));
-            out.begin = uniform(__shfl(bb, owner));
-            out.end = uniform(__shfl(ee, owner));
-            out.count = uniform(__shfl(cc, owner));
-            out.index = want - uniform(__shfl(pat, owner));
-            out.before = uniform(__shfl(wat, owner));
+            auto lane64 = [&](int64_t x) {
+                const uint32_t lo = __builtin_amdgcn_readlane((int)x, owner), hi = __builtin_amdgcn_readlane((int)(x >> 32), owner);
+                return (int64_t)(((uint64_t)hi << 32) | lo);
+            };
+            out.type = t0 + owner * 4 + __builtin_amdgcn_readlane(k, owner);
+            out.begin = lane64(bb);
+            out.end = lane64(ee);
+            out.index = want - __builtin_amdgcn_readlane(pat, owner);
+            out.before = WEIGHT ? __builtin_amdgcn_readlane(wat, owner) : 0;
             return true;
         }
         before += total;
-        wbefore += __shfl(wi, 63);
+        if (WEIGHT) wbefore += __builtin_amdgcn_readlane(wi, 63);
     }
     return false;
 }

@@ -17,12 +17,17 @@ __device__ __forceinline__ void load_lds(const char *from, char *lds)
     __builtin_amdgcn_global_load_lds((global_ptr)from, (lds_ptr)lds, 16, 0, 0);
 }
 
-// Every wave's loads into LDS have arrived and every wave is done with the step before.  The
-// barrier alone waits for LDS instructions only: loads into LDS count as loads.
+// Every wave's loads into LDS, but for its UNDER youngest, have arrived, and every wave has
+// read what it wanted of the step before.  (A __syncthreads() would wait for all loads.)  The
+// empty asm statements keep the compiler from moving reads and loads across.
+template <int UNDER>
 __device__ __forceinline__ void step_barrier()
 {
-    __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0)
-    __syncthreads();
+    static_assert(UNDER < 64, "vmcnt has six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (UNDER & 15) | (UNDER >> 4) << 14);   // vmcnt(UNDER) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -77,10 +82,10 @@ inline int xcd_window(int64_t tiles)
 inline int64_t xcd_grid(int64_t tiles, int window) { return (tiles + window * 8 - 1) / (window * 8) * (window * 8); }
 
 // The tile of a workgroup: each XCD, which takes every eighth workgroup, gets neighbours.
-__device__ __forceinline__ int64_t xcd_tile(int window)
+__device__ __forceinline__ int xcd_tile(int window)
 {
-    const uint32_t in = blockIdx.x % (uint32_t)(window * 8);
-    return (int64_t)(blockIdx.x - in) + (in & 7) * window + (in >> 3);
+    const uint32_t in = blockIdx.x & (uint32_t)(window * 8 - 1);   // a power of two
+    return (int)(blockIdx.x - in + (in & 7) * window + (in >> 3));
 }
 
 }  // namespace rgnn

@@ -22,7 +22,7 @@
 // row, and rows are written as whole 32-byte pieces.
 #include <algorithm>
 
-#include "linear_tiles.h"
+#include "wide_tile.h"
 
 namespace rgnn {
 
@@ -41,7 +41,8 @@ struct TileArgs {
     char *Y;
     int64_t y_rows, ldy;         // ldy in elements
     const int32_t *scatter;
-    int y_f32, y_f16, y_vec;     // fp32 outputs; of 8-bit products fp16 ones; whole vectors of four are aligned
+    int y_f32, y_f16;            // fp32 outputs; of 8-bit products fp16 ones
+    int y_vec, y_vec16;          // vectors of four outputs, of 16 bytes, are aligned
     int window;                  // workgroups dealt to the XCDs at a time, over 8
     const uint8_t *xs, *ws;      // fp8: scale bytes
     int ks, nb;                  // bytes of a row's scales; 128-blocks of n
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     const int64_t want = xcd_tile(a.window);
     const int nt = (a.N + BN - 1) / BN;
     Piece p;
-    if (!find_piece(a.ptr, a.T, a.M, want, [=](int64_t c) { return (c + BM - 1) / BM * nt; }, [](int64_t) { return 0; }, p))
+    if (!find_piece(a.ptr, a.T, a.M, want, [=](int64_t c) { return (c + BM - 1) / BM * nt; }, NoWeight(), p))
         return;
     int mi, ni;
     tile_place((int)p.index, (int)((p.end - p.begin + BM - 1) / BM), nt, mi, ni);
@@ -236,16 +237,16 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     load(sa0, sb0, 0);
     int step = 0;
     for (; step + 2 <= steps; step += 2) {
-        step_barrier();
+        step_barrier<0>();
         scales(step);
         load(sa1, sb1, step + 1);
         multiply(sa0, sb0);
-        step_barrier();
+        step_barrier<0>();
         if (step + 2 < steps) load(sa0, sb0, step + 2);
         multiply(sa1, sb1);
     }
     if (step < steps) {
-        step_barrier();
+        step_barrier<0>();
         scales(step);
         multiply(sa0, sb0);
     }
@@ -270,6 +271,186 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     }
 }
 
+// The wide tile (wide_tile.h).  A tile with at most half of its rows does half the work.
+template <class T, bool TRANS>
+__global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
+{
+    typedef typename T::elem E;
+    constexpr bool FP8 = sizeof(E) == 1;
+    constexpr int KE = kWideKB / sizeof(E);
+    __shared__ __attribute__((aligned(1024))) char s0[2 * kWideStage], s1[2 * kWideStage], s2[2 * kWideStage], s3[2 * kWideStage];
+    char *a0 = s0, *b0 = s0 + kWideStage, *a1 = s1, *b1 = s1 + kWideStage;
+    char *a2 = s2, *b2 = s2 + kWideStage, *a3 = s3, *b3 = s3 + kWideStage;
+
+    const int nt = (a.N + kWide - 1) / kWide;
+    Piece p;
+    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return (c + kWide - 1) / kWide * nt; },
+                    NoWeight(), p))
+        return;
+    int mi, ni;
+    tile_place((int)p.index, (int)((p.end - p.begin + kWide - 1) / kWide), nt, mi, ni);
+    const int64_t i0 = p.begin + (int64_t)mi * kWide;
+    const int j0 = ni * kWide;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+
+    // Each thread looks up one row of the tile: where its row of X lies (in rows from `X` on;
+    // a row outside X reads row 0, and zeros are written) and where it goes (-1: nowhere).
+    __shared__ int from[kWide], to[kWide];
+    const char *X = a.gather ? a.X : a.X + i0 * a.ldx;
+    {
+        const int r = threadIdx.x;
+        const int64_t i = min(i0 + r, p.end - 1);
+        const int row = a.gather ? a.gather[i] : (int)(i - i0);
+        const bool in = !a.gather || (row >= 0 && row < a.x_rows);
+        const int64_t out = a.scatter ? (int64_t)a.scatter[i] : i;
+        from[r] = in ? row : 0;
+        to[r] = i0 + r < p.end && out >= 0 && out < a.y_rows ? (int)out : -1;
+        if (!in) to[r] = to[r] < 0 ? -1 : ~to[r] - 1;   // below -1: zeros go to row -2 - to
+    }
+    __syncthreads();
+    WideSide sa, sb;
+    const int chunk = (lane & 3) ^ wide_turn_k(wave * 16 + (lane >> 2));   // of rows of k
+    sa.base = X;
+    sa.step = kWideKB;
+#pragma unroll
+    for (int x = 0; x < kWideLoads; ++x)
+        sa.off[x] = (uint32_t)(from[x * 64 + wave * 16 + (lane >> 2)] * a.ldx) + chunk * 16;
+    sb.base = a.W + (int64_t)p.type * a.w_type + (TRANS ? j0 * a.w_row : j0 * (int64_t)sizeof(E));
+    sb.step = TRANS ? kWideKB : KE * a.w_row;
+#pragma unroll
+    for (int x = 0; x < kWideLoads; ++x) {
+        if (TRANS) {
+            const int j = min(x * 64 + wave * 16 + (lane >> 2), a.N - 1 - j0);
+            sb.off[x] = (uint32_t)(j * a.w_row) + chunk * 16;
+        } else {
+            const int k = x * 8 + wave * 2 + (lane >> 5), pos = lane & 31;
+            const int j = ((pos >> 1 ^ wide_turn_n(k)) * 2 + (pos & 1)) * 8;
+            sb.off[x] = (uint32_t)(k * a.w_row) + (j0 + j < a.N ? j : 0) * (uint32_t)sizeof(E);
+        }
+    }
+    const int kbytes = a.K * (int)sizeof(E);
+    const int whole = kbytes / kWideKB, steps = (kbytes + kWideKB - 1) / kWideKB;
+
+    WideFragments<false> fa;
+    WideFragments<!TRANS> fb;
+    fb.init(wn * 128, lane);
+
+    f32x16 acc[4][4] = {};
+    auto walk = [&](auto fm) {
+        constexpr int FMV = decltype(fm)::value, LA = kWideLoads * FMV / 4;
+        fa.init(wm * FMV * 32, lane);
+        // fp8: the scale bytes of this lane's rows, a word is eight steps
+        uint32_t xoff[FP8 ? FMV : 1], sx[FP8 ? FMV : 1], nx[FP8 ? FMV : 1], sw = 0, nw = 0;
+        const uint8_t *xs = nullptr, *wp = nullptr;
+        if constexpr (FP8) {
+            xs = a.gather ? a.xs : a.xs + i0 * a.ks;
+#pragma unroll
+            for (int m = 0; m < FMV; ++m) {
+                xoff[m] = (uint32_t)(from[(wm * FMV + m) * 32 + (lane & 31)] * (int64_t)a.ks);
+                nx[m] = *(const uint32_t *)(xs + xoff[m]);
+            }
+            wp = a.ws + ((int64_t)p.type * a.nb + min(j0 + wn * 128, a.N - 1) / 128) * a.ks;
+            nw = *(const uint32_t *)wp;
+        }
+        auto load = [&](char *ta, char *tb) {
+            sa.load<LA>(ta, wave);
+            sb.load<kWideLoads>(tb, wave);
+            sa.base += sa.step;
+            sb.base += sb.step;
+        };
+        auto edge = [&](char *ta, char *tb, int step) {
+            if (step < whole) return load(ta, tb);
+            const bool in = step * kWideKB + chunk * 16 < kbytes;
+            sa.load_edge<LA>(ta, wave, [&](int) { return in; });
+            sb.load_edge<kWideLoads>(tb, wave, [&](int x) {
+                return TRANS ? in : step * KE + x * 8 + wave * 2 + (lane >> 5) < a.K;
+            });
+        };
+        auto shift = [&](int step) {
+            if constexpr (FP8) {
+                if ((step & 7) == 0) {              // the next word is read eight steps ahead
+#pragma unroll
+                    for (int m = 0; m < FMV; ++m) sx[m] = nx[m];
+                    sw = nw;
+                    const int next = step / 2 + 4;
+                    if (next < a.ks) {
+#pragma unroll
+                        for (int m = 0; m < FMV; ++m) nx[m] = *(const uint32_t *)(xs + next + xoff[m]);
+                        nw = *(const uint32_t *)(wp + next);
+                    }
+                } else if ((step & 1) == 0) {
+#pragma unroll
+                    for (int m = 0; m < FMV; ++m) sx[m] >>= 8;
+                    sw >>= 8;
+                }
+            }
+        };
+        auto multiply = [&](const i32x4 (&x)[FMV][2], const i32x4 (&w)[4][2], f32x16 (&c)[4][4]) {
+            if constexpr (FP8) {
+#pragma unroll
+                for (int m = 0; m < FMV; ++m)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const i32x8 xa = __builtin_shufflevector(x[m][0], x[m][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        const i32x8 wa = __builtin_shufflevector(w[n][0], w[n][1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        c[m][n] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa, xa, c[m][n], 0, 0, 0, (int)sw, 0, (int)sx[m]);
+                    }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+#pragma unroll
+                    for (int m = 0; m < FMV; ++m)
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) c[m][n] = mma32<T>(w[n][q], x[m][q], c[m][n]);
+            }
+        };
+        wide_walk<FMV, false, !TRANS, LA + kWideLoads>(a0, b0, a1, b1, a2, b2, a3, b3, fa, fb, steps, whole, load, edge, multiply,
+                                                       shift, acc);
+        typedef typename std::conditional<FP8, __bf16, E>::type O;
+        const int *out = to + wm * FMV * 32;
+        char *mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
+        if (!a.y_f32 && !a.y_f16 && a.y_vec16 && j0 + kWide <= a.N) {
+            wide_write<O, FMV>(mine, acc, (O *)a.Y + j0 + wn * 128, a.ldy, lane, out);
+            return;
+        }
+#pragma unroll
+        for (int m = 0; m < FMV; ++m) {
+            int row = out[m * 32 + (lane & 31)];
+            const bool zero = row < -1;
+            if (zero) row = -2 - row;
+            if (row < 0) continue;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int j = j0 + wn * 128 + n * 32 + q * 8 + (lane >> 5) * 4;
+                    if (j >= a.N) continue;
+                    const int64_t at = (int64_t)row * a.ldy + j;
+                    f32x4 v = {acc[m][n][q * 4], acc[m][n][q * 4 + 1], acc[m][n][q * 4 + 2], acc[m][n][q * 4 + 3]};
+                    if (zero) v = f32x4{0, 0, 0, 0};
+                    const bool whole = a.y_vec && j + 4 <= a.N;
+                    if (a.y_f32) write4((float *)a.Y + at, v, whole, a.N - j);
+                    else if (FP8 && a.y_f16) write4((_Float16 *)a.Y + at, v, whole, a.N - j);
+                    else write4((O *)a.Y + at, v, whole, a.N - j);
+                }
+        }
+    };
+    if (p.end - i0 <= kWide / 2) walk(std::integral_constant<int, 2>());
+    else walk(std::integral_constant<int, 4>());
+}
+
+template <class T, bool TRANS>
+rgnn_status launch_wide(TileArgs k, hipStream_t s)
+{
+    const int64_t tiles = row_tiles_bound(k.M, k.T, kWide) * ((k.N + kWide - 1) / kWide);
+    k.window = xcd_window(tiles);
+    const int64_t grid = xcd_grid(tiles, k.window);
+    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
+    hipLaunchKernelGGL((typed_linear_wide_kernel<T, TRANS>), dim3((uint32_t)grid), dim3(256), 0, s, k);
+    return RGNN_OK;
+}
+
 template <class T, int BM, int BN, int WM, int WN, bool TRANS>
 rgnn_status launch_tile(TileArgs k, hipStream_t s)
 {
@@ -290,7 +471,10 @@ rgnn_status launch_shape(const TileArgs &k, hipStream_t s)
         if (k.N <= 64) return launch_tile<T, 256, 64, 4, 1, TRANS>(k, s);
         if (rows <= 64) return launch_tile<T, 64, 128, 1, 4, TRANS>(k, s);
         if (rows <= 192 || k.N <= 128) return launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
-        return launch_tile<T, 256, 256, 2, 4, TRANS>(k, s);
+        // the wide tile's offsets have 32 bits
+        const bool near = k.x_rows > 0 && (k.gather ? k.x_rows : (int64_t)kWide) * k.ldx < (int64_t(1) << 32) &&
+                          kWide * k.w_row < (int64_t(1) << 32);
+        return near ? launch_wide<T, TRANS>(k, s) : launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
     }
 }
 
@@ -306,6 +490,7 @@ TileArgs tile_args(const LinearArgs &a)
     k.Y = (char *)a.Y; k.y_rows = a.y_rows; k.ldy = a.ldy; k.scatter = a.scatter;
     k.y_f32 = a.y_dtype == RGNN_F32;
     k.y_vec = (uintptr_t)a.Y % (4 * yel) == 0 && a.ldy % 4 == 0;
+    k.y_vec16 = (uintptr_t)a.Y % 16 == 0 && a.ldy * yel % 16 == 0;
     return k;
 }
 

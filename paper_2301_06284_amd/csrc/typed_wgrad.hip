@@ -157,11 +157,11 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
     }
     int step = 0;
     for (; step + 2 <= steps; step += 2) {
-        step_barrier();
+        step_barrier<0>();
         x.load(sx1, lane);
         y.load(sy1, lane);
         multiply(sx0, sy0);
-        step_barrier();
+        step_barrier<0>();
         if (step + 2 < steps) {
             x.load(sx0, lane);
             y.load(sy0, lane);
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
         multiply(sx1, sy1);
     }
     if (step < steps) {
-        step_barrier();
+        step_barrier<0>();
         multiply(sx0, sy0);
     }
 
