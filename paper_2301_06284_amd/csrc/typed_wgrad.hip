@@ -12,7 +12,7 @@
 // atomics, the same result every time.
 #include <algorithm>
 
-#include "linear_tiles.h"
+#include "wide_tile.h"
 
 namespace rgnn {
 
@@ -194,6 +194,106 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
     }
 }
 
+// The wide tile (wide_tile.h): rows as they are (without index arrays), whose places a base for
+// all lanes and an offset for each tell.
+template <class T>
+__global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
+{
+    typedef typename T::elem E;
+    constexpr int KE = kWideKB / sizeof(E);
+    __shared__ __attribute__((aligned(1024))) char s0[2 * kWideStage], s1[2 * kWideStage], s2[2 * kWideStage], s3[2 * kWideStage];
+    __shared__ int to[kWide];
+    char *a0 = s0, *b0 = s0 + kWideStage, *a1 = s1, *b1 = s1 + kWideStage;
+    char *a2 = s2, *b2 = s2 + kWideStage, *a3 = s3, *b3 = s3 + kWideStage;
+
+    const int nk = (a.K + kWide - 1) / kWide, nn = (a.N + kWide - 1) / kWide, per = nk * nn;
+    const int64_t chunk = a.chunk;
+    Piece p;
+    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return pieces_of(c, chunk) * per; },
+                    [=](int64_t c) { return slots_of(c, chunk); }, p))
+        return;
+    const int part = p.index / per;
+    int ki, ni;
+    tile_place(p.index - part * per, nk, nn, ki, ni);
+    const int64_t p0 = p.begin + part * chunk;
+    const int rows = (int)min(chunk, p.end - p0);
+    const int k0 = ki * kWide, n0 = ni * kWide;
+    const bool split = p.end - p.begin > chunk;
+    const int64_t slot = p.before + part;
+    if (split && slot >= a.slots) return;            // only where the offsets are not monotone
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    to[threadIdx.x] = k0 + (int)threadIdx.x < a.K ? (int)threadIdx.x : -1;
+
+    WideSide sx, sy;
+    sx.base = a.X + p0 * a.ldx + k0 * (int64_t)sizeof(E);
+    sy.base = a.dY + p0 * a.lddy + n0 * (int64_t)sizeof(E);
+    sx.step = KE * a.ldx;
+    sy.step = KE * a.lddy;
+    const int row0 = wave * 2 + (lane >> 5);         // of a step's 32, and 8 x more for load x
+#pragma unroll
+    for (int x = 0; x < kWideLoads; ++x) {
+        const int k = row0 + x * 8, pos = lane & 31, j = ((pos >> 1 ^ wide_turn_n(k)) * 2 + (pos & 1)) * 8;
+        sx.off[x] = (uint32_t)(k * a.ldx) + (k0 + j < a.K ? j : 0) * (uint32_t)sizeof(E);
+        sy.off[x] = (uint32_t)(k * a.lddy) + (n0 + j < a.N ? j : 0) * (uint32_t)sizeof(E);
+    }
+    const int whole = rows / KE, steps = (rows + KE - 1) / KE;
+    WideFragments<true> fx, fy;
+    fx.init(wm * 128, lane);
+    fy.init(wn * 128, lane);
+
+    f32x16 acc[4][4] = {};
+    constexpr int LOADS = 2 * kWideLoads;
+    auto load = [&](char *ta, char *tb) {
+        sx.load<kWideLoads>(ta, wave);
+        sy.load<kWideLoads>(tb, wave);
+        sx.base += sx.step;
+        sy.base += sy.step;
+    };
+    auto edge = [&](char *ta, char *tb, int step) {
+        if (step < whole) return load(ta, tb);
+        auto in = [&](int x) { return step * KE + row0 + x * 8 < rows; };
+        sx.load_edge<kWideLoads>(ta, wave, in);
+        sy.load_edge<kWideLoads>(tb, wave, in);
+    };
+    auto multiply = [&](const i32x4 (&x)[4][2], const i32x4 (&y)[4][2], f32x16 (&c)[4][4]) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) c[m][n] = mma32<T>(y[n][q], x[m][q], c[m][n]);
+    };
+    // a type without rows: nothing to walk, zeros to write
+    if (steps > 0) wide_walk<4, true, true, LOADS>(a0, b0, a1, b1, a2, b2, a3, b3, fx, fy, steps, whole, load, edge, multiply, [](int) {}, acc);
+    else __syncthreads();
+
+    const int64_t at0 = (split ? slot : (int64_t)p.type) * a.K + k0;
+    if (!split && !a.f32 && a.vec && a.N % 8 == 0 && n0 + kWide <= a.N) {
+        char *mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
+        wide_write<E, 4>(mine, acc, (E *)a.dW + at0 * a.N + n0 + wn * 128, a.N, lane, to + wm * 128);
+        return;
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const int k = wm * 128 + m * 32 + (lane & 31);
+        if (k0 + k >= a.K) continue;
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int j = n0 + wn * 128 + n * 32 + q * 8 + (lane >> 5) * 4;
+                if (j >= a.N) continue;
+                const int64_t at = (at0 + k) * a.N + j;
+                const f32x4 v = {acc[m][n][q * 4], acc[m][n][q * 4 + 1], acc[m][n][q * 4 + 2], acc[m][n][q * 4 + 3]};
+                const bool whole4 = a.vec && j + 4 <= a.N;
+                if (split) write4(a.partial + at, v, whole4, a.N - j);
+                else if (a.f32) write4((float *)a.dW + at, v, whole4, a.N - j);
+                else write4((E *)a.dW + at, v, whole4, a.N - j);
+            }
+    }
+}
+
 // dW[t] of the types with several pieces.  A workgroup takes 64 V values of one type's gradient
 // at a time and adds a quarter of the pieces in each wave, then the quarters.
 template <class E, int V>
@@ -258,10 +358,26 @@ rgnn_status launch_tile(WgradK k, hipStream_t s)
 }
 
 template <class T>
+rgnn_status launch_wide(WgradK k, hipStream_t s)
+{
+    const int64_t tiles = (k.T + k.slots) * ((k.K + kWide - 1) / kWide) * ((k.N + kWide - 1) / kWide);
+    k.window = xcd_window(tiles);
+    const int64_t grid = xcd_grid(tiles, k.window);
+    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
+    hipLaunchKernelGGL((typed_wgrad_wide_kernel<T>), dim3((uint32_t)grid), dim3(256), 0, s, k);
+    return RGNN_OK;
+}
+
+template <class T>
 rgnn_status launch_shape(const WgradK &k, const WgradPlan &p, hipStream_t s)
 {
     if constexpr (sizeof(typename T::elem) == 2)
-        if (p.bk == 256) return launch_tile<T, 256, 256, 2, 4>(k, s);
+        if (p.bk == 256) {
+            // the wide tile takes rows as they are, at 32-bit offsets in a step
+            const int64_t ld = std::max(k.ldx, k.lddy);
+            if (!k.gather && !k.dy_gather && ld * kWide < (int64_t(1) << 32)) return launch_wide<T>(k, s);
+            return launch_tile<T, 128, 128, 2, 2>(k, s);
+        }
     if (p.bk == 128 && p.bn == 128) return launch_tile<T, 128, 128, 2, 2>(k, s);
     if (p.bk == 128) return launch_tile<T, 128, 64, 2, 2>(k, s);
     if (p.bn == 128) return launch_tile<T, 64, 128, 2, 2>(k, s);
