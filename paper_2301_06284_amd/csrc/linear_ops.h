@@ -57,10 +57,8 @@ struct WgradPlan {
     int64_t chunk = 0, slots = 0;
 };
 WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
-rgnn_status launch_wgrad_any(const WgradArgs &a, const WgradPlan &plan, hipStream_t s);
 size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s);
-rgnn_status launch_linear_any(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s);
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s);

@@ -55,21 +55,90 @@ __device__ __forceinline__ void tile_place(int q, int mt, int nt, int &m, int &n
     m = group * 8 + rest - n * gm;
 }
 
-// Four outputs side by side, or the first `n` of them.
+// Four outputs side by side, or the first `n` of them, to any address of an element.
 template <class O>
-__device__ __forceinline__ void write4(O *y, f32x4 v, bool whole, int n)
+__device__ __forceinline__ void write4(O *y, f32x4 v, int n)
 {
     O o[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) o[q] = (O)v[q];
-    if (whole) {
-        if constexpr (sizeof(O) == 2) *(uint2 *)y = *(const uint2 *)o;
-        else *(i32x4 *)y = *(const i32x4 *)o;
-    } else {
+    if (n >= 4) __builtin_memcpy(y, o, sizeof(o));
+    else
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 3; ++q)
             if (q < n) y[q] = o[q];
+}
+
+// Writes a wave's outputs in 16 bits through LDS (FM * FN * 512 bytes of its own), so that rows
+// go out in pieces as wide as the wave's columns: from the accumulators a store would take 32 bytes each of
+// 16 rows.  `y` points at the wave's first column, of which `cols` are the matrix's.  Chunk c of row r
+// lies at c ^ (r >> 1 & 7) (FN = 4) or c ^ (r >> 2 & 3) (FN = 2): no bank conflicts.
+// to[r]: where row r goes, -1 nowhere; below -1: zeros to row -2 - to[r].
+template <class O, int FM, int FN>
+__device__ __forceinline__ void write_rows(char *lds, const f32x4 (&acc)[FM][FN], O *y, int64_t ldy, int cols, int lane,
+                                           const int *to)
+{
+    static_assert(FN == 2 || FN == 4, "pieces of 64 or 128 bytes");
+    constexpr int CH = FN * 2;                      // chunks of a row
+    auto turn = [](int r) { return FN == 4 ? r >> 1 & 7 : r >> 2 & 3; };
+    const int r16 = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int m = 0; m < FM; ++m)
+#pragma unroll
+        for (int f = 0; f < FN; ++f) {
+            O o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = (O)acc[m][f][q];
+            *(uint2 *)(lds + (m * 16 + r16) * (CH * 16) + ((f * 2 + (g >> 1)) ^ turn(r16)) * 16 + (g & 1) * 8) = *(const uint2 *)o;
+        }
+    // a wave's LDS instructions stay in order: its reads see its writes
+    const int c = lane % CH, left = cols - c * 8;   // this lane's columns
+#pragma unroll
+    for (int t = 0; t < FM * FN / 2; ++t) {
+        const int r = t * (64 / CH) + lane / CH;
+        i32x4 v = *(const i32x4 *)(lds + r * (CH * 16) + (c ^ turn(r)) * 16);
+        int row = to[r];
+        if (row < -1) { row = -2 - row; v = i32x4{0, 0, 0, 0}; }
+        if (row < 0 || left <= 0) continue;
+        O *at = y + row * ldy + c * 8;
+        if (left >= 8) __builtin_memcpy(at, &v, 16);
+        else {
+            O o[8];
+            __builtin_memcpy(o, &v, 16);
+#pragma unroll
+            for (int q = 0; q < 7; ++q)
+                if (q < left) at[q] = o[q];
+        }
     }
+}
+
+// 16 bytes from any address of an element; by elements, zero behind `end`, where they would
+// reach behind it.
+template <class E>
+__device__ __forceinline__ i32x4 load_any(const char *p, const char *end)
+{
+    i32x4 v = {0, 0, 0, 0};
+    if (p + 16 <= end) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+        E e[16 / sizeof(E)];
+#pragma unroll
+        for (int i = 0; i < (int)(16 / sizeof(E)); ++i)
+            e[i] = p + (i + 1) * sizeof(E) <= end ? ((const E *)p)[i] : (E)0.0f;
+        __builtin_memcpy(&v, e, 16);
+    }
+    return v;
+}
+
+// The first n bytes of v, the others zero.
+__device__ __forceinline__ i32x4 first_bytes(i32x4 v, int n)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = n - i * 4;
+        v[i] = left >= 4 ? v[i] : left <= 0 ? 0 : v[i] & ((1 << left * 8) - 1);
+    }
+    return v;
 }
 
 // XCD windows: up to 32 tiles for each of the 8 XCDs, an eighth of the work at most.

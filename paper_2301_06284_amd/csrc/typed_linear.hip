@@ -1,7 +1,6 @@
 // typed_linear.hip -- the typed linear over ragged segments whose offsets lie on the
 // device: Y[scatter[i]] = X[gather[i]] W[t(i)], weights as stored or transposed (the
-// input gradient), and its 8-bit form.  The tiles of linear_any.hip take what does not
-// fill vectors of 16 bytes.
+// input gradient), and its 8-bit form.
 //
 // A workgroup takes BM x BN outputs of one type and walks k in steps of 128 bytes of a row
 // (32 fp32, 64 16-bit or 128 8-bit values), which makes one kernel of all types: the same
@@ -42,7 +41,7 @@ struct TileArgs {
     int64_t y_rows, ldy;         // ldy in elements
     const int32_t *scatter;
     int y_f32, y_f16;            // fp32 outputs; of 8-bit products fp16 ones
-    int y_vec, y_vec16;          // vectors of four outputs, of 16 bytes, are aligned
+    const char *x_end, *w_end;   // behind the last element
     int window;                  // workgroups dealt to the XCDs at a time, over 8
     const uint8_t *xs, *ws;      // fp8: scale bytes
     int ks, nb;                  // bytes of a row's scales; 128-blocks of n
@@ -50,7 +49,22 @@ struct TileArgs {
 
 struct F8 { typedef uint8_t elem; };
 
-template <class T, int BM, int BN, int WM, int WN, bool TRANS>
+// Each thread of the first BM looks up one row of a tile: which row of X it reads (-1: none of
+// them, zeros) and where it goes (-1: nowhere; below -1: zeros go to row -2 - to).  A row outside X
+// counts as zeros whatever the weights hold.
+__device__ __forceinline__ void tile_row(const TileArgs &a, int64_t i, int64_t end, int &from, int &to)
+{
+    const int64_t at = min(i, end - 1);             // rows behind the type's: not written
+    const int64_t row = a.gather ? (int64_t)a.gather[at] : at, out = a.scatter ? (int64_t)a.scatter[at] : at;
+    const bool in = row >= 0 && row < a.x_rows;
+    from = in ? (int)row : -1;
+    to = i < end && out >= 0 && out < a.y_rows ? (int)out : -1;
+    if (!in && to >= 0) to = -2 - to;
+}
+
+// ANY: rows on any address.  Loads go through registers (16 bytes from any address; at the end of
+// k and of the matrix by elements) and are written to LDS a step later.
+template <class T, int BM, int BN, int WM, int WN, bool TRANS, bool ANY>
 __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a)
 {
     typedef typename T::elem E;
@@ -58,40 +72,34 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     constexpr int NW = WM * WN, KE = 128 / sizeof(E);
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;     // fragments of a wave
     constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;       // KB that a wave loads each step
-    static_assert(NA * 8 * NW == BM && NB * 8 * NW == BN, "whole loads");
-    __shared__ __attribute__((aligned(1024))) char sa0[BM * 128], sb0[BN * 128], sa1[BM * 128], sb1[BN * 128];
+    static_assert(NA * 8 * NW == BM && NB * 8 * NW == BN && NW % 2 == 0 && BM <= NW * 64, "whole loads");
+    __shared__ __attribute__((aligned(1024))) char s0[(BM + BN) * 128], s1[(BM + BN) * 128];
+    __shared__ int from[BM], to[BM];
+    char *sa0 = s0, *sb0 = s0 + BM * 128, *sa1 = s1, *sb1 = s1 + BM * 128;
 
-    const int64_t want = xcd_tile(a.window);
     const int nt = (a.N + BN - 1) / BN;
     Piece p;
-    if (!find_piece(a.ptr, a.T, a.M, want, [=](int64_t c) { return (c + BM - 1) / BM * nt; }, NoWeight(), p))
+    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return (c + BM - 1) / BM * nt; }, NoWeight(), p))
         return;
     int mi, ni;
-    tile_place((int)p.index, (int)((p.end - p.begin + BM - 1) / BM), nt, mi, ni);
+    tile_place(p.index, (int)((p.end - p.begin + BM - 1) / BM), nt, mi, ni);
     const int64_t i0 = p.begin + (int64_t)mi * BM;
     const int j0 = ni * BN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
+    if (threadIdx.x < BM) tile_row(a, i0 + threadIdx.x, p.end, from[threadIdx.x], to[threadIdx.x]);
+    __syncthreads();
 
     // ---- where this lane's loads come from
     const char *zeros = (const char *)&kZeros;
     const char *ap[NA], *bp[NB];
     uint32_t aok = 0;                               // bit x: row x is one of X
-    int ac, bc;                                     // chunk of k (bytes / 16) of the loads of rows of k
-    {
-        const int pos = lane & 7, sub = lane >> 3;
-        ac = pos ^ ((((wave & 1) << 2) | (sub >> 1)) & 7);
-        bc = ac;
-        static_assert(NW % 2 == 0 || NW == 1, "slab parity is the wave's");
-    }
+    const int chunk = (lane & 7) ^ ((wave & 1) << 2 | lane >> 4);   // of rows of k
 #pragma unroll
     for (int x = 0; x < NA; ++x) {
-        int64_t i = i0 + (x * NW + wave) * 8 + (lane >> 3);
-        if (i >= p.end) i = p.end - 1;              // its outputs are not written
-        const int64_t row = a.gather ? a.gather[i] : i;
-        const bool ok = row >= 0 && row < a.x_rows;
-        ap[x] = ok ? a.X + row * a.ldx + ac * 16 : zeros;
-        aok |= (ok ? 1u : 0u) << x;
+        const int row = from[(x * NW + wave) * 8 + (lane >> 3)];
+        ap[x] = row >= 0 ? a.X + row * a.ldx + chunk * 16 : zeros;
+        aok |= (row >= 0 ? 1u : 0u) << x;
     }
     const char *W = a.W + (int64_t)p.type * a.w_type;
     int bk[NB];                                     // rows of n: the k of the load
@@ -100,13 +108,11 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     for (int x = 0; x < NB; ++x) {
         if (TRANS) {
             const int j = min(j0 + (x * NW + wave) * 8 + (lane >> 3), a.N - 1);
-            bp[x] = W + (int64_t)j * a.w_row + bc * 16;
+            bp[x] = W + j * a.w_row + chunk * 16;
             bk[x] = 0;
         } else {
-            constexpr int CH = BN * sizeof(E) / 16;  // chunks of a row
-            const int at = (x * NW + wave) * 64 + lane;
-            const int k = at / CH, pos = at % CH;
-            constexpr int UC = sizeof(E) == 4 ? 4 : 2;   // chunks of a unit
+            constexpr int CH = BN * sizeof(E) / 16, UC = sizeof(E) == 4 ? 4 : 2;   // chunks of a row, of a unit
+            const int at = (x * NW + wave) * 64 + lane, k = at / CH, pos = at % CH;
             const int c = (pos / UC ^ unit_turn<T, BN>(k)) * UC + pos % UC;
             const int j = j0 + c * (16 / (int)sizeof(E));
             bk[x] = k;
@@ -125,10 +131,8 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     if constexpr (SCALES) {
         static_assert(BM / 64 <= NW && FN * 16 <= 128 && 128 % (FN * 16) == 0, "scales");
         if (wave < BM / 64) {
-            int64_t i = i0 + wave * 64 + lane;
-            if (i >= p.end) i = p.end - 1;
-            const int64_t row = a.gather ? a.gather[i] : i;
-            if (row >= 0 && row < a.x_rows) { xp = (const char *)a.xs + row * a.ks; xinc = 4; }
+            const int row = from[wave * 64 + lane];
+            if (row >= 0) { xp = (const char *)a.xs + (int64_t)row * a.ks; xinc = 4; }
         }
         const int jb = min(j0 + wave % WN * FN * 16, a.N - 1) / 128;
         wp = a.ws + ((int64_t)p.type * a.nb + jb) * a.ks;
@@ -136,23 +140,50 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     auto load = [&](char *sa, char *sb, int step) {
         if constexpr (SCALES) {
             if ((step & 3) == 0 && wave < BM / 64) {
-                char *to = step & 4 ? sx1 : sx0;
-                __builtin_amdgcn_global_load_lds((global_ptr)xp, (lds_ptr)(to + wave * 256), 4, 0, 0);
+                char *at = step & 4 ? sx1 : sx0;
+                __builtin_amdgcn_global_load_lds((global_ptr)xp, (lds_ptr)(at + wave * 256), 4, 0, 0);
                 xp += xinc;
             }
         }
         const bool tail = (step + 1) * 128 > kbytes;
 #pragma unroll
         for (int x = 0; x < NA; ++x) {
-            const char *src = tail && step * 128 + ac * 16 >= kbytes ? zeros : ap[x];
+            const char *src = tail && step * 128 + chunk * 16 >= kbytes ? zeros : ap[x];
             load_lds(src, sa + (x * NW + wave) * 1024);
             ap[x] += (aok >> x & 1) << 7;
         }
 #pragma unroll
         for (int x = 0; x < NB; ++x) {
-            const bool out = TRANS ? step * 128 + bc * 16 >= kbytes : step * KE + bk[x] >= a.K;
+            const bool out = TRANS ? step * 128 + chunk * 16 >= kbytes : step * KE + bk[x] >= a.K;
             load_lds(tail && out ? zeros : bp[x], sb + (x * NW + wave) * 1024);
             bp[x] += binc;
+        }
+    };
+    // ANY: a step's loads into registers, and from there to LDS
+    i32x4 ra[ANY ? NA : 1], rb[ANY ? NB : 1];
+    auto fetch = [&](int step) {
+        if constexpr (ANY) {
+            const int left = kbytes - step * 128 - chunk * 16;   // bytes of k from this chunk on
+#pragma unroll
+            for (int x = 0; x < NA; ++x) {
+                ra[x] = left > 0 && (aok >> x & 1) ? first_bytes(load_any<E>(ap[x], a.x_end), left) : i32x4{0, 0, 0, 0};
+                ap[x] += (aok >> x & 1) << 7;
+            }
+#pragma unroll
+            for (int x = 0; x < NB; ++x) {
+                const bool in = TRANS ? left > 0 : step * KE + bk[x] < a.K;
+                rb[x] = in ? load_any<E>(bp[x], a.w_end) : i32x4{0, 0, 0, 0};
+                if (TRANS) rb[x] = first_bytes(rb[x], left);
+                bp[x] += binc;
+            }
+        }
+    };
+    auto put = [&](char *sa, char *sb) {
+        if constexpr (ANY) {
+#pragma unroll
+            for (int x = 0; x < NA; ++x) *(i32x4 *)(sa + (x * NW + wave) * 1024 + lane * 16) = ra[x];
+#pragma unroll
+            for (int x = 0; x < NB; ++x) *(i32x4 *)(sb + (x * NW + wave) * 1024 + lane * 16) = rb[x];
         }
     };
 
@@ -181,9 +212,9 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     auto scales = [&](int step) {
         if constexpr (SCALES) {
             if ((step & 3) == 0) {
-                const char *from = (step & 4 ? sx1 : sx0) + (wm * FM * 16 + r16) * 4;
+                const char *at = (step & 4 ? sx1 : sx0) + (wm * FM * 16 + r16) * 4;
 #pragma unroll
-                for (int f = 0; f < FM; ++f) sx[f] = *(const int *)(from + f * 64);
+                for (int f = 0; f < FM; ++f) sx[f] = *(const int *)(at + f * 64);
                 sw = *(const int *)(wp + step);
             }
         }
@@ -234,41 +265,66 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
         }
     };
 
-    load(sa0, sb0, 0);
     int step = 0;
-    for (; step + 2 <= steps; step += 2) {
-        step_barrier<0>();
-        scales(step);
-        load(sa1, sb1, step + 1);
-        multiply(sa0, sb0);
-        step_barrier<0>();
-        if (step + 2 < steps) load(sa0, sb0, step + 2);
-        multiply(sa1, sb1);
-    }
-    if (step < steps) {
-        step_barrier<0>();
-        scales(step);
-        multiply(sa0, sb0);
+    if constexpr (ANY) {
+        fetch(0);
+        put(sa0, sb0);
+        if (steps > 1) fetch(1);
+        for (; step + 2 <= steps; step += 2) {
+            __syncthreads();
+            multiply(sa0, sb0);
+            put(sa1, sb1);
+            if (step + 2 < steps) fetch(step + 2);
+            __syncthreads();
+            multiply(sa1, sb1);
+            if (step + 2 < steps) put(sa0, sb0);
+            if (step + 3 < steps) fetch(step + 3);
+        }
+        if (step < steps) {
+            __syncthreads();
+            multiply(sa0, sb0);
+        }
+    } else {
+        load(sa0, sb0, 0);
+        for (; step + 2 <= steps; step += 2) {
+            step_barrier<0>();
+            scales(step);
+            load(sa1, sb1, step + 1);
+            multiply(sa0, sb0);
+            step_barrier<0>();
+            if (step + 2 < steps) load(sa0, sb0, step + 2);
+            multiply(sa1, sb1);
+        }
+        if (step < steps) {
+            step_barrier<0>();
+            scales(step);
+            multiply(sa0, sb0);
+        }
     }
 
     // ---- write
+    const int *out = to + wm * FM * 16;
+    const int j1 = j0 + wn * FN * 16;               // this wave's first column
+    if (sizeof(E) == 4 || a.y_f32) {
 #pragma unroll
-    for (int m = 0; m < FM; ++m) {
-        const int64_t i = i0 + (wm * FM + m) * 16 + r16;
-        int64_t row = -1;
-        if (i < p.end) row = a.scatter ? a.scatter[i] : i;
-        if (row < 0 || row >= a.y_rows) continue;
+        for (int m = 0; m < FM; ++m) {
+            int row = out[m * 16 + r16];
+            const bool zero = row < -1;
+            if (zero) row = -2 - row;
+            if (row < 0) continue;
 #pragma unroll
-        for (int f = 0; f < FN; ++f) {
-            const int j = j0 + (wn * FN + f) * 16 + g * 4;
-            if (j >= a.N) continue;
-            const int64_t at = row * a.ldy + j;
-            const bool whole = a.y_vec && j + 4 <= a.N;
-            if (sizeof(E) == 4 || a.y_f32) write4((float *)a.Y + at, acc[m][f], whole, a.N - j);
-            else if (FP8 && a.y_f16) write4((_Float16 *)a.Y + at, acc[m][f], whole, a.N - j);
-            else write4((typename std::conditional<FP8, __bf16, E>::type *)a.Y + at, acc[m][f], whole, a.N - j);
+            for (int f = 0; f < FN; ++f) {
+                const int j = j1 + f * 16 + g * 4;
+                write4((float *)a.Y + row * a.ldy + j, zero ? f32x4{0, 0, 0, 0} : acc[m][f], a.N - j);
+            }
         }
+        return;
     }
+    step_barrier<0>();                              // the stages may be used again
+    char *mine = s0 + wave * (FM * FN * 512);
+    if (FP8 && a.y_f16) write_rows<_Float16, FM, FN>(mine, acc, (_Float16 *)a.Y + j1, a.ldy, a.N - j1, lane, out);
+    else write_rows<typename std::conditional<sizeof(E) != 2, __bf16, E>::type, FM, FN>(
+        mine, acc, (typename std::conditional<sizeof(E) != 2, __bf16, E>::type *)a.Y + j1, a.ldy, a.N - j1, lane, out);
 }
 
 // The wide tile (wide_tile.h).  A tile with at most half of its rows does half the work.
@@ -294,19 +350,13 @@ __global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
 
-    // Each thread looks up one row of the tile: where its row of X lies (in rows from `X` on;
-    // a row outside X reads row 0, and zeros are written) and where it goes (-1: nowhere).
+    // the rows' places in 32 bits of bytes from `X` on
     __shared__ int from[kWide], to[kWide];
     const char *X = a.gather ? a.X : a.X + i0 * a.ldx;
     {
-        const int r = threadIdx.x;
-        const int64_t i = min(i0 + r, p.end - 1);
-        const int row = a.gather ? a.gather[i] : (int)(i - i0);
-        const bool in = !a.gather || (row >= 0 && row < a.x_rows);
-        const int64_t out = a.scatter ? (int64_t)a.scatter[i] : i;
-        from[r] = in ? row : 0;
-        to[r] = i0 + r < p.end && out >= 0 && out < a.y_rows ? (int)out : -1;
-        if (!in) to[r] = to[r] < 0 ? -1 : ~to[r] - 1;   // below -1: zeros go to row -2 - to
+        int row;
+        tile_row(a, i0 + threadIdx.x, p.end, row, to[threadIdx.x]);
+        from[threadIdx.x] = max(0, a.gather ? row : row - (int)i0);   // of zeros: any row
     }
     __syncthreads();
     WideSide sa, sb;
@@ -410,7 +460,7 @@ __global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
         typedef typename std::conditional<FP8, __bf16, E>::type O;
         const int *out = to + wm * FMV * 32;
         char *mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
-        if (!a.y_f32 && !a.y_f16 && a.y_vec16 && j0 + kWide <= a.N) {
+        if (!a.y_f32 && !a.y_f16 && j0 + kWide <= a.N) {
             wide_write<O, FMV>(mine, acc, (O *)a.Y + j0 + wn * 128, a.ldy, lane, out);
             return;
         }
@@ -425,14 +475,12 @@ __global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const int j = j0 + wn * 128 + n * 32 + q * 8 + (lane >> 5) * 4;
-                    if (j >= a.N) continue;
-                    const int64_t at = (int64_t)row * a.ldy + j;
+                    const int64_t at = row * a.ldy + j;
                     f32x4 v = {acc[m][n][q * 4], acc[m][n][q * 4 + 1], acc[m][n][q * 4 + 2], acc[m][n][q * 4 + 3]};
                     if (zero) v = f32x4{0, 0, 0, 0};
-                    const bool whole = a.y_vec && j + 4 <= a.N;
-                    if (a.y_f32) write4((float *)a.Y + at, v, whole, a.N - j);
-                    else if (FP8 && a.y_f16) write4((_Float16 *)a.Y + at, v, whole, a.N - j);
-                    else write4((O *)a.Y + at, v, whole, a.N - j);
+                    if (a.y_f32) write4((float *)a.Y + at, v, a.N - j);
+                    else if (FP8 && a.y_f16) write4((_Float16 *)a.Y + at, v, a.N - j);
+                    else write4((O *)a.Y + at, v, a.N - j);
                 }
         }
     };
@@ -451,36 +499,35 @@ rgnn_status launch_wide(TileArgs k, hipStream_t s)
     return RGNN_OK;
 }
 
-template <class T, int BM, int BN, int WM, int WN, bool TRANS>
+template <class T, int BM, int BN, int WM, int WN, bool TRANS, bool ANY>
 rgnn_status launch_tile(TileArgs k, hipStream_t s)
 {
     const int64_t tiles = row_tiles_bound(k.M, k.T, BM) * ((k.N + BN - 1) / BN);
     k.window = xcd_window(tiles);
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
+    hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
     return RGNN_OK;
 }
 
-template <class T, bool TRANS>
+template <class T, bool TRANS, bool ANY>
 rgnn_status launch_shape(const TileArgs &k, hipStream_t s)
 {
-    const int64_t rows = k.M / std::min<int64_t>(std::max<int64_t>(k.M, 1), k.T);   // of a type, on average
-    if constexpr (sizeof(typename T::elem) == 4) return launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
-    else {
-        if (k.N <= 64) return launch_tile<T, 256, 64, 4, 1, TRANS>(k, s);
-        if (rows <= 64) return launch_tile<T, 64, 128, 1, 4, TRANS>(k, s);
-        if (rows <= 192 || k.N <= 128) return launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
+    const int64_t rows = k.M / std::min<int64_t>(k.M, k.T);   // of a type, on average
+    if (rows <= 64) return launch_tile<T, 64, 128, 1, 4, TRANS, ANY>(k, s);
+    if (k.N <= 64) return launch_tile<T, 256, 64, 4, 1, TRANS, ANY>(k, s);
+    if constexpr (!ANY && sizeof(typename T::elem) != 4) {
         // the wide tile's offsets have 32 bits
         const bool near = k.x_rows > 0 && (k.gather ? k.x_rows : (int64_t)kWide) * k.ldx < (int64_t(1) << 32) &&
                           kWide * k.w_row < (int64_t(1) << 32);
-        return near ? launch_wide<T, TRANS>(k, s) : launch_tile<T, 128, 128, 2, 2, TRANS>(k, s);
+        if (rows > 192 && k.N > 128 && near) return launch_wide<T, TRANS>(k, s);
     }
+    return launch_tile<T, 128, 128, 2, 2, TRANS, ANY>(k, s);
 }
 
 TileArgs tile_args(const LinearArgs &a)
 {
-    const int el = dtype_bytes(a.dtype), yel = dtype_bytes(a.y_dtype);
+    const int el = dtype_bytes(a.dtype);
     TileArgs k{};
     k.X = (const char *)a.X; k.x_rows = a.x_rows; k.ldx = a.ldx * el; k.gather = a.gather;
     k.ptr = a.type_ptr; k.T = a.T; k.M = a.M;
@@ -489,9 +536,16 @@ TileArgs tile_args(const LinearArgs &a)
     k.w_type = (int64_t)a.K * a.N * el;
     k.Y = (char *)a.Y; k.y_rows = a.y_rows; k.ldy = a.ldy; k.scatter = a.scatter;
     k.y_f32 = a.y_dtype == RGNN_F32;
-    k.y_vec = (uintptr_t)a.Y % (4 * yel) == 0 && a.ldy % 4 == 0;
-    k.y_vec16 = (uintptr_t)a.Y % 16 == 0 && a.ldy * yel % 16 == 0;
+    k.x_end = k.X + ((a.x_rows - 1) * a.ldx + a.K) * el;
+    k.w_end = k.W + a.T * k.w_type;
     return k;
+}
+
+template <class T>
+rgnn_status launch_type(const TileArgs &k, int trans, bool whole, hipStream_t s)
+{
+    if (whole) return trans ? launch_shape<T, true, false>(k, s) : launch_shape<T, false, false>(k, s);
+    return trans ? launch_shape<T, true, true>(k, s) : launch_shape<T, false, true>(k, s);
 }
 
 }  // namespace
@@ -499,16 +553,16 @@ TileArgs tile_args(const LinearArgs &a)
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s)
 {
     const int el = dtype_bytes(a.dtype);
+    // whole vectors of 16 bytes in every row go straight to LDS
     const bool whole = (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.W % 16 == 0 && a.ldx * el % 16 == 0 &&
                        (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
-    if (!whole) return launch_linear_any(a, s);
     const TileArgs k = tile_args(a);
     rgnn_status st;
     {
         LaunchScope ls("typed_linear", s);
-        if (a.dtype == RGNN_F32) st = a.trans_w ? launch_shape<F32, true>(k, s) : launch_shape<F32, false>(k, s);
-        else if (a.dtype == RGNN_BF16) st = a.trans_w ? launch_shape<BF16, true>(k, s) : launch_shape<BF16, false>(k, s);
-        else st = a.trans_w ? launch_shape<F16, true>(k, s) : launch_shape<F16, false>(k, s);
+        if (a.dtype == RGNN_F32) st = launch_type<F32>(k, a.trans_w, whole, s);
+        else if (a.dtype == RGNN_BF16) st = launch_type<BF16>(k, a.trans_w, whole, s);
+        else st = launch_type<F16>(k, a.trans_w, whole, s);
     }
     if (st != RGNN_OK) return st;
     hipError_t e = hipGetLastError();
@@ -525,7 +579,7 @@ rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s)
     rgnn_status st;
     {
         LaunchScope ls("typed_linear_fp8", s);
-        st = launch_shape<F8, true>(k, s);
+        st = launch_shape<F8, true, false>(k, s);
     }
     if (st != RGNN_OK) return st;
     hipError_t e = hipGetLastError();

@@ -27,7 +27,8 @@ struct WgradK {
     int64_t M;
     int K, N;
     void *dW;
-    int f32, vec;                // fp32 gradients; whole vectors of four are aligned
+    int f32;                     // fp32 gradients
+    const char *x_end, *dy_end;  // behind the last element
     int64_t chunk, slots;
     float *partial;
     int window;
@@ -73,6 +74,24 @@ struct Side {
             next[x] = i < end ? index[i] : -1;
         }
     }
+    // rows on any address: a step's loads into registers, and from there to LDS
+    __device__ __forceinline__ void take(i32x4 (&r)[L], const char *last, int lane)
+    {
+#pragma unroll
+        for (int x = 0; x < L; ++x) {
+            const int64_t i = pos + row_of(x, wave, lane);
+            const int64_t row = index ? (int64_t)next[x] : i;
+            const bool ok = i < end && row >= 0 && row < rows;
+            r[x] = ok ? load_any<E>(base + row * ld + col[x], last) : i32x4{0, 0, 0, 0};
+        }
+        pos += KE;
+        fetch(lane);
+    }
+    __device__ __forceinline__ void put(const i32x4 (&r)[L], char *lds, int lane) const
+    {
+#pragma unroll
+        for (int x = 0; x < L; ++x) *(i32x4 *)(lds + (x * NW + wave) * 1024 + lane * 16) = r[x];
+    }
     __device__ __forceinline__ void load(char *lds, int lane)
     {
 #pragma unroll
@@ -87,7 +106,8 @@ struct Side {
     }
 };
 
-template <class T, int BK, int BN, int WM, int WN>
+// ANY: rows on any address (typed_linear.hip).
+template <class T, int BK, int BN, int WM, int WN, bool ANY>
 __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
 {
     typedef typename T::elem E;
@@ -151,26 +171,57 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
     };
 
     const int steps = (int)((p1 - p0 + KE - 1) / KE);
-    if (steps > 0) {
-        x.load(sx0, lane);
-        y.load(sy0, lane);
-    }
     int step = 0;
-    for (; step + 2 <= steps; step += 2) {
-        step_barrier<0>();
-        x.load(sx1, lane);
-        y.load(sy1, lane);
-        multiply(sx0, sy0);
-        step_barrier<0>();
-        if (step + 2 < steps) {
+    if constexpr (ANY) {
+        i32x4 rx[Side<T, BK, NW>::L], ry[Side<T, BN, NW>::L];
+        auto take = [&]() {
+            x.take(rx, a.x_end, lane);
+            y.take(ry, a.dy_end, lane);
+        };
+        auto put = [&](char *lx, char *ly) {
+            x.put(rx, lx, lane);
+            y.put(ry, ly, lane);
+        };
+        if (steps > 0) {
+            take();
+            put(sx0, sy0);
+            if (steps > 1) take();
+        }
+        for (; step + 2 <= steps; step += 2) {
+            __syncthreads();
+            multiply(sx0, sy0);
+            put(sx1, sy1);
+            if (step + 2 < steps) take();
+            __syncthreads();
+            multiply(sx1, sy1);
+            if (step + 2 < steps) put(sx0, sy0);
+            if (step + 3 < steps) take();
+        }
+        if (step < steps) {
+            __syncthreads();
+            multiply(sx0, sy0);
+        }
+    } else {
+        if (steps > 0) {
             x.load(sx0, lane);
             y.load(sy0, lane);
         }
-        multiply(sx1, sy1);
-    }
-    if (step < steps) {
-        step_barrier<0>();
-        multiply(sx0, sy0);
+        for (; step + 2 <= steps; step += 2) {
+            step_barrier<0>();
+            x.load(sx1, lane);
+            y.load(sy1, lane);
+            multiply(sx0, sy0);
+            step_barrier<0>();
+            if (step + 2 < steps) {
+                x.load(sx0, lane);
+                y.load(sy0, lane);
+            }
+            multiply(sx1, sy1);
+        }
+        if (step < steps) {
+            step_barrier<0>();
+            multiply(sx0, sy0);
+        }
     }
 
     const bool split = p.end - p.begin > chunk;
@@ -186,10 +237,9 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
             const int n = ni * BN + (wn * FN + f) * 16 + g * 4;
             if (n >= a.N) continue;
             const int64_t at = (at0 + k) * a.N + n;
-            const bool whole = a.vec && n + 4 <= a.N;
-            if (split) write4(a.partial + at, acc[m][f], whole, a.N - n);
-            else if (sizeof(E) == 4 || a.f32) write4((float *)a.dW + at, acc[m][f], whole, a.N - n);
-            else write4((E *)a.dW + at, acc[m][f], whole, a.N - n);
+            if (split) write4(a.partial + at, acc[m][f], a.N - n);
+            else if (sizeof(E) == 4 || a.f32) write4((float *)a.dW + at, acc[m][f], a.N - n);
+            else write4((E *)a.dW + at, acc[m][f], a.N - n);
         }
     }
 }
@@ -269,7 +319,7 @@ __global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
     else __syncthreads();
 
     const int64_t at0 = (split ? slot : (int64_t)p.type) * a.K + k0;
-    if (!split && !a.f32 && a.vec && a.N % 8 == 0 && n0 + kWide <= a.N) {
+    if (!split && !a.f32 && n0 + kWide <= a.N) {
         char *mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
         wide_write<E, 4>(mine, acc, (E *)a.dW + at0 * a.N + n0 + wn * 128, a.N, lane, to + wm * 128);
         return;
@@ -286,10 +336,9 @@ __global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
                 if (j >= a.N) continue;
                 const int64_t at = (at0 + k) * a.N + j;
                 const f32x4 v = {acc[m][n][q * 4], acc[m][n][q * 4 + 1], acc[m][n][q * 4 + 2], acc[m][n][q * 4 + 3]};
-                const bool whole4 = a.vec && j + 4 <= a.N;
-                if (split) write4(a.partial + at, v, whole4, a.N - j);
-                else if (a.f32) write4((float *)a.dW + at, v, whole4, a.N - j);
-                else write4((E *)a.dW + at, v, whole4, a.N - j);
+                if (split) write4(a.partial + at, v, a.N - j);
+                else if (a.f32) write4((float *)a.dW + at, v, a.N - j);
+                else write4((E *)a.dW + at, v, a.N - j);
             }
     }
 }
@@ -346,14 +395,14 @@ void launch_join(const WgradArgs &a, const WgradPlan &plan, hipStream_t s)
     else hipLaunchKernelGGL((wgrad_join_kernel<E, 1>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, plan.chunk, kn, part, plan.slots, a.dW, f32);
 }
 
-template <class T, int BK, int BN, int WM, int WN>
+template <class T, int BK, int BN, int WM, int WN, bool ANY>
 rgnn_status launch_tile(WgradK k, hipStream_t s)
 {
     const int64_t tiles = (k.T + k.slots) * ((k.K + BK - 1) / BK) * ((k.N + BN - 1) / BN);
     k.window = xcd_window(tiles);
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    hipLaunchKernelGGL((typed_wgrad_kernel<T, BK, BN, WM, WN>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
+    hipLaunchKernelGGL((typed_wgrad_kernel<T, BK, BN, WM, WN, ANY>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
     return RGNN_OK;
 }
 
@@ -368,20 +417,25 @@ rgnn_status launch_wide(WgradK k, hipStream_t s)
     return RGNN_OK;
 }
 
-template <class T>
+template <class T, bool ANY>
 rgnn_status launch_shape(const WgradK &k, const WgradPlan &p, hipStream_t s)
 {
-    if constexpr (sizeof(typename T::elem) == 2)
-        if (p.bk == 256) {
-            // the wide tile takes rows as they are, at 32-bit offsets in a step
-            const int64_t ld = std::max(k.ldx, k.lddy);
-            if (!k.gather && !k.dy_gather && ld * kWide < (int64_t(1) << 32)) return launch_wide<T>(k, s);
-            return launch_tile<T, 128, 128, 2, 2>(k, s);
-        }
-    if (p.bk == 128 && p.bn == 128) return launch_tile<T, 128, 128, 2, 2>(k, s);
-    if (p.bk == 128) return launch_tile<T, 128, 64, 2, 2>(k, s);
-    if (p.bn == 128) return launch_tile<T, 64, 128, 2, 2>(k, s);
-    return launch_tile<T, 64, 64, 2, 2>(k, s);
+    if (p.bk == 256) {
+        // the wide tile takes rows as they are, at 32-bit offsets in a step
+        if constexpr (!ANY && sizeof(typename T::elem) == 2)
+            if (!k.gather && !k.dy_gather && std::max(k.ldx, k.lddy) * kWide < (int64_t(1) << 32)) return launch_wide<T>(k, s);
+        return launch_tile<T, 128, 128, 2, 2, ANY>(k, s);
+    }
+    if (p.bk == 128 && p.bn == 128) return launch_tile<T, 128, 128, 2, 2, ANY>(k, s);
+    if (p.bk == 128) return launch_tile<T, 128, 64, 2, 2, ANY>(k, s);
+    if (p.bn == 128) return launch_tile<T, 64, 128, 2, 2, ANY>(k, s);
+    return launch_tile<T, 64, 64, 2, 2, ANY>(k, s);
+}
+
+template <class T>
+rgnn_status launch_type(const WgradK &k, const WgradPlan &p, bool whole, hipStream_t s)
+{
+    return whole ? launch_shape<T, false>(k, p, s) : launch_shape<T, true>(k, p, s);
 }
 
 }  // namespace
@@ -415,19 +469,19 @@ rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
     const int el = dtype_bytes(a.dtype);
     const bool whole = (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.dY % 16 == 0 && a.ldx * el % 16 == 0 && a.lddy * el % 16 == 0 &&
                        (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
+    WgradK k{};
+    k.X = (const char *)a.X; k.x_rows = a.x_rows; k.ldx = a.ldx * el; k.gather = a.gather;
+    k.dY = (const char *)a.dY; k.dy_rows = a.dy_rows; k.lddy = a.lddy * el; k.dy_gather = a.dy_gather;
+    k.x_end = k.X + ((a.x_rows - 1) * a.ldx + a.K) * el;
+    k.dy_end = k.dY + ((a.dy_rows - 1) * a.lddy + a.N) * el;
+    k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
+    k.dW = a.dW; k.f32 = a.dw_dtype == RGNN_F32;
+    k.chunk = plan.chunk; k.slots = plan.slots; k.partial = (float *)a.ws;
     rgnn_status st;
-    if (!whole) {
-        st = launch_wgrad_any(a, plan, s);
-    } else {
-        WgradK k{};
-        k.X = (const char *)a.X; k.x_rows = a.x_rows; k.ldx = a.ldx * el; k.gather = a.gather;
-        k.dY = (const char *)a.dY; k.dy_rows = a.dy_rows; k.lddy = a.lddy * el; k.dy_gather = a.dy_gather;
-        k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
-        k.dW = a.dW; k.f32 = a.dw_dtype == RGNN_F32;
-        k.vec = (uintptr_t)a.dW % 16 == 0;           // N is a multiple of 4
-        k.chunk = plan.chunk; k.slots = plan.slots; k.partial = (float *)a.ws;
+    {
         LaunchScope ls("typed_wgrad", s);
-        st = a.dtype == RGNN_F32 ? launch_shape<F32>(k, plan, s) : a.dtype == RGNN_BF16 ? launch_shape<BF16>(k, plan, s) : launch_shape<F16>(k, plan, s);
+        st = a.dtype == RGNN_F32 ? launch_type<F32>(k, plan, whole, s)
+             : a.dtype == RGNN_BF16 ? launch_type<BF16>(k, plan, whole, s) : launch_type<F16>(k, plan, whole, s);
     }
     if (st != RGNN_OK) return st;
     if (plan.slots > 0) {

@@ -220,7 +220,7 @@ __device__ __forceinline__ void wide_write(char *lds, const f32x16 (&acc)[4][4],
         if (r & 16) v = i32x4{v[2], v[3], v[0], v[1]};
         int row = to[r];
         if (row < -1) { row = -2 - row; v = i32x4{0, 0, 0, 0}; }
-        if (row >= 0) *(i32x4 *)(y + row * ldy + c * 8) = v;
+        if (row >= 0) __builtin_memcpy(y + row * ldy + c * 8, &v, 16);   // on any address
     }
 }
 
