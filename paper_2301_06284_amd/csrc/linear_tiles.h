@@ -11,6 +11,13 @@ static __device__ const i32x4 kZeros = {0, 0, 0, 0};
 typedef const __attribute__((address_space(1))) uint32_t *global_ptr;
 typedef __attribute__((address_space(3))) uint32_t *lds_ptr;
 
+// 16 bytes, whatever the pointer was chosen from (a plain read of &kZeros or another would be a
+// flat one, which counts as an LDS instruction too).
+__device__ __forceinline__ i32x4 read_global(const char *p)
+{
+    return *(const __attribute__((address_space(1))) i32x4 *)p;
+}
+
 // 16 bytes of every lane's address to LDS, lane after lane from `lds` on
 __device__ __forceinline__ void load_lds(const char *from, char *lds)
 {
@@ -69,6 +76,20 @@ __device__ __forceinline__ void write4(O *y, f32x4 v, int n)
             if (q < n) y[q] = o[q];
 }
 
+// Eight 16-bit outputs side by side, or the first `n` of them (none for n <= 0), to any address.
+template <class O>
+__device__ __forceinline__ void write8(O *y, i32x4 v, int n)
+{
+    if (n >= 8) __builtin_memcpy(y, &v, 16);
+    else {
+        O o[8];
+        __builtin_memcpy(o, &v, 16);
+#pragma unroll
+        for (int q = 0; q < 7; ++q)
+            if (q < n) y[q] = o[q];
+    }
+}
+
 // Writes a wave's outputs in 16 bits through LDS (FM * FN * 512 bytes of its own), so that rows
 // go out in pieces as wide as the wave's columns: from the accumulators a store would take 32 bytes each of
 // 16 rows.  `y` points at the wave's first column, of which `cols` are the matrix's.  Chunk c of row r
@@ -99,16 +120,7 @@ __device__ __forceinline__ void write_rows(char *lds, const f32x4 (&acc)[FM][FN]
         i32x4 v = *(const i32x4 *)(lds + r * (CH * 16) + (c ^ turn(r)) * 16);
         int row = to[r];
         if (row < -1) { row = -2 - row; v = i32x4{0, 0, 0, 0}; }
-        if (row < 0 || left <= 0) continue;
-        O *at = y + row * ldy + c * 8;
-        if (left >= 8) __builtin_memcpy(at, &v, 16);
-        else {
-            O o[8];
-            __builtin_memcpy(o, &v, 16);
-#pragma unroll
-            for (int q = 0; q < 7; ++q)
-                if (q < left) at[q] = o[q];
-        }
+        if (row >= 0) write8(y + row * ldy + c * 8, v, left);
     }
 }
 

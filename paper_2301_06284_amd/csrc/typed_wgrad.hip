@@ -306,22 +306,22 @@ __global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
         sx.load_edge<kWideLoads>(ta, wave, in);
         sy.load_edge<kWideLoads>(tb, wave, in);
     };
-    auto multiply = [&](const i32x4 (&x)[4][2], const i32x4 (&y)[4][2], f32x16 (&c)[4][4]) {
+    auto multiply = [&](const i32x8 (&x)[4], const i32x8 (&y)[4], f32x16 (&c)[4][4]) {
 #pragma unroll
         for (int q = 0; q < 2; ++q)
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) c[m][n] = mma32<T>(y[n][q], x[m][q], c[m][n]);
+                for (int n = 0; n < 4; ++n) c[m][n] = mma32<T>(chunk_of(y[n], q), chunk_of(x[m], q), c[m][n]);
     };
     // a type without rows: nothing to walk, zeros to write
     if (steps > 0) wide_walk<4, true, true, LOADS>(a0, b0, a1, b1, a2, b2, a3, b3, fx, fy, steps, whole, load, edge, multiply, [](int) {}, acc);
     else __syncthreads();
 
     const int64_t at0 = (split ? slot : (int64_t)p.type) * a.K + k0;
-    if (!split && !a.f32 && n0 + kWide <= a.N) {
+    if (!split && !a.f32) {
         char *mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
-        wide_write<E, 4>(mine, acc, (E *)a.dW + at0 * a.N + n0 + wn * 128, a.N, lane, to + wm * 128);
+        wide_write<E, 4>(mine, acc, (E *)a.dW + at0 * a.N + n0 + wn * 128, a.N, a.N - n0 - wn * 128, lane, to + wm * 128);
         return;
     }
 #pragma unroll
@@ -337,8 +337,7 @@ __global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
                 const int64_t at = (at0 + k) * a.N + j;
                 const f32x4 v = {acc[m][n][q * 4], acc[m][n][q * 4 + 1], acc[m][n][q * 4 + 2], acc[m][n][q * 4 + 3]};
                 if (split) write4(a.partial + at, v, a.N - j);
-                else if (a.f32) write4((float *)a.dW + at, v, a.N - j);
-                else write4((E *)a.dW + at, v, a.N - j);
+                else write4((float *)a.dW + at, v, a.N - j);
             }
     }
 }
@@ -450,7 +449,7 @@ WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
     if (dtype != RGNN_F32 && K > 128 && N > 128 && (int64_t)((K + 255) / 256) * ((N + 255) / 256) * T >= 256) p.bk = p.bn = 256;
     // pieces: enough workgroups over all tiles, and rows enough to pay for a piece's sums,
     // which are written and read back in fp32
-    const int64_t want = p.bk == 256 ? 512 : 2048, least = p.bk == 256 ? 4096 : 1024;
+    const int64_t want = 512, least = p.bk == 256 ? 4096 : 128;
     p.chunk = std::max<int64_t>(least, (M * tiles() + want - 1) / want);
     p.chunk = (p.chunk + 63) / 64 * 64;
     // ceil(c / chunk) <= 2 c / chunk where c > chunk; written so that it never falls as M grows

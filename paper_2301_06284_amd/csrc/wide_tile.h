@@ -35,6 +35,12 @@ __device__ __forceinline__ f32x16 mma32<F16>(i32x4 a, i32x4 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// Chunk q of a fragment.
+__device__ __forceinline__ i32x4 chunk_of(i32x8 v, int q)
+{
+    return q ? __builtin_shufflevector(v, v, 4, 5, 6, 7) : __builtin_shufflevector(v, v, 0, 1, 2, 3);
+}
+
 // LDS rows of 64 bytes of k: chunk c of row r lies at c ^ (r >> 3 & 3).  A 16-byte read takes lanes
 // 0-3, 12-15, 20-23, 24-27 of 32 together and the others together: with this turn their chunks
 // lie in different banks (no conflicts by the counters).
@@ -97,15 +103,12 @@ __device__ __forceinline__ void wide_walk(char *a0, char *b0, char *a1, char *b1
                                           const WideFragments<ACOLS> &fa, const WideFragments<BCOLS> &fb, int steps, int whole,
                                           Load load, Edge edge, Multiply multiply, Shift shift, f32x16 (&acc)[4][4])
 {
-    struct Set { i32x4 a[FMV][2], b[4][2]; };
+    struct Set { i32x8 a[FMV], b[4]; };      // both chunks side by side
     auto fetch = [&](Set &s, const char *a, const char *b) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int n = 0; n < 4; ++n) s.b[n] = __builtin_shufflevector(fb.read(b, n, 0), fb.read(b, n, 1), 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-            for (int n = 0; n < 4; ++n) s.b[n][q] = fb.read(b, n, q);
-#pragma unroll
-            for (int m = 0; m < FMV; ++m) s.a[m][q] = fa.read(a, m, q);
-        }
+        for (int m = 0; m < FMV; ++m) s.a[m] = __builtin_shufflevector(fa.read(a, m, 0), fa.read(a, m, 1), 0, 1, 2, 3, 4, 5, 6, 7);
     };
     // A wave's instructions issue in order: a load into LDS that waits for its turn holds up the
     // products behind it.  So reads and loads go between the products, as evenly as they can.
@@ -195,10 +198,11 @@ __device__ __forceinline__ void wide_walk(char *a0, char *b0, char *a1, char *b1
 
 // Writes a wave's FMV x 128 x 128 / 4 outputs in 16 bits through LDS (32 KB of its own), so that
 // rows go out as whole pieces of 256 bytes: from the accumulators a store would take 16 bytes each
-// of 32 rows.  Chunk c of row r lies at c ^ (r & 15), its halves exchanged where r & 16.
+// of 32 rows.  `y` points at the wave's first column, of which `cols` are the matrix's.  Chunk c of row r lies at c ^ (r & 15), its halves exchanged where r & 16.
 // to[r]: where row r of the wave goes, -1 nowhere; below -1: zeros to row -2 - to[r].
 template <class O, int FMV>
-__device__ __forceinline__ void wide_write(char *lds, const f32x16 (&acc)[4][4], O *y, int64_t ldy, int lane, const int *to)
+__device__ __forceinline__ void wide_write(char *lds, const f32x16 (&acc)[4][4], O *y, int64_t ldy, int cols, int lane,
+                                           const int *to)
 {
     const int r32 = lane & 31, half = (lane >> 5) ^ (r32 >> 4);
 #pragma unroll
@@ -220,7 +224,7 @@ __device__ __forceinline__ void wide_write(char *lds, const f32x16 (&acc)[4][4],
         if (r & 16) v = i32x4{v[2], v[3], v[0], v[1]};
         int row = to[r];
         if (row < -1) { row = -2 - row; v = i32x4{0, 0, 0, 0}; }
-        if (row >= 0) __builtin_memcpy(y + row * ldy + c * 8, &v, 16);   // on any address
+        if (row >= 0) write8(y + row * ldy + c * 8, v, cols - c * 8);
     }
 }
 
