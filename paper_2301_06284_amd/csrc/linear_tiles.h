@@ -11,13 +11,6 @@ static __device__ const i32x4 kZeros = {0, 0, 0, 0};
 typedef const __attribute__((address_space(1))) uint32_t *global_ptr;
 typedef __attribute__((address_space(3))) uint32_t *lds_ptr;
 
-// 16 bytes, whatever the pointer was chosen from (a plain read of &kZeros or another would be a
-// flat one, which counts as an LDS instruction too).
-__device__ __forceinline__ i32x4 read_global(const char *p)
-{
-    return *(const __attribute__((address_space(1))) i32x4 *)p;
-}
-
 // 16 bytes of every lane's address to LDS, lane after lane from `lds` on
 __device__ __forceinline__ void load_lds(const char *from, char *lds)
 {

@@ -65,7 +65,8 @@ __device__ __forceinline__ void tile_row(const TileArgs &a, int64_t i, int64_t e
 
 // ANY: rows on any address.  Loads go through registers (16 bytes from any address; at the end of
 // k and of the matrix by elements) and are written to LDS a step later.  STAGES: 1 where all of k is
-// one step, which leaves LDS and registers for more workgroups on a CU.
+// one step, which leaves LDS and registers for more workgroups on a CU; 4 where a CU has few of them and
+// memory's latency is theirs to bear.
 template <class T, int BM, int BN, int WM, int WN, bool TRANS, bool ANY, int STAGES>
 __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a)
 {
@@ -76,8 +77,10 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;       // KB that a wave loads each step
     static_assert(NA * 8 * NW == BM && NB * 8 * NW == BN && NW % 2 == 0 && BM <= NW * 64, "whole loads");
     __shared__ __attribute__((aligned(1024))) char s0[(BM + BN) * 128], s1[STAGES > 1 ? (BM + BN) * 128 : 16];
+    __shared__ __attribute__((aligned(1024))) char s2[STAGES > 2 ? (BM + BN) * 128 : 16], s3[STAGES > 2 ? (BM + BN) * 128 : 16];
     __shared__ int from[BM], to[BM];
     char *sa0 = s0, *sb0 = s0 + BM * 128, *sa1 = s1, *sb1 = s1 + (STAGES > 1 ? BM * 128 : 0);
+    char *sa2 = s2, *sb2 = s2 + (STAGES > 2 ? BM * 128 : 0), *sa3 = s3, *sb3 = s3 + (STAGES > 2 ? BM * 128 : 0);
 
     const int nt = (a.N + BN - 1) / BN;
     Piece p;
@@ -123,30 +126,7 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     }
     const int kbytes = a.K * (int)sizeof(E);
     const int steps = (kbytes + 127) / 128;
-    // fp8: a word of scale bytes is four steps.  Those of the rows go through LDS, one row a
-    // lane; those of the weights are one for a wave, whose columns lie in one block of 128.
-    constexpr bool SCALES = FP8;
-    __shared__ __attribute__((aligned(256))) char sx0[SCALES ? BM * 4 : 4], sx1[SCALES ? BM * 4 : 4];
-    const char *xp = zeros;
-    int xinc = 0, sx[SCALES ? FM : 1], sw = 0;
-    const uint8_t *wp = nullptr;
-    if constexpr (SCALES) {
-        static_assert(BM / 64 <= NW && FN * 16 <= 128 && 128 % (FN * 16) == 0, "scales");
-        if (wave < BM / 64) {
-            const int row = from[wave * 64 + lane];
-            if (row >= 0) { xp = (const char *)a.xs + (int64_t)row * a.ks; xinc = 4; }
-        }
-        const int jb = min(j0 + wave % WN * FN * 16, a.N - 1) / 128;
-        wp = a.ws + ((int64_t)p.type * a.nb + jb) * a.ks;
-    }
     auto load = [&](char *sa, char *sb, int step) {
-        if constexpr (SCALES) {
-            if ((step & 3) == 0 && wave < BM / 64) {
-                char *at = step & 4 ? sx1 : sx0;
-                __builtin_amdgcn_global_load_lds((global_ptr)xp, (lds_ptr)(at + wave * 256), 4, 0, 0);
-                xp += xinc;
-            }
-        }
         const bool tail = (step + 1) * 128 > kbytes;
 #pragma unroll
         for (int x = 0; x < NA; ++x) {
@@ -210,14 +190,38 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     }
     f32x4 acc[FM][FN] = {};
 
-    // before the next loads are issued: a read of LDS that they might write would wait for them
-    auto scales = [&](int step) {
-        if constexpr (SCALES) {
-            if ((step & 3) == 0) {
-                const char *at = (step & 4 ? sx1 : sx0) + (wm * FM * 16 + r16) * 4;
+    // fp8: the scale bytes of this lane's rows and of the weights, whose columns of a wave lie in one
+    // block of 128.  A word is four steps; the next one is read a word ahead.
+    const char *xs[FP8 ? FM : 1];
+    const uint8_t *wp = nullptr;
+    int sx[FP8 ? FM : 1], nx[FP8 ? FM : 1], sw = 0, nw = 0;
+    uint32_t xin = 0;
+    if constexpr (FP8) {
+        static_assert(FN * 16 <= 128 && 128 % (FN * 16) == 0, "scales");
 #pragma unroll
-                for (int f = 0; f < FM; ++f) sx[f] = *(const int *)(at + f * 64);
-                sw = *(const int *)(wp + step);
+        for (int m = 0; m < FM; ++m) {
+            const int row = from[(wm * FM + m) * 16 + r16];
+            xs[m] = row >= 0 ? (const char *)a.xs + (int64_t)row * a.ks : zeros;
+            xin |= (row >= 0 ? 4u : 0u) << m * 3;
+            nx[m] = *(const __attribute__((address_space(1))) int *)xs[m];
+        }
+        wp = a.ws + ((int64_t)p.type * a.nb + min(j0 + wn * FN * 16, a.N - 1) / 128) * a.ks;
+        nw = *(const int *)wp;
+    }
+    auto scales = [&](int step) {
+        if constexpr (FP8) {
+            if ((step & 3) == 0) {
+                sw = nw;
+#pragma unroll
+                for (int m = 0; m < FM; ++m) sx[m] = nx[m];
+                if (step + 4 < a.ks) {
+                    nw = *(const int *)(wp + step + 4);
+#pragma unroll
+                    for (int m = 0; m < FM; ++m) {
+                        xs[m] += xin >> m * 3 & 4;
+                        nx[m] = *(const __attribute__((address_space(1))) int *)xs[m];
+                    }
+                }
             }
         }
     };
@@ -278,6 +282,37 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
         step_barrier<0>();
         scales(0);
         multiply(sa0, sb0);
+    } else if constexpr (STAGES == 4) {
+        // three steps under way, in whole rounds of four: what lies behind K is zeros
+        constexpr int ONE = NA + NB;
+        load(sa0, sb0, 0);
+        load(sa1, sb1, 1);
+        load(sa2, sb2, 2);
+        for (; step + 4 < steps; step += 4) {
+            step_barrier<2 * ONE>();
+            load(sa3, sb3, step + 3);
+            scales(step);
+            multiply(sa0, sb0);
+            step_barrier<2 * ONE>();
+            load(sa0, sb0, step + 4);
+            multiply(sa1, sb1);
+            step_barrier<2 * ONE>();
+            load(sa1, sb1, step + 5);
+            multiply(sa2, sb2);
+            step_barrier<2 * ONE>();
+            load(sa2, sb2, step + 6);
+            multiply(sa3, sb3);
+        }
+        step_barrier<2 * ONE>();
+        load(sa3, sb3, step + 3);
+        scales(step);
+        multiply(sa0, sb0);
+        step_barrier<2 * ONE>();
+        multiply(sa1, sb1);
+        step_barrier<ONE>();
+        multiply(sa2, sb2);
+        step_barrier<0>();
+        multiply(sa3, sb3);
     } else if constexpr (ANY) {
         fetch(0);
         put(sa0, sb0);
@@ -494,187 +529,6 @@ __global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
     else walk(std::integral_constant<int, 4>());
 }
 
-// Few rows (BM = 16 FM): the weights' bytes are what it costs, so they stream through registers,
-// DEPTH steps under way in each wave, and the waves of a workgroup take k in turn and add their
-// sums in LDS, in order.  Nothing is shared before that, so no wave waits for another.
-//   Weights as rows of k: 16 rows of 128 bytes are a fragment as they arrive.
-//   Rows of n: 32 k of 16 FN columns go through 32 rows of LDS of the wave's own to the
-//     transposing read.  A wave's LDS instructions stay in order, so one buffer does.
-template <class T, int FM, int FN, bool TRANS>
-__global__ __launch_bounds__(512, FM == 1 ? 4 : 2) void typed_linear_few_kernel(TileArgs a)
-{
-    typedef typename T::elem E;
-    constexpr bool FP8 = sizeof(E) == 1;
-    constexpr int NW = 8, BM = FM * 16, BN = FN * 16;
-    constexpr int KE = TRANS ? 128 / sizeof(E) : 32, KC = KE * sizeof(E) / 64;    // k of a step, 64-byte parts of it
-    constexpr int LW = TRANS ? 2 * FN : FN, DEPTH = FP8 ? 2 : 3;
-    constexpr int ROW = BN * 2, CH = ROW / 16;       // rows of n in LDS: bytes, chunks
-    __shared__ __attribute__((aligned(1024))) float sums[NW][BM * BN];
-    __shared__ __attribute__((aligned(1024))) char turn_lds[TRANS ? 16 : NW * 32 * ROW];
-    __shared__ int from[BM], to[BM];
-    static_assert(TRANS || (FN * 64 * 16 == 32 * ROW), "whole loads");
-
-    const int nt = (a.N + BN - 1) / BN;
-    Piece p;
-    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return (c + BM - 1) / BM * nt; }, NoWeight(), p))
-        return;
-    int mi, ni;
-    tile_place(p.index, (int)((p.end - p.begin + BM - 1) / BM), nt, mi, ni);
-    const int64_t i0 = p.begin + (int64_t)mi * BM;
-    const int j0 = ni * BN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r16 = lane & 15, g = lane >> 4;
-    if (threadIdx.x < BM) tile_row(a, i0 + threadIdx.x, p.end, from[threadIdx.x], to[threadIdx.x]);
-
-    // A load's address is a base that all lanes share and moves with the step, and an offset that
-    // does not; only a step that K does not fill looks at each lane's k.  The weights do not wait
-    // for the rows' places.
-    const char *W = a.W + (int64_t)p.type * a.w_type + (TRANS ? j0 * a.w_row : j0 * (int64_t)sizeof(E));
-    const int64_t wstep = TRANS ? KE * (int64_t)sizeof(E) : KE * a.w_row;
-    const int steps = (a.K + KE - 1) / KE, whole = a.K / KE;
-    uint32_t woff[LW];
-    int wk[LW];                                      // k in a step
-#pragma unroll
-    for (int x = 0; x < LW; ++x) {
-        if (TRANS) {
-            wk[x] = g * (16 / (int)sizeof(E)) + (x & 1) * (KE / 2);
-            woff[x] = (uint32_t)(min((x >> 1) * 16 + r16, a.N - 1 - j0) * a.w_row) + wk[x] * (uint32_t)sizeof(E);
-        } else {
-            const int at = x * 64 + lane, j = at % CH * 8;
-            wk[x] = at / CH;
-            woff[x] = (uint32_t)(wk[x] * a.w_row) + (j0 + j < a.N ? j : 0) * 2;
-        }
-    }
-    i32x4 w[DEPTH][LW], v[DEPTH][KC * FM];
-    auto load_w = [&](i32x4 (&r)[LW], int step) {
-        const char *base = W + step * wstep;
-        if (step < whole) {
-#pragma unroll
-            for (int x = 0; x < LW; ++x) r[x] = read_global(base + woff[x]);
-        } else {
-#pragma unroll
-            for (int x = 0; x < LW; ++x) r[x] = read_global(step * KE + wk[x] < a.K ? base + woff[x] : (const char *)&kZeros);
-        }
-    };
-    const char *xp[FM];
-    uint32_t xok = 0;                                // bit m: row m is one of X
-    // fp8: the scales of the lane's rows, and the weights', whose 64 columns lie in one block.  Behind
-    // the last step the codes are zeros and the scales the last one's.
-    const char *xs[FP8 ? FM : 1];
-    int xinc[FP8 ? FM : 1], sx[DEPTH][FP8 ? FM : 1], sw[DEPTH];
-    const uint8_t *ws = FP8 ? a.ws + ((int64_t)p.type * a.nb + j0 / 128) * a.ks : nullptr;
-    static_assert(128 % BN == 0, "columns of one block");
-    auto load_x = [&](i32x4 (&r)[KC * FM], int (&rs)[FP8 ? FM : 1], int &wscale, int step) {
-        if constexpr (FP8) {
-            const int at = min(step, steps - 1);
-            wscale = ws[at];
-#pragma unroll
-            for (int m = 0; m < FM; ++m) rs[m] = *(const __attribute__((address_space(1))) uint8_t *)(xs[m] + at * xinc[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < FM; ++m)
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                // a row of zeros stays where it is
-                const int k = step * KE + g * (16 / (int)sizeof(E)) + c * (KE / 2);
-                r[m * KC + c] = read_global(xok >> m & 1 && k < a.K ? xp[m] + (uint32_t)k * (uint32_t)sizeof(E) : (const char *)&kZeros);
-            }
-    };
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) load_w(w[d], wave + d * NW);
-    __syncthreads();
-#pragma unroll
-    for (int m = 0; m < FM; ++m) {
-        const int row = from[m * 16 + r16];
-        xok |= (row >= 0 ? 1u : 0u) << m;
-        xp[m] = row >= 0 ? a.X + row * a.ldx : (const char *)&kZeros;
-        if constexpr (FP8) {
-            xs[m] = row >= 0 ? (const char *)a.xs + (int64_t)row * a.ks : (const char *)&kZeros;
-            xinc[m] = row >= 0 ? 1 : 0;
-        }
-    }
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) load_x(v[d], sx[d], sw[d], wave + d * NW);
-
-    char *mine = turn_lds + wave * (32 * ROW);
-    f32x4 acc[FM][FN] = {};
-    auto turn = [](int k) { return FN >= 4 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k >> 3) & 1; };   // of units of 32 bytes
-    auto multiply = [&](const i32x4 (&x)[LW], const i32x4 (&y)[KC * FM], const int (&rs)[FP8 ? FM : 1], int wscale) {
-        if constexpr (FP8) {
-#pragma unroll
-            for (int m = 0; m < FM; ++m)
-#pragma unroll
-                for (int f = 0; f < FN; ++f)
-                    acc[m][f] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                        __builtin_shufflevector(x[2 * f], x[2 * f + 1], 0, 1, 2, 3, 4, 5, 6, 7),
-                        __builtin_shufflevector(y[2 * m], y[2 * m + 1], 0, 1, 2, 3, 4, 5, 6, 7), acc[m][f], 0, 0, 0, wscale, 0, rs[m]);
-        } else if constexpr (TRANS) {
-#pragma unroll
-            for (int c = 0; c < KC; ++c)
-#pragma unroll
-                for (int m = 0; m < FM; ++m)
-#pragma unroll
-                    for (int f = 0; f < FN; ++f) acc[m][f] = mma16<T>(x[2 * f + c], y[m * KC + c], acc[m][f]);
-        } else {
-#pragma unroll
-            for (int q = 0; q < LW; ++q) {
-                const int at = q * 64 + lane, k = at / CH, c = at % CH;
-                *(i32x4 *)(mine + k * ROW + ((c >> 1) ^ turn(k)) * 32 + (c & 1) * 16) = x[q];
-            }
-            const int k = g * 8 + (r16 >> 2);
-#pragma unroll
-            for (int f = 0; f < FN; ++f) {
-                const char *at = mine + k * ROW + (f ^ turn(k)) * 32 + (r16 & 3) * 8;
-                const uint64_t lo = read_turned(at), hi = read_turned(at + 4 * ROW);
-                const i32x4 b = {(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
-#pragma unroll
-                for (int m = 0; m < FM; ++m) acc[m][f] = mma16<T>(b, y[m], acc[m][f]);
-            }
-        }
-    };
-    // steps wave, wave + NW, ...; those behind the last are zeros
-    for (int s = wave; s < steps; s += NW * DEPTH) {
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            multiply(w[d], v[d], sx[d], sw[d]);
-            load_w(w[d], s + (d + DEPTH) * NW);
-            load_x(v[d], sx[d], sw[d], s + (d + DEPTH) * NW);
-        }
-    }
-
-#pragma unroll
-    for (int m = 0; m < FM; ++m)
-#pragma unroll
-        for (int f = 0; f < FN; ++f) *(f32x4 *)&sums[wave][(m * 16 + r16) * BN + f * 16 + g * 4] = acc[m][f];
-    __syncthreads();
-    for (int q = threadIdx.x; q < BM * BN / 4; q += NW * 64) {
-        const int r = q / (BN / 4), j = j0 + q % (BN / 4) * 4;
-        int row = to[r];
-        const bool zero = row < -1;
-        if (zero) row = -2 - row;
-        if (row < 0) continue;
-        f32x4 s = {0, 0, 0, 0};
-#pragma unroll
-        for (int n = 0; n < NW; ++n) s += *(const f32x4 *)&sums[n][q * 4];
-        if (zero) s = f32x4{0, 0, 0, 0};
-        const int64_t at = row * a.ldy + j;
-        if (a.y_f32) write4((float *)a.Y + at, s, a.N - j);
-        else if (FP8 && a.y_f16) write4((_Float16 *)a.Y + at, s, a.N - j);
-        else write4((typename std::conditional<FP8, __bf16, E>::type *)a.Y + at, s, a.N - j);
-    }
-}
-
-template <class T, int FM, int FN, bool TRANS>
-rgnn_status launch_few(TileArgs k, hipStream_t s)
-{
-    const int64_t tiles = row_tiles_bound(k.M, k.T, FM * 16) * ((k.N + FN * 16 - 1) / (FN * 16));
-    k.window = xcd_window(tiles);
-    const int64_t grid = xcd_grid(tiles, k.window);
-    if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    hipLaunchKernelGGL((typed_linear_few_kernel<T, FM, FN, TRANS>), dim3((uint32_t)grid), dim3(512), 0, s, k);
-    return RGNN_OK;
-}
-
 template <class T, bool TRANS>
 rgnn_status launch_wide(TileArgs k, hipStream_t s)
 {
@@ -686,7 +540,7 @@ rgnn_status launch_wide(TileArgs k, hipStream_t s)
     return RGNN_OK;
 }
 
-template <class T, int BM, int BN, int WM, int WN, bool TRANS, bool ANY>
+template <class T, int BM, int BN, int WM, int WN, bool TRANS, bool ANY, bool DEEP = false>
 rgnn_status launch_tile(TileArgs k, hipStream_t s)
 {
     const int64_t tiles = row_tiles_bound(k.M, k.T, BM) * ((k.N + BN - 1) / BN);
@@ -697,15 +551,15 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
     if (k.K * (int)sizeof(typename T::elem) <= 128)
         hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, 1>), g, b, 0, s, k);
     else
-        hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, 2>), g, b, 0, s, k);
+        hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, DEEP ? 4 : 2>), g, b, 0, s, k);
     return RGNN_OK;
 }
 
-// Which tile: each is priced by what it measured (us; 16384 and fewer rows, k of 512 to 4096, one to
-// 32 types) and the cheapest is taken.  `slots` workgroups fit the chip; a round of them costs `each`
-// and, for each KB of k of a row, `full`, down to `light` where a CU has few of them.  fp32 is bound by its
-// matrix cores, which take 7 us for 64 x 128 outputs and a KB of k.  The estimate of the
-// row tiles: every type that has rows leaves half a tile, and has one at least.
+// Which tile: each is priced by what it measured (us; 16 to 16384 rows, k of 512 to 4096, one to 32
+// types) and the cheapest is taken.  `slots` workgroups fit the chip; a round of them costs `each` and, for
+// each KB of k of a row, `full`, down to `light` where few of the slots are taken.  The deep ones, with
+// four stages, are for few tiles: 16 rows, 4096 x 4096 22 us (64 x 128 with two stages 47), 1024 rows 57
+// (46).  fp32 is bound by its matrix cores, which take 7 us for 64 x 128 outputs and a KB of k.
 struct TileCost {
     int bm, bn, slots;
     double each, light, full;
@@ -714,11 +568,15 @@ constexpr TileCost kCostWide = {256, 256, 256, 7.0, 12.5, 12.5};
 constexpr TileCost kCost128 = {128, 128, 512, 3.0, 6.0, 8.5};
 constexpr TileCost kCost64 = {64, 128, 768, 2.5, 4.65, 7.7};
 constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 5.15, 7.2};
+constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 2.9};
+constexpr TileCost kCostDeep128 = {64, 128, 256, 2.0, 2.9, 3.1};
 
 double tile_cost(const TileArgs &k, const TileCost &c, int el)
 {
+    // every type that has rows leaves half a tile, and has one at least
     const double types = (double)std::min<int64_t>(k.M, k.T);
-    const double tiles = std::max((double)k.M / c.bm + types / 2, types) * ((k.N + c.bn - 1) / c.bn);
+    const double rows = types == 1 ? std::ceil((double)k.M / c.bm) : std::max((double)k.M / c.bm + types / 2, types);
+    const double tiles = rows * ((k.N + c.bn - 1) / c.bn);
     const double kb = (double)k.K * el / 1024, f32 = c.bm * c.bn / (64.0 * 128) * 7;
     const double light = el == 4 ? f32 : c.light, full = el == 4 ? f32 * c.slots / 256 : c.full;
     const double rounds = std::floor(tiles / c.slots), rest = tiles / c.slots - rounds;
@@ -729,24 +587,18 @@ template <class T, bool TRANS, bool ANY>
 rgnn_status launch_shape(const TileArgs &k, hipStream_t s)
 {
     constexpr int el = sizeof(typename T::elem);
-    const int64_t types = std::min<int64_t>(k.M, k.T), rows = k.M / types;
     const double narrow = tile_cost(k, kCostNarrow, el), c64 = tile_cost(k, kCost64, el), c128 = tile_cost(k, kCost128, el);
     const double best = std::min(narrow, std::min(c64, c128));
     if constexpr (!ANY && el != 4) {
-        // Few rows of each type: the weights stream through registers.  16 tokens, 2048 x 1536 of 32
-        // types 20.4 us (64 x 128 tiles 22.6), 4096 x 4096 of one 15 (47); up to 64 rows only where those
-        // tiles are few (64 rows, one type 21 against 49; 512 rows of 16 types 36 against 23).
-        if (64 * k.w_row < (int64_t(1) << 32)) {     // its offsets have 32 bits
-            if (rows <= 8) {
-                if (TRANS || types * ((k.N + 63) / 64) < 256) return launch_few<T, 1, 2, TRANS>(k, s);
-                return launch_few<T, 1, TRANS ? 2 : 4, TRANS>(k, s);
-            }
-            if (rows <= 64 && types * ((k.N + 127) / 128) < 128) return launch_few<T, 2, 2, TRANS>(k, s);
-        }
         // the wide tile's offsets have 32 bits
         const bool near = k.x_rows > 0 && (k.gather ? k.x_rows : (int64_t)kWide) * k.ldx < (int64_t(1) << 32) &&
                           kWide * k.w_row < (int64_t(1) << 32);
-        if (near && tile_cost(k, kCostWide, el) < best) return launch_wide<T, TRANS>(k, s);
+        const double wide = tile_cost(k, kCostWide, el), deep = tile_cost(k, kCostDeep, el), deep128 = tile_cost(k, kCostDeep128, el);
+        if (near && wide < std::min(best, std::min(deep, deep128))) return launch_wide<T, TRANS>(k, s);
+        if (k.K * el > 128) {      // more than one step
+            if (deep < std::min(best, deep128)) return launch_tile<T, 64, 64, 2, 2, TRANS, ANY, true>(k, s);
+            if (deep128 < best) return launch_tile<T, 64, 128, 1, 4, TRANS, ANY, true>(k, s);
+        }
     }
     if (narrow == best) return launch_tile<T, 128, 64, 4, 1, TRANS, ANY>(k, s);
     if (c64 == best) return launch_tile<T, 64, 128, 1, 4, TRANS, ANY>(k, s);
