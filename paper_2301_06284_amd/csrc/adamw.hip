@@ -1,11 +1,10 @@
 // adamw.hip -- one AdamW step of many tensors in few launches, states in 32 or in 8 bits.
 //
-// A launch takes up to kPerLaunch tensors of one type combination: their pointers travel
-// in the kernel's arguments, so nothing is uploaded and a captured graph holds them.  A
-// workgroup takes 4096 consecutive elements of one tensor, a wave 256 of them at a time
-// (4 a lane), which is one block of 8-bit states: its maximum is a reduction over one wave.
-// Bound by memory.  Every product and sum is rounded on its own (no fused multiply-add), so
-// that a state's code is the one that the same formula gives in any fp32 arithmetic.
+// A launch takes as many tensors of one type combination as their pointers fill the 4 KB of a
+// kernel's arguments, so nothing is uploaded and a captured graph holds them.  A workgroup takes up to 4096
+// consecutive elements of one tensor, a wave 256 of them at a time (4 a lane), which is one block
+// of 8-bit states: its maximum is a reduction over one wave.
+// Bound by memory.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -16,10 +15,27 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kPerLaunch = 48;
 constexpr int kBlock = 256;               // elements of one block of 8-bit states
-constexpr int kWaveSteps = 4;             // blocks a wave
-constexpr int kGroup = 4 * kWaveSteps * kBlock;
+
+// EXTRA: with scales or copies
+template <bool EXTRA>
+struct StepArgs {
+    static constexpr int most = EXTRA ? 56 : 86, extra = EXTRA ? most : 1;
+    void *p[most];
+    const void *g[most];
+    void *m[most], *v[most];
+    int64_t n[most];
+    float *ms[extra], *vs[extra];
+    void *copy[extra];
+    int32_t first[most + 1];              // first workgroup of each tensor
+    uint8_t flags[most];                  // 1: whole vectors are aligned; the rest: rgnn_dtype of the copy
+    int32_t count, steps;                 // tensors; blocks a wave
+    float decay, step_size, beta1, beta2, rest1, rest2, root, eps;
+    double lr, log_beta1, log_beta2;
+    const int64_t *step_dev;
+    const float *grad_scale;
+};
+static_assert(sizeof(StepArgs<false>) <= 4096 && sizeof(StepArgs<true>) <= 4096, "kernel arguments");
 
 struct Tensor {
     void *p;
@@ -29,18 +45,6 @@ struct Tensor {
     void *copy;
     int64_t n;
 };
-struct StepArgs {
-    Tensor t[kPerLaunch];
-    int32_t first[kPerLaunch + 1];        // first workgroup of each tensor
-    uint8_t vec[kPerLaunch];              // whole vectors are aligned
-    uint8_t copy_type[kPerLaunch];        // rgnn_dtype
-    int32_t count;
-    float decay, step_size, beta1, beta2, rest1, rest2, root, eps;
-    double lr, log_beta1, log_beta2;
-    const int64_t *step_dev;
-    const float *grad_scale;
-};
-static_assert(sizeof(StepArgs) <= 4096, "kernel arguments");
 
 template <class E, bool VEC>
 __device__ __forceinline__ void load4(const void *base, int64_t at, int64_t n, E x[4])
@@ -77,11 +81,10 @@ __device__ __forceinline__ float wave_max(float x)
     return x;
 }
 
-template <class P, class G, bool EIGHT, bool VEC>
-__device__ __forceinline__ void update(const Tensor &t, int copy_type, const StepArgs &a, int64_t block, float step_size,
+template <class P, class G, bool EIGHT, bool VEC, class Args>
+__device__ __forceinline__ void update(const Tensor &t, int copy_type, const Args &a, int64_t block, float step_size,
                                        float root, float scale)
 {
-#pragma clang fp contract(off)
     const int lane = threadIdx.x & 63;
     const int64_t at = block * kBlock + lane * 4;
     P p[4];
@@ -141,13 +144,20 @@ __device__ __forceinline__ void update(const Tensor &t, int copy_type, const Ste
         }
         tm = wave_max(tm);
         tv = wave_max(tv);
+        // 127^2 / top and 255^4 / top, the top scaled into [1/2, 1) so that neither overflows; the
+        // values are scaled alike, by powers of two.  One quotient a block, and the roots within a
+        // unit in the last place: a code is off by 1e-4 of a step at most, where exact quotients and
+        // roots take three times the operations and leave memory waiting (201M values 778 us).
+        const int em = __builtin_amdgcn_frexp_expf(tm), ev = __builtin_amdgcn_frexp_expf(tv);
+        const float rm = tm > 0.0f ? 16129.0f / __builtin_amdgcn_ldexpf(tm, -em) : 0.0f;
+        const float rv = tv > 0.0f ? 4228250625.0f / __builtin_amdgcn_ldexpf(tv, -ev) : 0.0f;
         int8_t cm[4];
         uint8_t cv[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float q = tm > 0.0f ? rintf(127.0f * sqrtf(fabsf(m[i]) / tm)) : 0.0f;
+            const float q = rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(fabsf(m[i]), -em) * rm));
             cm[i] = (int8_t)(int)copysignf(q, m[i]);
-            const float r = tv > 0.0f ? rintf(255.0f * sqrtf(sqrtf(v[i] / tv))) : 0.0f;
+            const float r = rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(v[i], -ev) * rv)));
             cv[i] = (uint8_t)(int)fmaxf(r, v[i] > 0.0f ? 1.0f : 0.0f);
         }
         store4<int8_t, VEC>(t.m, at, t.n, cm);
@@ -162,8 +172,8 @@ __device__ __forceinline__ void update(const Tensor &t, int copy_type, const Ste
     }
 }
 
-template <class P, class G, bool EIGHT>
-__global__ __launch_bounds__(256) void adamw_kernel(StepArgs a)
+template <class P, class G, bool EIGHT, bool EXTRA>
+__global__ __launch_bounds__(256) void adamw_kernel(StepArgs<EXTRA> a)
 {
     int e = 0;
     for (int k = 1; k < a.count; ++k) e += (int)blockIdx.x >= a.first[k];
@@ -174,25 +184,31 @@ __global__ __launch_bounds__(256) void adamw_kernel(StepArgs a)
         root = (float)(1.0 / sqrt(-expm1(t * a.log_beta2)));
     }
     const float scale = a.grad_scale ? a.grad_scale[0] : 1.0f;
-    const Tensor t = a.t[e];
-    const bool vec = a.vec[e];
+    const int flags = a.flags[e];
+    const Tensor t = {a.p[e], a.g[e], a.m[e], a.v[e], EXTRA ? a.ms[e] : nullptr, EXTRA ? a.vs[e] : nullptr,
+                      EXTRA ? a.copy[e] : nullptr, a.n[e]};
     const int64_t blocks = (t.n + kBlock - 1) / kBlock;
-    const int64_t b0 = ((int64_t)((int)blockIdx.x - a.first[e]) * 4 + (threadIdx.x >> 6)) * kWaveSteps;
-    for (int k = 0; k < kWaveSteps; ++k) {
+    const int64_t b0 = ((int64_t)((int)blockIdx.x - a.first[e]) * 4 + (threadIdx.x >> 6)) * a.steps;
+    for (int k = 0; k < a.steps; ++k) {
         if (b0 + k >= blocks) return;
-        if (vec) update<P, G, EIGHT, true>(t, a.copy_type[e], a, b0 + k, step_size, root, scale);
-        else update<P, G, EIGHT, false>(t, a.copy_type[e], a, b0 + k, step_size, root, scale);
+        if (flags & 1) update<P, G, EIGHT, true>(t, flags >> 1, a, b0 + k, step_size, root, scale);
+        else update<P, G, EIGHT, false>(t, flags >> 1, a, b0 + k, step_size, root, scale);
     }
 }
 
 template <class P, class G>
-void launch_states(const StepArgs &a, bool eight, int64_t grid, hipStream_t s)
+void launch_states(const StepArgs<true> &a, bool eight, int64_t grid, hipStream_t s)
 {
-    if (eight) hipLaunchKernelGGL((adamw_kernel<P, G, true>), dim3((uint32_t)grid), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((adamw_kernel<P, G, false>), dim3((uint32_t)grid), dim3(256), 0, s, a);
+    if (eight) hipLaunchKernelGGL((adamw_kernel<P, G, true, true>), dim3((uint32_t)grid), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((adamw_kernel<P, G, false, true>), dim3((uint32_t)grid), dim3(256), 0, s, a);
 }
-template <class P>
-void launch_grads(const StepArgs &a, int gd, bool eight, int64_t grid, hipStream_t s)
+template <class P, class G>
+void launch_states(const StepArgs<false> &a, bool, int64_t grid, hipStream_t s)
+{
+    hipLaunchKernelGGL((adamw_kernel<P, G, false, false>), dim3((uint32_t)grid), dim3(256), 0, s, a);
+}
+template <class P, bool EXTRA>
+void launch_grads(const StepArgs<EXTRA> &a, int gd, bool eight, int64_t grid, hipStream_t s)
 {
     if (gd == RGNN_F32) launch_states<P, float>(a, eight, grid, s);
     else if (gd == RGNN_BF16) launch_states<P, __bf16>(a, eight, grid, s);
@@ -201,12 +217,46 @@ void launch_grads(const StepArgs &a, int gd, bool eight, int64_t grid, hipStream
 
 bool aligned(const void *p, size_t b) { return (uintptr_t)p % b == 0; }
 
-}  // namespace
-
-rgnn_status launch_adamw(const rgnn_adamw_tensor_t *t, int32_t count, const rgnn_adamw_t &h, int64_t step,
-                         const int64_t *step_dev, const float *grad_scale, hipStream_t s)
+// The tensors of list[begin, end), all of one type combination.
+template <bool EXTRA>
+void launch_some(StepArgs<EXTRA> &a, const rgnn_adamw_tensor_t *t, const std::vector<int32_t> &list, hipStream_t s)
 {
-    StepArgs a{};
+    int64_t blocks = 0;
+    for (int32_t i : list) blocks += (t[i].n + kBlock - 1) / kBlock;
+    // up to 16 blocks a workgroup, fewer where the chip would not be full
+    a.steps = (int32_t)std::min<int64_t>(4, std::max<int64_t>(1, blocks / 8192));
+    size_t k = 0;
+    while (k < list.size()) {
+        a.count = 0;
+        int64_t grid = 0;
+        for (; k < list.size() && a.count < StepArgs<EXTRA>::most; ++k) {
+            const rgnn_adamw_tensor_t &x = t[list[k]];
+            const int64_t groups = (x.n + kBlock * 4 * a.steps - 1) / (kBlock * 4 * a.steps);
+            if (grid + groups >= (int64_t(1) << 31) - 1 && a.count) break;
+            const int c = a.count++;
+            const bool eight = x.state_bits == 8;
+            a.p[c] = x.param; a.g[c] = x.grad; a.m[c] = x.m; a.v[c] = x.v; a.n[c] = x.n;
+            if constexpr (EXTRA) { a.ms[c] = x.m_scale; a.vs[c] = x.v_scale; a.copy[c] = x.copy; }
+            const bool vec = aligned(x.param, 4 * dtype_bytes(x.param_dtype)) && aligned(x.grad, 4 * dtype_bytes(x.grad_dtype)) &&
+                             aligned(x.m, eight ? 4 : 16) && aligned(x.v, eight ? 4 : 16) &&
+                             (!x.copy || aligned(x.copy, 4 * dtype_bytes(x.copy_dtype)));
+            a.flags[c] = (uint8_t)((vec ? 1 : 0) | (x.copy ? x.copy_dtype << 1 : 0));
+            a.first[c] = (int32_t)grid;
+            grid += groups;
+        }
+        a.first[a.count] = (int32_t)grid;
+        const rgnn_adamw_tensor_t &x = t[list[0]];
+        LaunchScope ls("adamw", s);
+        if (x.param_dtype == RGNN_F32) launch_grads<float>(a, x.grad_dtype, x.state_bits == 8, grid, s);
+        else if (x.param_dtype == RGNN_BF16) launch_grads<__bf16>(a, x.grad_dtype, x.state_bits == 8, grid, s);
+        else launch_grads<_Float16>(a, x.grad_dtype, x.state_bits == 8, grid, s);
+    }
+}
+
+template <class Args>
+Args step_args(const rgnn_adamw_t &h, int64_t step, const int64_t *step_dev, const float *grad_scale)
+{
+    Args a{};
     const double b1 = h.beta1, b2 = h.beta2;
     // 1 - beta from the double: from beta rounded to fp32 it would be off by 1e-5 at 0.999
     a.beta1 = (float)b1; a.beta2 = (float)b2;
@@ -219,41 +269,29 @@ rgnn_status launch_adamw(const rgnn_adamw_tensor_t *t, int32_t count, const rgnn
         a.step_size = (float)(h.lr / -std::expm1((double)step * a.log_beta1));
         a.root = (float)(1.0 / std::sqrt(-std::expm1((double)step * a.log_beta2)));
     }
-    // by type combination, in order of appearance
-    std::vector<uint8_t> done(count, 0);
+    return a;
+}
+
+}  // namespace
+
+rgnn_status launch_adamw(const rgnn_adamw_tensor_t *t, int32_t count, const rgnn_adamw_t &h, int64_t step,
+                         const int64_t *step_dev, const float *grad_scale, hipStream_t s)
+{
+    // by type combination: parameter, gradient, and states in 32 bits, with copies, in 8 bits
+    std::vector<int32_t> lists[27];
+    for (int32_t i = 0; i < count; ++i)
+        if (t[i].n > 0)
+            lists[t[i].param_dtype * 9 + t[i].grad_dtype * 3 + (t[i].state_bits == 8 ? 2 : t[i].copy ? 1 : 0)].push_back(i);
     bool launched = false;
-    for (int32_t i = 0; i < count; ++i) {
-        if (done[i] || t[i].n == 0) continue;
-        int32_t k = i;
-        while (k < count) {
-            a.count = 0;
-            int64_t grid = 0;
-            for (; k < count && a.count < kPerLaunch; ++k) {
-                const rgnn_adamw_tensor_t &x = t[k];
-                if (done[k] || x.n == 0 || x.param_dtype != t[i].param_dtype || x.grad_dtype != t[i].grad_dtype ||
-                    x.state_bits != t[i].state_bits)
-                    continue;
-                const int64_t groups = (x.n + kGroup - 1) / kGroup;
-                if (grid + groups >= (int64_t(1) << 31) - 1) break;
-                const int c = a.count++;
-                const bool eight = x.state_bits == 8;
-                a.t[c] = Tensor{x.param, x.grad, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n};
-                a.copy_type[c] = (uint8_t)x.copy_dtype;
-                a.vec[c] = aligned(x.param, 4 * dtype_bytes(x.param_dtype)) && aligned(x.grad, 4 * dtype_bytes(x.grad_dtype)) &&
-                           aligned(x.m, eight ? 4 : 16) && aligned(x.v, eight ? 4 : 16) &&
-                           (!x.copy || aligned(x.copy, 4 * dtype_bytes(x.copy_dtype)));
-                a.first[c] = (int32_t)grid;
-                grid += groups;
-                done[k] = 1;
-            }
-            if (a.count == 0) break;
-            a.first[a.count] = (int32_t)grid;
-            const bool eight = t[i].state_bits == 8;
-            launched = true;
-            LaunchScope ls("adamw", s);
-            if (t[i].param_dtype == RGNN_F32) launch_grads<float>(a, t[i].grad_dtype, eight, grid, s);
-            else if (t[i].param_dtype == RGNN_BF16) launch_grads<__bf16>(a, t[i].grad_dtype, eight, grid, s);
-            else launch_grads<_Float16>(a, t[i].grad_dtype, eight, grid, s);
+    for (int l = 0; l < 27; ++l) {
+        if (lists[l].empty()) continue;
+        launched = true;
+        if (l % 3) {
+            auto a = step_args<StepArgs<true>>(h, step, step_dev, grad_scale);
+            launch_some(a, t, lists[l], s);
+        } else {
+            auto a = step_args<StepArgs<false>>(h, step, step_dev, grad_scale);
+            launch_some(a, t, lists[l], s);
         }
     }
     if (!launched) return RGNN_OK;

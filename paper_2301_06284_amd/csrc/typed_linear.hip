@@ -141,31 +141,39 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
             bp[x] += binc;
         }
     };
-    // ANY: a step's loads into registers, and from there to LDS
-    i32x4 ra[ANY ? NA : 1], rb[ANY ? NB : 1];
-    auto fetch = [&](int step) {
+    // ANY: a step's loads into registers, and from there to LDS.  Several steps are under way (SETS).
+    constexpr int SETS = !ANY || STAGES == 1 ? 1 : NA + NB <= 6 ? 4 : 2;
+    struct Set { i32x4 a[ANY ? NA : 1], b[ANY ? NB : 1]; } set[SETS];
+    auto fetch = [&](Set &r, int step) {
         if constexpr (ANY) {
             const int left = kbytes - step * 128 - chunk * 16;   // bytes of k from this chunk on
 #pragma unroll
             for (int x = 0; x < NA; ++x) {
-                ra[x] = left > 0 && (aok >> x & 1) ? first_bytes(load_any<E>(ap[x], a.x_end), left) : i32x4{0, 0, 0, 0};
+                r.a[x] = left > 0 && (aok >> x & 1) ? load_any<E>(ap[x], a.x_end) : i32x4{0, 0, 0, 0};
                 ap[x] += (aok >> x & 1) << 7;
             }
 #pragma unroll
             for (int x = 0; x < NB; ++x) {
                 const bool in = TRANS ? left > 0 : step * KE + bk[x] < a.K;
-                rb[x] = in ? load_any<E>(bp[x], a.w_end) : i32x4{0, 0, 0, 0};
-                if (TRANS) rb[x] = first_bytes(rb[x], left);
+                r.b[x] = in ? load_any<E>(bp[x], a.w_end) : i32x4{0, 0, 0, 0};
                 bp[x] += binc;
             }
         }
     };
-    auto put = [&](char *sa, char *sb) {
+    auto put = [&](Set &r, char *sa, char *sb, int step) {
         if constexpr (ANY) {
+            if ((step + 1) * 128 > kbytes) {        // here, not at the load: nothing is to wait for it before
+                const int left = kbytes - step * 128 - chunk * 16;
 #pragma unroll
-            for (int x = 0; x < NA; ++x) *(i32x4 *)(sa + (x * NW + wave) * 1024 + lane * 16) = ra[x];
+                for (int x = 0; x < NA; ++x) r.a[x] = first_bytes(r.a[x], left);
+                if (TRANS)
 #pragma unroll
-            for (int x = 0; x < NB; ++x) *(i32x4 *)(sb + (x * NW + wave) * 1024 + lane * 16) = rb[x];
+                    for (int x = 0; x < NB; ++x) r.b[x] = first_bytes(r.b[x], left);
+            }
+#pragma unroll
+            for (int x = 0; x < NA; ++x) *(i32x4 *)(sa + (x * NW + wave) * 1024 + lane * 16) = r.a[x];
+#pragma unroll
+            for (int x = 0; x < NB; ++x) *(i32x4 *)(sb + (x * NW + wave) * 1024 + lane * 16) = r.b[x];
         }
     };
 
@@ -274,8 +282,8 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
     int step = 0;
     if constexpr (STAGES == 1) {
         if constexpr (ANY) {
-            fetch(0);
-            put(sa0, sb0);
+            fetch(set[0], 0);
+            put(set[0], sa0, sb0, 0);
         } else {
             load(sa0, sb0, 0);
         }
@@ -314,22 +322,20 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_linear_kernel(TileArgs a
         step_barrier<0>();
         multiply(sa3, sb3);
     } else if constexpr (ANY) {
-        fetch(0);
-        put(sa0, sb0);
-        if (steps > 1) fetch(1);
-        for (; step + 2 <= steps; step += 2) {
-            __syncthreads();
-            multiply(sa0, sb0);
-            put(sa1, sb1);
-            if (step + 2 < steps) fetch(step + 2);
-            __syncthreads();
-            multiply(sa1, sb1);
-            if (step + 2 < steps) put(sa0, sb0);
-            if (step + 3 < steps) fetch(step + 3);
-        }
-        if (step < steps) {
-            __syncthreads();
-            multiply(sa0, sb0);
+        // whole rounds of SETS steps; those behind K are zeros
+#pragma unroll
+        for (int u = 0; u < SETS; ++u) fetch(set[u], u);
+        put(set[0], sa0, sb0, 0);
+        fetch(set[0], SETS);
+        for (; step < steps; step += SETS) {
+#pragma unroll
+            for (int u = 0; u < SETS; ++u) {
+                __syncthreads();
+                multiply(u & 1 ? sa1 : sa0, u & 1 ? sb1 : sb0);
+                Set &next = set[(u + 1) % SETS];
+                put(next, u & 1 ? sa0 : sa1, u & 1 ? sb0 : sb1, step + u + 1);
+                fetch(next, step + u + 1 + SETS);
+            }
         }
     } else {
         load(sa0, sb0, 0);
@@ -566,9 +572,9 @@ struct TileCost {
 };
 constexpr TileCost kCostWide = {256, 256, 256, 7.0, 12.5, 12.5};
 constexpr TileCost kCost128 = {128, 128, 512, 3.0, 6.0, 8.5};
-constexpr TileCost kCost64 = {64, 128, 768, 2.5, 4.65, 7.7};
-constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 5.15, 7.2};
-constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 2.9};
+constexpr TileCost kCost64 = {64, 128, 768, 2.5, 3.6, 7.7};
+constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 3.7, 7.2};
+constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 3.0};
 constexpr TileCost kCostDeep128 = {64, 128, 256, 2.0, 2.9, 3.1};
 
 double tile_cost(const TileArgs &k, const TileCost &c, int el)
