@@ -4,7 +4,8 @@
 // kernel's arguments, so nothing is uploaded and a captured graph holds them.  A workgroup takes up to 4096
 // consecutive elements of one tensor, a wave 256 of them at a time (4 a lane), which is one block
 // of 8-bit states: its maximum is a reduction over one wave.
-// Bound by memory.
+// Bound by memory.  Every product and sum is rounded on its own (no fused multiply-add), so that a
+// state's code is the one that the same formula gives in any fp32 arithmetic.
 #include <algorithm>
 #include <cmath>
 #include <vector>
@@ -85,6 +86,7 @@ template <class P, class G, bool EIGHT, bool VEC, class Args>
 __device__ __forceinline__ void update(const Tensor &t, int copy_type, const Args &a, int64_t block, float step_size,
                                        float root, float scale)
 {
+#pragma clang fp contract(off)
     const int lane = threadIdx.x & 63;
     const int64_t at = block * kBlock + lane * 4;
     P p[4];
@@ -144,21 +146,39 @@ __device__ __forceinline__ void update(const Tensor &t, int copy_type, const Arg
         }
         tm = wave_max(tm);
         tv = wave_max(tv);
-        // 127^2 / top and 255^4 / top, the top scaled into [1/2, 1) so that neither overflows; the
-        // values are scaled alike, by powers of two.  One quotient a block, and the roots within a
-        // unit in the last place: a code is off by 1e-4 of a step at most, where exact quotients and
-        // roots take three times the operations and leave memory waiting (201M values 778 us).
+        // First with one quotient a block and with roots within a unit in the last place: 127^2 / top
+        // and 255^4 / top, the top scaled into [1/2, 1) and the values alike, so that neither
+        // overflows.  With u = 2^-24 that is within 255 * 3.75 u of the root of the quotient, and the
+        // formula in fp32 within 255 * 2.75 u: where no value is within 2e-4 of the middle
+        // between two codes, the codes are the formula's.  Else (one block in six) the formula
+        // itself, whose quotients and roots take three times the operations and leave memory
+        // waiting (201M values: 778 us alone).
         const int em = __builtin_amdgcn_frexp_expf(tm), ev = __builtin_amdgcn_frexp_expf(tv);
         const float rm = tm > 0.0f ? 16129.0f / __builtin_amdgcn_ldexpf(tm, -em) : 0.0f;
         const float rv = tv > 0.0f ? 4228250625.0f / __builtin_amdgcn_ldexpf(tv, -ev) : 0.0f;
+        float qm[4], qv[4];
+        bool middle = false;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = __builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(fabsf(m[i]), -em) * rm);
+            const float y = __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(v[i], -ev) * rv));
+            qm[i] = rintf(x);
+            qv[i] = rintf(y);
+            middle = middle || fabsf(x - qm[i]) > 0.4998f || fabsf(y - qv[i]) > 0.4998f;
+        }
+        if (__ballot(middle)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                qm[i] = tm > 0.0f ? rintf(127.0f * sqrtf(fabsf(m[i]) / tm)) : 0.0f;
+                qv[i] = tv > 0.0f ? rintf(255.0f * sqrtf(sqrtf(v[i] / tv))) : 0.0f;
+            }
+        }
         int8_t cm[4];
         uint8_t cv[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float q = rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(fabsf(m[i]), -em) * rm));
-            cm[i] = (int8_t)(int)copysignf(q, m[i]);
-            const float r = rintf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(__builtin_amdgcn_ldexpf(v[i], -ev) * rv)));
-            cv[i] = (uint8_t)(int)fmaxf(r, v[i] > 0.0f ? 1.0f : 0.0f);
+            cm[i] = (int8_t)(int)copysignf(qm[i], m[i]);
+            cv[i] = (uint8_t)(int)fmaxf(qv[i], v[i] > 0.0f ? 1.0f : 0.0f);
         }
         store4<int8_t, VEC>(t.m, at, t.n, cm);
         store4<uint8_t, VEC>(t.v, at, t.n, cv);
