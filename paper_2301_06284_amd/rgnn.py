@@ -345,56 +345,78 @@ def _need(ok, why: str):
         raise ValueError(why)
 
 
-def _same_device(first, *others):
+def _same_device(first, *others) -> int:
+    """The device of the tensors, which is the current one."""
     import torch
-    _need(first.is_cuda, "tensors must be on a GPU")
-    _need(first.get_device() == torch.cuda.current_device(),
-          f"tensors are on device {first.get_device()}, the current one is {torch.cuda.current_device()}")
+    d = first.get_device()
+    if d < 0:
+        raise ValueError("tensors must be on a GPU")
+    if d != torch.cuda.current_device():
+        raise ValueError(f"tensors are on device {d}, the current one is {torch.cuda.current_device()}")
     for t in others:
-        _need(t is None or t.device == first.device, "tensors must be on one device")
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors must be on one device")
+    return d
+
+
+def _stream_on(stream, device: int):
+    """The stream's handle; None: the device's current stream, without making an object of it."""
+    if stream is not None:
+        return _stream(stream)
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else _stream(None)
 
 
 def _matrix(t, name: str, cols: int):
     """(pointer, rows, leading dimension) of a matrix with `cols` columns."""
-    _need(t.dim() == 2 and t.shape[1] == cols, f"{name} must have {cols} columns")
+    if t.dim() != 2 or t.shape[1] != cols:
+        raise ValueError(f"{name} must have {cols} columns")
     rows, ld = t.shape[0], t.stride(0)
     if rows <= 1:
         ld = max(ld, cols)
-    _need((cols <= 1 or t.stride(1) == 1) and ld >= cols, f"{name}'s columns must lie side by side, its rows apart")
+    if ld < cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}'s columns must lie side by side, its rows apart")
     return t.data_ptr(), rows, ld
 
 
-def _indices(type_ptr, types: int, *index):
-    """Checks the offsets and index arrays; the number of positions, or None."""
+def _index(t):
+    """Pointer of an index array, None for none."""
+    if t is None:
+        return None
     import torch
-    _need(type_ptr.dtype == torch.int64 and type_ptr.dim() == 1 and type_ptr.is_contiguous() and
-          type_ptr.shape[0] == types + 1, "type_ptr must be int64 [types + 1]")
-    M = None
-    for i in index:
-        if i is None:
-            continue
-        _need(i.dtype == torch.int32 and i.dim() == 1 and i.is_contiguous(), "gather and scatter must be int32 [M]")
-        _need(M is None or i.shape[0] == M, "gather and scatter must have one length")
-        M = i.shape[0]
-    return M
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError("gather and scatter must be contiguous int32 [M]")
+    return t.data_ptr()
+
+
+def _positions(type_ptr, types: int, first, second, rows: int) -> int:
+    """Checks the offsets and the index arrays' lengths; the number of positions."""
+    import torch
+    if type_ptr.dtype != torch.int64 or type_ptr.dim() != 1 or type_ptr.shape[0] != types + 1 or \
+            not type_ptr.is_contiguous():
+        raise ValueError("type_ptr must be contiguous int64 [types + 1]")
+    if first is not None and second is not None and first.shape[0] != second.shape[0]:
+        raise ValueError("gather and scatter must have one length")
+    return first.shape[0] if first is not None else second.shape[0] if second is not None else rows
 
 
 def typed_linear(X, type_ptr, W, Y, gather=None, scatter=None, trans_w=False, stream=None):
     """Y[scatter[i]] = X[gather[i]] W[t(i)] over the positions of device offsets
     type_ptr [types + 1] (trans_w: W [types, N, K] used transposed).  X, W, Y fp32, bf16
     or fp16; Y of that type or fp32."""
-    _same_device(X, type_ptr, W, Y, gather, scatter)
-    _need(W.dim() == 3 and W.is_contiguous() and W.dtype == X.dtype, "W must be contiguous [types, ., .] of X's type")
+    d = _same_device(X, type_ptr, W, Y, gather, scatter)
+    if W.dim() != 3 or not W.is_contiguous() or W.dtype != X.dtype:
+        raise ValueError("W must be contiguous [types, ., .] of X's type")
     T, K, N = W.shape
     if trans_w:
         K, N = N, K
     xp, xr, ldx = _matrix(X, "X", K)
     yp, yr, ldy = _matrix(Y, "Y", N)
-    M = _indices(type_ptr, T, gather, scatter)
-    if M is None:
-        M = xr
-    _check(_lib.rgnn_typed_linear(_dtype(X), xp, xr, ldx, _ptr(gather), type_ptr.data_ptr(), T, M, W.data_ptr(), K, N,
-                                  1 if trans_w else 0, _dtype(Y), yp, yr, ldy, _ptr(scatter), _stream(stream)))
+    gp, sp = _index(gather), _index(scatter)
+    M = _positions(type_ptr, T, gather, scatter, xr)
+    _check(_lib.rgnn_typed_linear(_dtype(X), xp, xr, ldx, gp, type_ptr.data_ptr(), T, M, W.data_ptr(), K, N,
+                                  1 if trans_w else 0, _dtype(Y), yp, yr, ldy, sp, _stream_on(stream, d)))
 
 
 def typed_linear_wgrad_workspace_size(dtype, M: int, num_types: int, K: int, N: int) -> int:
@@ -408,18 +430,19 @@ def typed_linear_wgrad_workspace_size(dtype, M: int, num_types: int, K: int, N: 
 
 def typed_linear_wgrad(X, dY, type_ptr, dW, ws, gather=None, dy_gather=None, stream=None):
     """dW[t] = sum over the positions i of type t of X[gather[i]]^T dY[dy_gather[i]]."""
-    _same_device(X, dY, type_ptr, dW, ws, gather, dy_gather)
-    _need(dY.dtype == X.dtype, "dY must be of X's type")
-    _need(dW.dim() == 3 and dW.is_contiguous(), "dW must be contiguous [types, K, N]")
+    d = _same_device(X, dY, type_ptr, dW, ws, gather, dy_gather)
+    if dY.dtype != X.dtype:
+        raise ValueError("dY must be of X's type")
+    if dW.dim() != 3 or not dW.is_contiguous():
+        raise ValueError("dW must be contiguous [types, K, N]")
     T, K, N = dW.shape
     xp, xr, ldx = _matrix(X, "X", K)
     dp, dr, ldd = _matrix(dY, "dY", N)
-    M = _indices(type_ptr, T, gather, dy_gather)
-    if M is None:
-        M = xr
-    _check(_lib.rgnn_typed_linear_wgrad(_dtype(X), xp, xr, ldx, _ptr(gather), dp, dr, ldd, _ptr(dy_gather),
-                                        type_ptr.data_ptr(), T, M, K, N, _dtype(dW), dW.data_ptr(), _ptr(ws),
-                                        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)))
+    gp, sp = _index(gather), _index(dy_gather)
+    M = _positions(type_ptr, T, gather, dy_gather, xr)
+    _check(_lib.rgnn_typed_linear_wgrad(_dtype(X), xp, xr, ldx, gp, dp, dr, ldd, sp, type_ptr.data_ptr(), T, M, K, N,
+                                        _dtype(dW), dW.data_ptr(), _ptr(ws),
+                                        0 if ws is None else ws.numel() * ws.element_size(), _stream_on(stream, d)))
 
 
 def fp8_widths(K: int):
@@ -441,51 +464,55 @@ def _fp8_out(codes, scales, lead, blocks, K, device):
 def _fp8_check(codes, scales, lead, blocks, K):
     import torch
     Kp, Ks = fp8_widths(K)
-    _need(codes.dtype == torch.float8_e4m3fn and tuple(codes.shape) == (*lead, Kp) and codes.is_contiguous(),
-          f"codes must be contiguous float8_e4m3fn {(*lead, Kp)}")
-    _need(scales.dtype == torch.uint8 and tuple(scales.shape) == (*blocks, Ks) and scales.is_contiguous(),
-          f"scales must be contiguous uint8 {(*blocks, Ks)}")
+    if codes.dtype != torch.float8_e4m3fn or codes.shape != (*lead, Kp) or not codes.is_contiguous():
+        raise ValueError(f"codes must be contiguous float8_e4m3fn {(*lead, Kp)}")
+    if scales.dtype != torch.uint8 or scales.shape != (*blocks, Ks) or not scales.is_contiguous():
+        raise ValueError(f"scales must be contiguous uint8 {(*blocks, Ks)}")
 
 
 def fp8_quantize_rows(X, codes=None, scales=None, stream=None):
     """X [rows, K] -> (codes float8_e4m3fn [rows, Kp], scales uint8 [rows, Ks]), a
     power-of-two scale for each 128 columns of a row."""
-    _need(X.dim() == 2, "X must be a matrix")
-    xp, rows, ldx = _matrix(X, "X", X.shape[1])
-    codes, scales = _fp8_out(codes, scales, (rows,), (rows,), X.shape[1], X.device)
-    _same_device(X, codes, scales)
-    _check(_lib.rgnn_fp8_quantize_rows(_dtype(X), xp, rows, ldx, X.shape[1], codes.data_ptr(), scales.data_ptr(),
-                                       _stream(stream)))
+    if X.dim() != 2:
+        raise ValueError("X must be a matrix")
+    K = X.shape[1]
+    xp, rows, ldx = _matrix(X, "X", K)
+    codes, scales = _fp8_out(codes, scales, (rows,), (rows,), K, X.device)
+    d = _same_device(X, codes, scales)
+    _check(_lib.rgnn_fp8_quantize_rows(_dtype(X), xp, rows, ldx, K, codes.data_ptr(), scales.data_ptr(),
+                                       _stream_on(stream, d)))
     return codes, scales
 
 
 def fp8_quantize_weights(W, codes=None, scales=None, stream=None):
     """W [types, K, N] -> (codes float8_e4m3fn [types, N, Kp], scales uint8
     [types, ceil(N / 128), Ks]), a power-of-two scale for each 128 x 128 block."""
-    _need(W.dim() == 3 and W.is_contiguous(), "W must be contiguous [types, K, N]")
+    if W.dim() != 3 or not W.is_contiguous():
+        raise ValueError("W must be contiguous [types, K, N]")
     T, K, N = W.shape
     codes, scales = _fp8_out(codes, scales, (T, N), (T, -(-N // 128)), K, W.device)
-    _same_device(W, codes, scales)
+    d = _same_device(W, codes, scales)
     _check(_lib.rgnn_fp8_quantize_weights(_dtype(W), W.data_ptr(), T, K, N, codes.data_ptr(), scales.data_ptr(),
-                                          _stream(stream)))
+                                          _stream_on(stream, d)))
     return codes, scales
 
 
 def typed_linear_fp8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatter=None, stream=None):
     """typed_linear on the codes and scales of fp8_quantize_rows and
     fp8_quantize_weights; Y fp32, bf16 or fp16."""
-    _same_device(X, x_scales, type_ptr, W, w_scales, Y, gather, scatter)
-    _need(W.dim() == 3 and X.dim() == 2, "X must be [rows, Kp], W [types, N, Kp]")
+    d = _same_device(X, x_scales, type_ptr, W, w_scales, Y, gather, scatter)
+    if W.dim() != 3 or X.dim() != 2:
+        raise ValueError("X must be [rows, Kp], W [types, N, Kp]")
     T, N, K = W.shape
-    _fp8_check(X, x_scales, (X.shape[0],), (X.shape[0],), K)
+    rows = X.shape[0]
+    _fp8_check(X, x_scales, (rows,), (rows,), K)
     _fp8_check(W, w_scales, (T, N), (T, -(-N // 128)), K)
     yp, yr, ldy = _matrix(Y, "Y", N)
-    M = _indices(type_ptr, T, gather, scatter)
-    if M is None:
-        M = X.shape[0]
-    _check(_lib.rgnn_typed_linear_fp8(X.data_ptr(), x_scales.data_ptr(), X.shape[0], _ptr(gather), type_ptr.data_ptr(),
-                                      T, M, W.data_ptr(), w_scales.data_ptr(), K, N, _dtype(Y), yp, yr, ldy,
-                                      _ptr(scatter), _stream(stream)))
+    gp, sp = _index(gather), _index(scatter)
+    M = _positions(type_ptr, T, gather, scatter, rows)
+    _check(_lib.rgnn_typed_linear_fp8(X.data_ptr(), x_scales.data_ptr(), rows, gp, type_ptr.data_ptr(), T, M,
+                                      W.data_ptr(), w_scales.data_ptr(), K, N, _dtype(Y), yp, yr, ldy, sp,
+                                      _stream_on(stream, d)))
 
 
 class AdamwTensors:
@@ -503,12 +530,12 @@ class AdamwTensors:
         self._kept = [list(x) for x in lists]
         self._array = (AdamwTensor * max(n, 1))()
         self._n = n
-        self.device = params[0].device if n else None
+        self.device = params[0].get_device() if n else None
         for k, (p, g, a, b, sa, sb, c) in enumerate(zip(*lists)):
             size, eight = p.numel(), a.dtype == torch.int8
-            _need(all(t is None or (t.is_contiguous() and t.device == self.device) for t in (p, g, a, b, sa, sb, c)),
+            _need(p.get_device() >= 0, "tensors must be on a GPU")
+            _need(all(t is None or (t.is_contiguous() and t.get_device() == self.device) for t in (p, g, a, b, sa, sb, c)),
                   f"tensor {k}: tensors must be contiguous and on one device")
-            _need(p.is_cuda, "tensors must be on a GPU")
             _need(all(t is None or t.numel() == size for t in (g, a, b, c)), f"tensor {k}: lengths differ")
             if eight:
                 blocks = -(-size // 256)
@@ -530,20 +557,23 @@ def adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8
     """One AdamW step.  step: the step's number from 1, or a device int64 [1] that
     holds it; grad_scale: None or a device fp32 [1]."""
     import torch
-    if tensors.device is not None:
-        _need(tensors.device.index == torch.cuda.current_device(), "tensors are not on the current device")
+    d = tensors.device
+    if d is None:
+        return
+    if d != torch.cuda.current_device():
+        raise ValueError(f"tensors are on device {d}, the current one is {torch.cuda.current_device()}")
     step_dev = None
     if isinstance(step, torch.Tensor):
-        _need(step.dtype == torch.int64 and step.numel() == 1 and step.device == tensors.device,
-              "step must be a number or a device int64 [1]")
+        if step.dtype != torch.int64 or step.numel() != 1 or step.get_device() != d:
+            raise ValueError("step must be a number or a device int64 [1]")
         step, step_dev = 0, step.data_ptr()
     if grad_scale is not None:
-        _need(grad_scale.dtype == torch.float32 and grad_scale.numel() == 1 and grad_scale.device == tensors.device,
-              "grad_scale must be a device fp32 [1]")
+        if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.get_device() != d:
+            raise ValueError("grad_scale must be a device fp32 [1]")
         grad_scale = grad_scale.data_ptr()
     hyper = AdamwHyper(lr, beta1, beta2, eps, weight_decay)
     _check(_lib.rgnn_adamw_step(tensors._array, tensors._n, ctypes.byref(hyper), step, step_dev, grad_scale,
-                                _stream(stream)))
+                                _stream_on(stream, d)))
 
 
 def profile_enable(on: bool):
