@@ -354,11 +354,13 @@ rgnn_status rgnn_segment_gemm_workspace_size(int64_t M, int32_t num_types, size_
  *   - type_ptr: DEVICE int64 [num_types + 1], ascending; type t owns the positions
  *     [type_ptr[t], type_ptr[t+1]).  M is how many positions the index arrays and the
  *     rows hold, a capacity: positions outside [type_ptr[0], type_ptr[num_types]) belong
- *     to no type, and nothing of theirs is read or written.  Offsets are kept inside [0, M]
- *     by the kernels; offsets that descend give wrong rows, and no access out of range.
+ *     to no type, and nothing of theirs is read or written.  The kernels keep offsets
+ *     inside [0, M], and one below an earlier one counts as that: no rows of two types,
+ *     no access out of range.
  *   - gather / scatter: DEVICE int32 [M] or NULL for the identity (then the matrix
- *     needs M rows).  A gathered index outside the matrix's rows (-1, say) reads a row of
- *     zeros, a scattered one writes nothing.  Gathered rows may repeat; scattered
+ *     needs M rows).  A gathered index outside the matrix's rows (-1, say) is
+ *     a row of zeros: zero outputs, and nothing in the weight gradient, whatever the
+ *     other operand holds.  A scattered one writes nothing.  Gathered rows may repeat; scattered
  *     rows that repeat race.
  *   - ldx, ldy, lddy: elements from one row to the next.  Weights are dense.
  *   - Types of the elements (rgnn_dtype): X, W and dY alike RGNN_F32, RGNN_BF16 or

@@ -50,11 +50,11 @@ struct WgradArgs {
     void *ws = nullptr;
 };
 
-// How the weight gradient's contraction is cut: pieces of `chunk` rows of a type, and how many
-// pieces the types with more rows than one have, at most (their sums go through the workspace).
+// How the weight gradient's contraction is cut: types with more rows than `whole` into pieces of
+// `chunk` rows, and how many pieces those can be (their sums go through the workspace).
 struct WgradPlan {
     int bk = 0, bn = 0;          // the tile
-    int64_t chunk = 0, slots = 0;
+    int64_t whole = 0, chunk = 0, slots = 0;
 };
 WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
@@ -118,17 +118,9 @@ __device__ __forceinline__ f32x4 mma16<F32>(i32x4 a, i32x4 b, f32x4 c)
 
 // ---------------------------------------------------------------- tiles
 
-// Rows [begin, end) of type t, with offsets that the host has not seen kept inside
-// [0, M): a table that is not monotone gives wrong rows, and no access out of range.
-__device__ __forceinline__ void type_rows(int64_t p, int64_t q, int64_t M, int64_t &begin, int64_t &end)
-{
-    begin = p < 0 ? 0 : p > M ? M : p;
-    end = q < begin ? begin : q > M ? M : q;
-}
-
 struct Piece {          // a workgroup's share: number `index` of type `type`'s pieces
     int type;
-    int64_t begin, end;   // the type's rows
+    int64_t begin, end;   // the type's rows, inside [0, M)
     int index;            // which of the type's pieces
     int before;           // what `weight` counted in the types before it
 };
@@ -145,34 +137,56 @@ __device__ __forceinline__ int wave_prefix_sum(int x)
     return x;
 }
 
+// The same for the largest; x >= 0.
+__device__ __forceinline__ int wave_prefix_max(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));
+    return max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
+}
+
 struct NoWeight {
     __device__ __forceinline__ int operator()(int64_t) const { return 0; }
 };
 
 // The type that owns piece number `want`, where a type with c rows makes count(c) pieces (fewer
 // than 2^31 over all types: the host checks the grid).  Every wave of a workgroup searches
-// alike, 256 types a turn: one load of the offsets and a prefix sum over the lanes, no LDS and no
+// alike, 256 types a turn: one load of the offsets and prefix sums over the lanes, no LDS and no
 // barrier.  weight(c) is a second count summed over the types before the owner.  False where
 // there are fewer pieces.
+//
+// The host has not seen the offsets: they are kept inside [0, M), and one below an earlier one
+// counts as that (a running maximum), so that the types' rows never overlap and the counts
+// over all types stay within what the host sized grid and workspace for.
 template <class Count, class Weight>
 __device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int T, int64_t M, int want,
                                            Count count, Weight weight, Piece &out)
 {
     constexpr bool WEIGHT = !std::is_same<Weight, NoWeight>::value;
-    const int lane = threadIdx.x & 63;
-    int before = 0, wbefore = 0;
+    const int lane = threadIdx.x & 63, most = (int)M;
+    int before = 0, wbefore = 0, top = 0;
     for (int t0 = 0; t0 < T; t0 += 256) {
-        int64_t b[4], e[4];
-        int c[4], w[4], cs = 0, ws = 0;
-        int64_t at[5];       // loads that depend on nothing, all at once
+        int at[5], c[4], w[4], cs = 0, ws = 0;
+        int64_t raw[5];      // loads that depend on nothing, all at once
 #pragma unroll
-        for (int i = 0; i < 5; ++i) at[i] = ptr[min(t0 + lane * 4 + i, T)];
+        for (int i = 0; i < 5; ++i) raw[i] = ptr[min(t0 + lane * 4 + i, T)];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) at[i] = raw[i] < 0 ? 0 : raw[i] > M ? most : (int)raw[i];
+        at[0] = max(at[0], top);
+#pragma unroll
+        for (int i = 1; i < 5; ++i) at[i] = max(at[i], at[i - 1]);
+        const int upto = wave_prefix_max(at[4]);
+        const int earlier = __builtin_amdgcn_update_dpp(0, upto, 0x138, 0xF, 0xF, false);   // wave_shr:1
+#pragma unroll
+        for (int i = 0; i < 5; ++i) at[i] = max(at[i], earlier);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool own = t0 + lane * 4 + i < T;
-            type_rows(at[i], at[i + 1], M, b[i], e[i]);
-            c[i] = own ? (int)count(e[i] - b[i]) : 0;
-            w[i] = own ? (int)weight(e[i] - b[i]) : 0;
+            c[i] = own ? (int)count(at[i + 1] - at[i]) : 0;
+            w[i] = own ? (int)weight(at[i + 1] - at[i]) : 0;
             cs += c[i];
             ws += w[i];
         }
@@ -186,21 +200,18 @@ __device__ __forceinline__ bool find_piece(const int64_t *__restrict__ ptr, int 
 #pragma unroll
             for (int i = 0; i < 3; ++i)
                 if (k == i && pat + c[i] <= want) { pat += c[i]; wat += w[i]; k = i + 1; }
-            const int64_t bb = k == 0 ? b[0] : k == 1 ? b[1] : k == 2 ? b[2] : b[3];
-            const int64_t ee = k == 0 ? e[0] : k == 1 ? e[1] : k == 2 ? e[2] : e[3];
-            auto lane64 = [&](int64_t x) {
-                const uint32_t lo = __builtin_amdgcn_readlane((int)x, owner), hi = __builtin_amdgcn_readlane((int)(x >> 32), owner);
-                return (int64_t)(((uint64_t)hi << 32) | lo);
-            };
+            const int bb = k == 0 ? at[0] : k == 1 ? at[1] : k == 2 ? at[2] : at[3];
+            const int ee = k == 0 ? at[1] : k == 1 ? at[2] : k == 2 ? at[3] : at[4];
             out.type = t0 + owner * 4 + __builtin_amdgcn_readlane(k, owner);
-            out.begin = lane64(bb);
-            out.end = lane64(ee);
+            out.begin = __builtin_amdgcn_readlane(bb, owner);
+            out.end = __builtin_amdgcn_readlane(ee, owner);
             out.index = want - __builtin_amdgcn_readlane(pat, owner);
             out.before = WEIGHT ? __builtin_amdgcn_readlane(wat, owner) : 0;
             return true;
         }
         before += total;
         if (WEIGHT) wbefore += __builtin_amdgcn_readlane(wi, 63);
+        top = __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }

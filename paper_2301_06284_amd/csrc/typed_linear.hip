@@ -561,54 +561,80 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
     return RGNN_OK;
 }
 
-// Which tile: each is priced by what it measured (us; 16 to 16384 rows, k of 512 to 4096, one to 32
-// types) and the cheapest is taken.  `slots` workgroups fit the chip; a round of them costs `each` and, for
-// each KB of k of a row, `full`, down to `light` where few of the slots are taken.  The deep ones, with
-// four stages, are for few tiles: 16 rows, 4096 x 4096 22 us (64 x 128 with two stages 47), 1024 rows 57
-// (46).  fp32 is bound by its matrix cores, which take 7 us for 64 x 128 outputs and a KB of k.
+// Which tile of 16 and 8 bits: each is priced by what it measured (us; 1 to 16384 rows, k of 512 to
+// 4096, one to 32 types) and the cheapest is taken.  `slots` workgroups fit the chip; a round of them
+// costs `each` and, for each KB of k of a row, `full`, down to `light` where few of the slots are taken.
+// The deep ones, with four stages, are for few tiles (64 rows, 4096 x 4096, bf16: 32 x 64 17 us, 64 x 64
+// 20, 128 x 64 with two stages 36; 1024 rows 76, 58 and 47).  Rows on any address wait for registers at
+// each step: theirs are priced apart (292 rows, 1561 -> 333: 32 x 64 16 us, 128 x 64 28, 128 x 128 36; 8192
+// rows, 2047 -> 1535: 200, 138 and 105).
 struct TileCost {
     int bm, bn, slots;
     double each, light, full;
 };
 constexpr TileCost kCostWide = {256, 256, 256, 7.0, 12.5, 12.5};
 constexpr TileCost kCost128 = {128, 128, 512, 3.0, 6.0, 8.5};
-constexpr TileCost kCost64 = {64, 128, 768, 2.5, 3.6, 7.7};
 constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 3.7, 7.2};
 constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 3.0};
-constexpr TileCost kCostDeep128 = {64, 128, 256, 2.0, 2.9, 3.1};
+constexpr TileCost kCostDeepSmall = {32, 64, 768, 2.0, 1.6, 3.3};
+constexpr TileCost kAnyCost128 = {128, 128, 512, 3.0, 11.0, 14.0};
+constexpr TileCost kAnyCostNarrow = {128, 64, 768, 2.5, 8.5, 10.0};
+constexpr TileCost kAnyCostSmall = {32, 64, 768, 2.5, 4.6, 6.0};
+
+// Tiles that the rows make: every type that has some leaves half a tile, and has one at least.
+double tiles_of(const TileArgs &k, int bm, int bn)
+{
+    const double types = (double)std::min<int64_t>(k.M, k.T);
+    const double rows = types == 1 ? std::ceil((double)k.M / bm) : std::max((double)k.M / bm + types / 2, types);
+    return rows * ((k.N + bn - 1) / bn);
+}
 
 double tile_cost(const TileArgs &k, const TileCost &c, int el)
 {
-    // every type that has rows leaves half a tile, and has one at least
-    const double types = (double)std::min<int64_t>(k.M, k.T);
-    const double rows = types == 1 ? std::ceil((double)k.M / c.bm) : std::max((double)k.M / c.bm + types / 2, types);
-    const double tiles = rows * ((k.N + c.bn - 1) / c.bn);
-    const double kb = (double)k.K * el / 1024, f32 = c.bm * c.bn / (64.0 * 128) * 7;
-    const double light = el == 4 ? f32 : c.light, full = el == 4 ? f32 * c.slots / 256 : c.full;
+    const double tiles = tiles_of(k, c.bm, c.bn), kb = (double)k.K * el / 1024;
     const double rounds = std::floor(tiles / c.slots), rest = tiles / c.slots - rounds;
-    return rounds * (c.each + full * kb) + (rest > 0 ? c.each + (light + (full - light) * rest) * kb : 0);
+    return rounds * (c.each + c.full * kb) + (rest > 0 ? c.each + (c.light + (c.full - c.light) * rest) * kb : 0);
+}
+
+// fp32 is bound by its matrix cores, which take as long for a tile of few rows as for a full one: 64 x 64
+// where those give every CU two, 32 x 64 below (33 rows of 7 types, 2624 -> 128: 38 us, 64 x 64 59,
+// 128 x 128 182; 600 000 rows 128 -> 128: 294, 253).  Four stages from 16 steps of k on (1816 -> 1192:
+// 26-29 us, with two 30; 5 steps 13, with two 11).
+template <bool TRANS, bool ANY>
+rgnn_status launch_shape_f32(const TileArgs &k, hipStream_t s)
+{
+    if (tiles_of(k, 64, 64) >= 512) return launch_tile<F32, 64, 64, 2, 2, TRANS, ANY>(k, s);
+    if constexpr (!ANY)
+        if (k.K >= 512) return launch_tile<F32, 32, 64, 2, 2, TRANS, false, true>(k, s);
+    return launch_tile<F32, 32, 64, 2, 2, TRANS, ANY>(k, s);
 }
 
 template <class T, bool TRANS, bool ANY>
 rgnn_status launch_shape(const TileArgs &k, hipStream_t s)
 {
     constexpr int el = sizeof(typename T::elem);
-    const double narrow = tile_cost(k, kCostNarrow, el), c64 = tile_cost(k, kCost64, el), c128 = tile_cost(k, kCost128, el);
-    const double best = std::min(narrow, std::min(c64, c128));
-    if constexpr (!ANY && el != 4) {
+    if constexpr (el == 4) {
+        return launch_shape_f32<TRANS, ANY>(k, s);
+    } else if constexpr (ANY) {
+        const double small = tile_cost(k, kAnyCostSmall, el), narrow = tile_cost(k, kAnyCostNarrow, el), c128 = tile_cost(k, kAnyCost128, el);
+        if (small < std::min(narrow, c128)) return launch_tile<T, 32, 64, 2, 2, TRANS, true>(k, s);
+        if (narrow <= c128) return launch_tile<T, 128, 64, 4, 1, TRANS, true>(k, s);
+        return launch_tile<T, 128, 128, 2, 2, TRANS, true>(k, s);
+    } else {
+        const double narrow = tile_cost(k, kCostNarrow, el), c128 = tile_cost(k, kCost128, el), wide = tile_cost(k, kCostWide, el);
+        const double best = std::min(narrow, c128);
         // the wide tile's offsets have 32 bits
         const bool near = k.x_rows > 0 && (k.gather ? k.x_rows : (int64_t)kWide) * k.ldx < (int64_t(1) << 32) &&
                           kWide * k.w_row < (int64_t(1) << 32);
-        const double wide = tile_cost(k, kCostWide, el), deep = tile_cost(k, kCostDeep, el), deep128 = tile_cost(k, kCostDeep128, el);
-        if (near && wide < std::min(best, std::min(deep, deep128))) return launch_wide<T, TRANS>(k, s);
         if (k.K * el > 128) {      // more than one step
-            if (deep < std::min(best, deep128)) return launch_tile<T, 64, 64, 2, 2, TRANS, ANY, true>(k, s);
-            if (deep128 < best) return launch_tile<T, 64, 128, 1, 4, TRANS, ANY, true>(k, s);
+            const double deep = tile_cost(k, kCostDeep, el), small = tile_cost(k, kCostDeepSmall, el);
+            if (small < std::min(deep, best)) return launch_tile<T, 32, 64, 2, 2, TRANS, false, true>(k, s);
+            if (deep < best && !(near && wide < deep)) return launch_tile<T, 64, 64, 2, 2, TRANS, false, true>(k, s);
         }
+        if (near && wide < best) return launch_wide<T, TRANS>(k, s);
+        if (narrow <= c128) return launch_tile<T, 128, 64, 4, 1, TRANS, false>(k, s);
+        return launch_tile<T, 128, 128, 2, 2, TRANS, false>(k, s);
     }
-    if (narrow == best) return launch_tile<T, 128, 64, 4, 1, TRANS, ANY>(k, s);
-    if (c64 == best) return launch_tile<T, 64, 128, 1, 4, TRANS, ANY>(k, s);
-    return launch_tile<T, 128, 128, 2, 2, TRANS, ANY>(k, s);
 }
 
 TileArgs tile_args(const LinearArgs &a)

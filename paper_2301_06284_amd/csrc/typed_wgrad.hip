@@ -18,6 +18,15 @@ namespace rgnn {
 
 namespace {
 
+// Pieces of a type's rows: one up to `whole` of them, of `chunk` rows beyond; and those whose sums
+// go through the workspace.
+struct Cut {
+    int64_t whole, chunk;
+    __device__ __forceinline__ bool split(int64_t rows) const { return rows > whole; }
+    __device__ __forceinline__ int64_t pieces(int64_t rows) const { return split(rows) ? (rows + chunk - 1) / chunk : 1; }
+    __device__ __forceinline__ int64_t slots(int64_t rows) const { return split(rows) ? (rows + chunk - 1) / chunk : 0; }
+};
+
 struct WgradK {
     const char *X, *dY;
     int64_t x_rows, ldx, dy_rows, lddy;   // ld in bytes
@@ -29,33 +38,32 @@ struct WgradK {
     void *dW;
     int f32;                     // fp32 gradients
     const char *x_end, *dy_end;  // behind the last element
-    int64_t chunk, slots;
+    Cut cut;
+    int64_t slots;
     float *partial;
     int window;
 };
 
-__host__ __device__ constexpr int64_t pieces_of(int64_t rows, int64_t chunk) { return rows <= chunk ? 1 : (rows + chunk - 1) / chunk; }
-__host__ __device__ constexpr int64_t slots_of(int64_t rows, int64_t chunk) { return rows <= chunk ? 0 : (rows + chunk - 1) / chunk; }
-
-// One operand's loads: rows of the contraction, B columns from c0 on.
+// One operand's loads: rows of the contraction, B columns from c0 on.  A position whose row of
+// either operand lies outside its matrix brings zeros for both: nothing, whatever the other holds.
 template <class T, int B, int NW>
 struct Side {
     typedef typename T::elem E;
     static constexpr int KE = 128 / sizeof(E), L = B / 8 / NW, CH = B * sizeof(E) / 16, UC = sizeof(E) == 4 ? 4 : 2;
     static_assert(L * 8 * NW == B, "whole loads");
     const char *base;
-    const int32_t *index;
-    int64_t rows, ld, pos, end;  // pos: the position of this lane's first load of the next step
+    const int32_t *index, *other;         // other: the other operand's
+    int64_t rows, other_rows, ld, pos, end;   // pos: the position of this lane's first load of the next step
     int col[L];                  // bytes
-    int next[L];                 // indices of the next step's rows
+    int next[L];                 // with index arrays: the next step's rows, -1 for zeros
     int wave;
 
     __device__ __forceinline__ static int row_of(int x, int wave, int lane) { return ((x * NW + wave) * 64 + lane) / CH; }
 
-    __device__ __forceinline__ void init(const char *m, const int32_t *idx, int64_t m_rows, int64_t m_ld, int64_t p0, int64_t p1, int c0,
-                                         int width, int w, int lane)
+    __device__ __forceinline__ void init(const char *m, const int32_t *idx, int64_t m_rows, const int32_t *other_idx, int64_t o_rows,
+                                         int64_t m_ld, int64_t p0, int64_t p1, int c0, int width, int w, int lane)
     {
-        base = m; index = idx; rows = m_rows; ld = m_ld; pos = p0; end = p1; wave = w;
+        base = m; index = idx; rows = m_rows; other = other_idx; other_rows = o_rows; ld = m_ld; pos = p0; end = p1; wave = w;
 #pragma unroll
         for (int x = 0; x < L; ++x) {
             const int at = (x * NW + w) * 64 + lane, k = at / CH, p = at % CH;
@@ -67,22 +75,34 @@ struct Side {
     }
     __device__ __forceinline__ void fetch(int lane)
     {
-        if (!index) return;
+        if (!index && !other) return;
 #pragma unroll
         for (int x = 0; x < L; ++x) {
             const int64_t i = pos + row_of(x, wave, lane);
-            next[x] = i < end ? index[i] : -1;
+            int r = -1;
+            if (i < end) {
+                r = index ? index[i] : (int)i;
+                if (r >= rows) r = -1;
+                const int o = other ? other[i] : 0;
+                if (o < 0 || (other && o >= other_rows)) r = -1;
+            }
+            next[x] = r;
         }
+    }
+    // the row of load x, or one below 0
+    __device__ __forceinline__ int64_t row_at(int x, int lane) const
+    {
+        if (index || other) return next[x];
+        const int64_t i = pos + row_of(x, wave, lane);
+        return i < end ? i : -1;
     }
     // rows on any address: a step's loads into registers, and from there to LDS
     __device__ __forceinline__ void take(i32x4 (&r)[L], const char *last, int lane)
     {
 #pragma unroll
         for (int x = 0; x < L; ++x) {
-            const int64_t i = pos + row_of(x, wave, lane);
-            const int64_t row = index ? (int64_t)next[x] : i;
-            const bool ok = i < end && row >= 0 && row < rows;
-            r[x] = ok ? load_any<E>(base + row * ld + col[x], last) : i32x4{0, 0, 0, 0};
+            const int64_t row = row_at(x, lane);
+            r[x] = row >= 0 ? load_any<E>(base + row * ld + col[x], last) : i32x4{0, 0, 0, 0};
         }
         pos += KE;
         fetch(lane);
@@ -96,10 +116,8 @@ struct Side {
     {
 #pragma unroll
         for (int x = 0; x < L; ++x) {
-            const int64_t i = pos + row_of(x, wave, lane);
-            const int64_t row = index ? (int64_t)next[x] : i;
-            const bool ok = i < end && row >= 0 && row < rows;
-            load_lds(ok ? base + row * ld + col[x] : (const char *)&kZeros, lds + (x * NW + wave) * 1024);
+            const int64_t row = row_at(x, lane);
+            load_lds(row >= 0 ? base + row * ld + col[x] : (const char *)&kZeros, lds + (x * NW + wave) * 1024);
         }
         pos += KE;
         fetch(lane);
@@ -116,23 +134,24 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
     __shared__ __attribute__((aligned(1024))) char sx0[BK * 128], sy0[BN * 128], sx1[BK * 128], sy1[BN * 128];
 
     const int nk = (a.K + BK - 1) / BK, nn = (a.N + BN - 1) / BN, per = nk * nn;
-    const int64_t chunk = a.chunk;
+    const Cut cut = a.cut;
     Piece p;
-    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return pieces_of(c, chunk) * per; },
-                    [=](int64_t c) { return slots_of(c, chunk); }, p))
+    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return cut.pieces(c) * per; },
+                    [=](int64_t c) { return cut.slots(c); }, p))
         return;
+    const bool split = cut.split(p.end - p.begin);
     const int part = (int)(p.index / per);
     int ki, ni;
     tile_place((int)(p.index - (int64_t)part * per), nk, nn, ki, ni);
-    const int64_t p0 = p.begin + part * chunk;
-    const int64_t p1 = p0 + chunk < p.end ? p0 + chunk : p.end;
+    const int64_t p0 = p.begin + part * cut.chunk;
+    const int64_t p1 = split ? min(p0 + cut.chunk, p.end) : p.end;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4, wm = wave / WN, wn = wave % WN;
 
     Side<T, BK, NW> x;
     Side<T, BN, NW> y;
-    x.init(a.X, a.gather, a.x_rows, a.ldx, p0, p1, ki * BK, a.K, wave, lane);
-    y.init(a.dY, a.dy_gather, a.dy_rows, a.lddy, p0, p1, ni * BN, a.N, wave, lane);
+    x.init(a.X, a.gather, a.x_rows, a.dy_gather, a.dy_rows, a.ldx, p0, p1, ki * BK, a.K, wave, lane);
+    y.init(a.dY, a.dy_gather, a.dy_rows, a.gather, a.x_rows, a.lddy, p0, p1, ni * BN, a.N, wave, lane);
 
     // fragment f lies at (units before the wave's) + (f ^ turn): the turn sits in the address
     // bits of the units, so an exclusive or with f's bits moves from fragment to fragment
@@ -224,9 +243,7 @@ __global__ __launch_bounds__(WM *WN * 64, 1) void typed_wgrad_kernel(WgradK a)
         }
     }
 
-    const bool split = p.end - p.begin > chunk;
     const int64_t slot = p.before + part;
-    if (split && slot >= a.slots) return;            // only where the offsets are not monotone
     const int64_t at0 = (split ? slot : (int64_t)p.type) * a.K;
 #pragma unroll
     for (int m = 0; m < FM; ++m) {
@@ -257,20 +274,19 @@ __global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
     char *a2 = s2, *b2 = s2 + kWideStage, *a3 = s3, *b3 = s3 + kWideStage;
 
     const int nk = (a.K + kWide - 1) / kWide, nn = (a.N + kWide - 1) / kWide, per = nk * nn;
-    const int64_t chunk = a.chunk;
+    const Cut cut = a.cut;
     Piece p;
-    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return pieces_of(c, chunk) * per; },
-                    [=](int64_t c) { return slots_of(c, chunk); }, p))
+    if (!find_piece(a.ptr, a.T, a.M, xcd_tile(a.window), [=](int64_t c) { return cut.pieces(c) * per; },
+                    [=](int64_t c) { return cut.slots(c); }, p))
         return;
+    const bool split = cut.split(p.end - p.begin);
     const int part = p.index / per;
     int ki, ni;
     tile_place(p.index - part * per, nk, nn, ki, ni);
-    const int64_t p0 = p.begin + part * chunk;
-    const int rows = (int)min(chunk, p.end - p0);
+    const int64_t p0 = p.begin + part * cut.chunk;
+    const int rows = (int)(split ? min(cut.chunk, p.end - p0) : p.end - p0);
     const int k0 = ki * kWide, n0 = ni * kWide;
-    const bool split = p.end - p.begin > chunk;
     const int64_t slot = p.before + part;
-    if (split && slot >= a.slots) return;            // only where the offsets are not monotone
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
     to[threadIdx.x] = k0 + (int)threadIdx.x < a.K ? (int)threadIdx.x : -1;
@@ -345,15 +361,15 @@ __global__ __launch_bounds__(256, 1) void typed_wgrad_wide_kernel(WgradK a)
 // dW[t] of the types with several pieces.  A workgroup takes 64 V values of one type's gradient
 // at a time and adds a quarter of the pieces in each wave, then the quarters.
 template <class E, int V>
-__global__ __launch_bounds__(256) void wgrad_join_kernel(const int64_t *ptr, int T, int64_t M, int64_t chunk, int64_t KN,
-                                                         const float *partial, int64_t slots, void *dW, int out_f32)
+__global__ __launch_bounds__(256) void wgrad_join_kernel(const int64_t *ptr, int T, int64_t M, Cut cut, int64_t KN,
+                                                         const float *partial, void *dW, int out_f32)
 {
     typedef float vec __attribute__((ext_vector_type(V)));
     __shared__ vec sums[4][64];
     Piece p;
-    if (!find_piece(ptr, T, M, blockIdx.y, [](int64_t) { return 1; }, [=](int64_t c) { return slots_of(c, chunk); }, p)) return;
-    const int64_t n = slots_of(p.end - p.begin, chunk);
-    if (n == 0 || p.before + n > slots) return;
+    if (!find_piece(ptr, T, M, blockIdx.y, [](int64_t) { return 1; }, [=](int64_t c) { return cut.slots(c); }, p)) return;
+    const int64_t n = cut.slots(p.end - p.begin);
+    if (n == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t quarter = (n + 3) / 4, c0 = min(wave * quarter, n), c1 = min(c0 + quarter, n);
     for (int64_t i0 = blockIdx.x * (int64_t)(64 * V); i0 < KN; i0 += (int64_t)gridDim.x * (64 * V)) {
@@ -390,8 +406,8 @@ void launch_join(const WgradArgs &a, const WgradPlan &plan, hipStream_t s)
     const int f32 = a.dw_dtype == RGNN_F32;
     const float *part = (const float *)a.ws;
     LaunchScope ls("typed_wgrad_join", s);
-    if (v == 4) hipLaunchKernelGGL((wgrad_join_kernel<E, 4>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, plan.chunk, kn, part, plan.slots, a.dW, f32);
-    else hipLaunchKernelGGL((wgrad_join_kernel<E, 1>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, plan.chunk, kn, part, plan.slots, a.dW, f32);
+    if (v == 4) hipLaunchKernelGGL((wgrad_join_kernel<E, 4>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, Cut{plan.whole, plan.chunk}, kn, part, a.dW, f32);
+    else hipLaunchKernelGGL((wgrad_join_kernel<E, 1>), g, dim3(256), 0, s, a.type_ptr, a.T, a.M, Cut{plan.whole, plan.chunk}, kn, part, a.dW, f32);
 }
 
 template <class T, int BK, int BN, int WM, int WN, bool ANY>
@@ -444,16 +460,26 @@ WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
     WgradPlan p;
     p.bk = K <= 64 ? 64 : 128;
     p.bn = N <= 64 ? 64 : 128;
-    auto tiles = [&]() { return (int64_t)((K + p.bk - 1) / p.bk) * ((N + p.bn - 1) / p.bn); };
-    // the widest tile where its tiles alone fill the chip
-    if (dtype != RGNN_F32 && K > 128 && N > 128 && (int64_t)((K + 255) / 256) * ((N + 255) / 256) * T >= 256) p.bk = p.bn = 256;
+    auto tiles = [&](int64_t b) { return (K + b - 1) / b * ((N + b - 1) / b); };
+    const int64_t small = tiles(64);
+    // 64 x 64 where little work is to be spread over the chip, and for fp32, bound by matrix cores that
+    // take as long for a tile's empty part (10 007 rows of 7 types, 100 x 77: 16 us, 128 x 128 25; bf16, 292
+    // rows, 1561 x 333: 17, 19; 20 000 rows, 512 x 512: 47, 39); the widest where its tiles alone fill the chip
+    if (dtype == RGNN_F32 || (M * small <= 1 << 19 && T * small <= 1024)) p.bk = p.bn = 64;
+    else if (K > 128 && N > 128 && tiles(256) * T >= 256) p.bk = p.bn = 256;
+    const int64_t own = (int64_t)((K + p.bk - 1) / p.bk) * ((N + p.bn - 1) / p.bn);
     // pieces: enough workgroups over all tiles, and rows enough to pay for a piece's sums,
     // which are written and read back in fp32
-    const int64_t want = 512, least = p.bk == 256 ? 4096 : 128;
-    p.chunk = std::max<int64_t>(least, (M * tiles() + want - 1) / want);
+    const int64_t want = dtype == RGNN_F32 ? 1024 : 512, least = p.bk == 256 ? 4096 : 128;
+    p.chunk = std::max<int64_t>(least, (M * own + want - 1) / want);
     p.chunk = (p.chunk + 63) / 64 * 64;
-    // ceil(c / chunk) <= 2 c / chunk where c > chunk; written so that it never falls as M grows
-    p.slots = std::min(2 * M / least, 2 * want / tiles());
+    // A type is not cut where its walk takes less than the join: 256 rows (fp32, 1212 rows of 3 types, 40 x
+    // 104: 12 us, up to 512 whole 18), or 1024 where the tiles fill the chip as they are (3916 rows of 5 types, 368 x
+    // 712, bf16: 19 us, at 512 27).
+    const int64_t least_whole = T * own >= 256 ? 1024 : 256;
+    p.whole = std::max(p.chunk, least_whole);
+    // rows / chunk + 1 of at most M / whole types; written so that it never falls as M grows
+    p.slots = std::min(M / least, want / own) + std::min(M / least_whole, want / own);
     return p;
 }
 
@@ -475,7 +501,7 @@ rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
     k.dy_end = k.dY + ((a.dy_rows - 1) * a.lddy + a.N) * el;
     k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
     k.dW = a.dW; k.f32 = a.dw_dtype == RGNN_F32;
-    k.chunk = plan.chunk; k.slots = plan.slots; k.partial = (float *)a.ws;
+    k.cut = Cut{plan.whole, plan.chunk}; k.slots = plan.slots; k.partial = (float *)a.ws;
     rgnn_status st;
     {
         LaunchScope ls("typed_wgrad", s);

@@ -882,3 +882,72 @@ def test_two_streams_at_once():
             rgnn.typed_linear_wgrad(x, dy[k], dptr, both[k], works[k], stream=streams[k])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(alone, both))
+
+
+@pytest.mark.parametrize("ptr", [[0, 700, 300, 900, 900, 1000], [500, -7, 1200, 3, 800, 5000], [0] * 3 + [900] + [100] * 300 + [1000],
+                                 [40] + [0, 2 ** 62] * 300])
+def test_offsets_that_descend(ptr):
+    """Offsets are kept inside [0, M], and one below an earlier one counts as that: forward, weight
+    gradient and 8 bits as with the running maximum."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    M, K, N, T = 1000, 136, 72, len(ptr) - 1
+    kept = np.maximum.accumulate(np.clip(np.array(ptr), 0, M)).tolist()
+    g, x, w, dkept = case(torch.bfloat16, kept, K, N, T, extra=M - kept[-1])
+    given = torch.tensor(ptr, dtype=torch.int64, device="cuda")
+    xq, xs = rgnn.fp8_quantize_rows(x)
+    wq, ws = rgnn.fp8_quantize_weights(w)
+    print(f"descending offsets {T}", flush=True)
+    out = []
+    for p in (given, dkept):
+        y, y8 = (torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        dw = torch.full((T, K, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+        rgnn.typed_linear(x, p, w, y)
+        rgnn.typed_linear_fp8(xq, xs, p, wq, ws, y8)
+        rgnn.typed_linear_wgrad(x, x[:, :N], p, dw, workspace(torch.bfloat16, M, T, K, N))
+        out.append((y, y8, dw))
+    ref, size = linear_ref(x, kept, w, None, M)
+    close(out[1][0][kept[0]:kept[-1]], ref[kept[0]:kept[-1]], size[kept[0]:kept[-1]], K)
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("K,N", [(64, 64), (91, 80), (264, 136)])
+def test_wgrad_of_rows_outside(dtype, K, N):
+    """A position whose row of X or of dY lies outside adds nothing, whatever the other row holds."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    dt, ptr, rows = types()[dtype], [0, 90, 90, 700, 3000], 500
+    M, T = ptr[-1], 4
+    g = torch.Generator(device="cuda").manual_seed(K)
+    x, dy = (torch.randn(rows, c, generator=g, device="cuda").to(dt) for c in (K, N))
+    x[3], dy[5] = float("nan"), float("inf")
+    gather, dyg = (torch.randint(6, rows, (M,), generator=g, device="cuda", dtype=torch.int32) for _ in range(2))
+    for k, (a, b) in enumerate([(-1, 5), (3, rows), (rows + 9, 5), (3, -8)]):
+        gather[k::97], dyg[k::97] = a, b
+    print(f"wgrad of rows outside {dtype} {K}x{N}", flush=True)
+    dw = torch.full((T, K, N), float("nan"), dtype=dt, device="cuda")
+    rgnn.typed_linear_wgrad(x, dy, torch.tensor(ptr, device="cuda"), dw, workspace(dt, M, T, K, N), gather=gather, dy_gather=dyg)
+    inside = (gather > 5) & (gather < rows) & (dyg > 5) & (dyg < rows)
+    sel = torch.where(inside, gather, torch.full_like(gather, -1))
+    x[3], dy[5] = 0.0, 0.0
+    ref, size = wgrad_ref(x, dy, ptr, sel, dyg, T)
+    close(dw, ref, size, 2300)
+
+
+def test_typed_linear_of_no_rows():
+    """X without rows, reached through an index array: zeros; and a gradient of no positions: zeros."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    dt, K, N = torch.bfloat16, 256, 128
+    w = torch.randn(2, K, N, device="cuda").to(dt)
+    none = torch.empty(0, K, dtype=dt, device="cuda")
+    ptr = torch.tensor([0, 3, 40], device="cuda")
+    gather = torch.zeros(40, dtype=torch.int32, device="cuda")
+    y = torch.full((40, N), float("nan"), dtype=dt, device="cuda")
+    print("no rows", flush=True)
+    rgnn.typed_linear(none, ptr, w, y, gather=gather)
+    assert (y == 0).all()
+    dw = torch.full((2, K, N), float("nan"), dtype=dt, device="cuda")
+    rgnn.typed_linear_wgrad(none, torch.empty(0, N, dtype=dt, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda"), dw, None)
+    assert (dw == 0).all()
