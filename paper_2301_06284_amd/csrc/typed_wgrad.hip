@@ -400,8 +400,9 @@ void launch_join(const WgradArgs &a, const WgradPlan &plan, hipStream_t s)
 {
     const int64_t kn = (int64_t)a.K * a.N;
     const int v = kn % 4 == 0 ? 4 : 1;
-    // a workgroup looks for its type first: few of them for many types
-    const int64_t most = std::max<int64_t>(1, 4096 / a.T);
+    // a workgroup looks for its type first: no more than fill the chip (16 types, 2048 x 1536: 1024 of them
+    // 5.5 us, 4096 6.7), but 16 for a type while all are a few thousand (96 types, 64 x 64: 7.2 us, 10 for each 9.6)
+    const int64_t most = std::max<int64_t>(1, std::max<int64_t>(1024 / a.T, std::min<int64_t>(16, 4096 / a.T)));
     const dim3 g((uint32_t)std::min((kn + 64 * v - 1) / (64 * v), most), (uint32_t)a.T);
     const int f32 = a.dw_dtype == RGNN_F32;
     const float *part = (const float *)a.ws;

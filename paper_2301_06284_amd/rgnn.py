@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -66,6 +67,9 @@ class AdamwTensor(ctypes.Structure):
                 ("copy", ctypes.c_void_p), ("n", ctypes.c_int64), ("param_dtype", ctypes.c_int32),
                 ("grad_dtype", ctypes.c_int32), ("copy_dtype", ctypes.c_int32),
                 ("state_bits", ctypes.c_int32)]
+
+
+_ADAMW_PACK = struct.Struct("7Qq4i")    # an AdamwTensor at once
 
 
 class AdamwHyper(ctypes.Structure):
@@ -330,11 +334,15 @@ def segment_gemm(X, gather, type_ptr, W, Y, scatter, ws, K, Nc, stream=None):
 _DTYPES: dict = {}
 
 
-def _dtype(t) -> int:
+def _dtype_codes() -> dict:
     if not _DTYPES:
         import torch
         _DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
-    d = _DTYPES.get(t.dtype)
+    return _DTYPES
+
+
+def _dtype(t) -> int:
+    d = _dtype_codes().get(t.dtype)
     if d is None:
         raise ValueError(f"tensors must be fp32, bf16 or fp16, not {t.dtype}")
     return d
@@ -531,25 +539,30 @@ class AdamwTensors:
         self._array = (AdamwTensor * max(n, 1))()
         self._n = n
         self.device = params[0].get_device() if n else None
+        device, codes = self.device, _dtype_codes()
+        pack, at, size_of = _ADAMW_PACK.pack_into, 0, _ADAMW_PACK.size
         for k, (p, g, a, b, sa, sb, c) in enumerate(zip(*lists)):
             size, eight = p.numel(), a.dtype == torch.int8
-            _need(p.get_device() >= 0, "tensors must be on a GPU")
-            _need(all(t is None or (t.is_contiguous() and t.get_device() == self.device) for t in (p, g, a, b, sa, sb, c)),
-                  f"tensor {k}: tensors must be contiguous and on one device")
-            _need(all(t is None or t.numel() == size for t in (g, a, b, c)), f"tensor {k}: lengths differ")
+            for t in (p, g, a, b, sa, sb, c):
+                if t is not None and (t.get_device() != device or device < 0 or not t.is_contiguous()):
+                    raise ValueError(f"tensor {k}: tensors must be contiguous, on a GPU and on one device")
+            if g.numel() != size or a.numel() != size or b.numel() != size or (c is not None and c.numel() != size):
+                raise ValueError(f"tensor {k}: lengths differ")
             if eight:
                 blocks = -(-size // 256)
                 _need(b.dtype == torch.uint8 and all(t is not None and t.dtype == torch.float32 and
                                                      t.numel() == blocks for t in (sa, sb)),
                       f"tensor {k}: 8-bit states are int8 and uint8 with fp32 scales [{blocks}]")
-            else:
-                _need(a.dtype == b.dtype == torch.float32 and sa is None and sb is None,
-                      f"tensor {k}: states are fp32 without scales, or int8 and uint8 with them")
-            at = self._array[k]
-            at.param, at.grad, at.m, at.v, at.n = p.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(), size
-            at.m_scale, at.v_scale, at.copy = (None if t is None else t.data_ptr() for t in (sa, sb, c))
-            at.param_dtype, at.grad_dtype, at.copy_dtype = _dtype(p), _dtype(g), F32 if c is None else _dtype(c)
-            at.state_bits = 8 if eight else 32
+            elif a.dtype != torch.float32 or b.dtype != torch.float32 or sa is not None or sb is not None:
+                raise ValueError(f"tensor {k}: states are fp32 without scales, or int8 and uint8 with them")
+            try:
+                types = codes[p.dtype], codes[g.dtype], F32 if c is None else codes[c.dtype]
+            except KeyError:
+                raise ValueError(f"tensor {k}: parameter, gradient and copy must be fp32, bf16 or fp16") from None
+            pack(self._array, at, p.data_ptr(), g.data_ptr(), a.data_ptr(), b.data_ptr(),
+                 0 if sa is None else sa.data_ptr(), 0 if sb is None else sb.data_ptr(),
+                 0 if c is None else c.data_ptr(), size, *types, 8 if eight else 32)
+            at += size_of
 
 
 def adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
