@@ -24,7 +24,7 @@
 //   few rows: the weights' bytes, and the latency of the steps (16 rows of 2048 -> 1536, 16 of 32 types'
 //     weights read: 18 us, 5.4 TB/s; in 8 bits 10 us, 4.8 TB/s);
 //   many rows of narrow weights: memory (300 007 rows 64 -> 64, fp16: 16 us, 4.7 TB/s; 1 000 003
-//     gathered and scattered rows 64 -> 128, bf16: 106 us, 3.6 TB/s of rows at random);
+//     gathered and scattered rows 64 -> 128, bf16: 98 us, 3.9 TB/s of rows at random);
 //   many rows of wide weights: the matrix cores, at the rate of the whole tiles that the types' sizes
 //     leave (16 384 rows of 32 types, 2048 -> 4096, bf16: 300 us, 0.92 PFLOP/s; one type 233 us, 1.18; 8
 //     bits, 8192 rows 4096 -> 4096: 150 us, 1.83 PFLOP/s).

@@ -951,3 +951,38 @@ def test_typed_linear_of_no_rows():
     dw = torch.full((2, K, N), float("nan"), dtype=dt, device="cuda")
     rgnn.typed_linear_wgrad(none, torch.empty(0, N, dtype=dt, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda"), dw, None)
     assert (dw == 0).all()
+
+
+def test_wide_tile_near_32_bits():
+    """Rows whose byte offsets lie just below 2^32, where the widest tile takes 32-bit offsets from the matrix, and
+    beyond, where it does not: the same bits as the same rows of a small matrix."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    K, N, M = 2048, 4096, 16384
+    g = torch.Generator(device="cuda").manual_seed(9)
+    tail = torch.randn(1000, K, generator=g, device="cuda").to(torch.bfloat16)
+    w = (torch.randn(1, K, N, generator=g, device="cuda") / 45).to(torch.bfloat16)
+    index = torch.randint(0, 1000, (M,), generator=g, device="cuda", dtype=torch.int32)
+    ptr = torch.tensor([0, M], device="cuda")
+    ref = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    rgnn.typed_linear(tail, ptr, w, ref, gather=index)
+    for rows in ((1 << 20) - 1, (1 << 20) + 700):      # 4096 bytes each
+        x = torch.zeros(rows, K, dtype=torch.bfloat16, device="cuda")
+        x[-1000:] = tail
+        y = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+        print(f"wide tile, {rows} rows", flush=True)
+        rgnn.typed_linear(x, ptr, w, y, gather=index + (rows - 1000))
+        size = (tail.double().abs().mean() * 0.02 * K).item()
+        assert (y.double() - ref.double()).abs().max().item() <= 2 * (K * 2.0 ** -23 * size + 2.0 ** -8 * ref.double().abs().max().item())
+        if rows < 1 << 20:
+            assert torch.equal(y, ref)
+        # positions far into the matrix, without an index array for X
+        at = rows - 1000
+        far = torch.tensor([at, rows], device="cuda")
+        scatter = torch.arange(-at, rows - at, dtype=torch.int32, device="cuda")
+        z = torch.full((1000, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+        rgnn.typed_linear(x, far, w, z, scatter=scatter)
+        first = torch.full((1000, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+        rgnn.typed_linear(tail, torch.tensor([0, 1000], device="cuda"), w, first)
+        assert (z.double() - first.double()).abs().max().item() <= 2 * (K * 2.0 ** -23 * size + 2.0 ** -8 * first.double().abs().max().item())
+        del x, y, z
