@@ -362,7 +362,8 @@ rgnn_status rgnn_segment_gemm_workspace_size(int64_t M, int32_t num_types, size_
  *     a row of zeros: zero outputs, and nothing in the weight gradient, whatever the
  *     other operand holds.  A scattered one writes nothing.  Gathered rows may repeat; scattered
  *     rows that repeat race.
- *   - ldx, ldy, lddy: elements from one row to the next.  Weights are dense.
+ *   - ldx, ldy, lddy: elements from one row to the next.  Weights are dense.  Outputs
+ *     and the workspace overlap no input.
  *   - Types of the elements (rgnn_dtype): X, W and dY alike RGNN_F32, RGNN_BF16 or
  *     RGNN_F16; outputs of the same type, or RGNN_F32.  Sums are kept in fp32 and rounded
  *     once, to nearest.  fp32 operands are multiplied by the fp32 matrix cores, so
@@ -465,8 +466,8 @@ typedef struct {
 } rgnn_adamw_t;
 
 /* One step of the tensors (HOST array, read during the call only).  Tensors may lie
- * anywhere and be of any length (0 is skipped); no two may overlap, and one named twice
- * is refused (RGNN_EINVAL).
+ * anywhere and be of any length up to 2^35 (0 is skipped; RGNN_ERANGE beyond); no two may
+ * overlap, and one named twice is refused (RGNN_EINVAL).
  *   step: t, from 1.  step_dev: NULL, or DEVICE int64 [1] that holds t and is read
  *   when the kernels run, so that a captured graph counts on; `step` is then unused.
  *   grad_scale: NULL, or DEVICE fp32 [1], a factor on every gradient (clipping, loss

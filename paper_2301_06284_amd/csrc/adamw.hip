@@ -254,7 +254,7 @@ void launch_some(StepArgs<EXTRA> &a, const rgnn_adamw_tensor_t *t, const std::ve
         for (; k < list.size() && a.count < StepArgs<EXTRA>::most; ++k) {
             const rgnn_adamw_tensor_t &x = t[list[k]];
             const int64_t groups = (x.n + kBlock * 4 * a.steps - 1) / (kBlock * 4 * a.steps);
-            if (grid + groups >= (int64_t(1) << 31) - 1 && a.count) break;
+            if (grid + groups >= int64_t(1) << 24 && a.count) break;      // 2^32 threads
             const int c = a.count++;
             const bool eight = x.state_bits == 8;
             a.p[c] = x.param; a.g[c] = x.grad; a.m[c] = x.m; a.v[c] = x.v; a.n[c] = x.n;

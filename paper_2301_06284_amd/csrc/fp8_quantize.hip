@@ -63,7 +63,7 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(const E *X, int64_t rows,
                                                        uint8_t *codes, uint8_t *scales)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t task = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
+    const int64_t task = flat_block() * (int64_t)4 + (threadIdx.x >> 6);
     if (task >= rows * words) return;
     const int64_t row = task / words;
     const int w = (int)(task % words);
@@ -141,7 +141,7 @@ template <class E>
 void rows_of(const void *X, int64_t rows, int64_t ldx, int K, int Kp, int words, uint8_t *c, uint8_t *sc, hipStream_t s)
 {
     const bool vec = ((uintptr_t)X % 16 == 0) && (ldx * sizeof(E)) % 16 == 0;
-    const dim3 g((uint32_t)((rows * words + 3) / 4));
+    const dim3 g = flat_grid((rows * words + 3) / 4);
     if (vec) hipLaunchKernelGGL((fp8_rows_kernel<E, true>), g, dim3(256), 0, s, (const E *)X, rows, ldx, K, Kp, words, c, sc);
     else hipLaunchKernelGGL((fp8_rows_kernel<E, false>), g, dim3(256), 0, s, (const E *)X, rows, ldx, K, Kp, words, c, sc);
 }

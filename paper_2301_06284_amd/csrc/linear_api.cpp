@@ -174,7 +174,7 @@ extern "C" rgnn_status rgnn_adamw_step(const rgnn_adamw_tensor_t *tensors, int32
     for (int32_t i = 0; i < num_tensors; ++i) {
         const rgnn_adamw_tensor_t &t = tensors[i];
         if (t.n < 0) return bad(RGNN_EINVAL, i, "negative length");
-        if (t.n >= (int64_t(1) << 40)) return bad(RGNN_ERANGE, i, "too long");
+        if (t.n > (int64_t(1) << 35)) return bad(RGNN_ERANGE, i, "too long");
         if (!float_type(t.param_dtype) || !float_type(t.grad_dtype) || (t.copy && !float_type(t.copy_dtype)))
             return bad(RGNN_EINVAL, i, "parameter, gradient and copy must be fp32, bf16 or fp16");
         if (t.state_bits != 32 && t.state_bits != 8) return bad(RGNN_EINVAL, i, "states have 32 or 8 bits");

@@ -158,8 +158,8 @@ inline int64_t xcd_grid(int64_t tiles, int window) { return (tiles + window * 8 
 // The tile of a workgroup: each XCD, which takes every eighth workgroup, gets neighbours.
 __device__ __forceinline__ int xcd_tile(int window)
 {
-    const uint32_t in = blockIdx.x & (uint32_t)(window * 8 - 1);   // a power of two
-    return (int)(blockIdx.x - in + (in & 7) * window + (in >> 3));
+    const uint32_t block = flat_block(), in = block & (uint32_t)(window * 8 - 1);   // a power of two
+    return (int)(block - in + (in & 7) * window + (in >> 3));
 }
 
 }  // namespace rgnn

@@ -552,7 +552,7 @@ rgnn_status launch_wide(TileArgs k, hipStream_t s)
     k.window = xcd_window(tiles);
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    hipLaunchKernelGGL((typed_linear_wide_kernel<T, TRANS>), dim3((uint32_t)grid), dim3(256), 0, s, k);
+    hipLaunchKernelGGL((typed_linear_wide_kernel<T, TRANS>), flat_grid(grid), dim3(256), 0, s, k);
     return RGNN_OK;
 }
 
@@ -563,7 +563,7 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
     k.window = xcd_window(tiles);
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    const dim3 g((uint32_t)grid), b(WM * WN * 64);
+    const dim3 g = flat_grid(grid), b(WM * WN * 64);
     if (k.K * (int)sizeof(typename T::elem) <= 128)
         hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, 1>), g, b, 0, s, k);
     else

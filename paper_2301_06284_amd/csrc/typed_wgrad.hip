@@ -424,7 +424,7 @@ rgnn_status launch_tile(WgradK k, hipStream_t s)
     k.window = xcd_window(tiles);
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    hipLaunchKernelGGL((typed_wgrad_kernel<T, BK, BN, WM, WN, ANY>), dim3((uint32_t)grid), dim3(WM * WN * 64), 0, s, k);
+    hipLaunchKernelGGL((typed_wgrad_kernel<T, BK, BN, WM, WN, ANY>), flat_grid(grid), dim3(WM * WN * 64), 0, s, k);
     return RGNN_OK;
 }
 
@@ -435,7 +435,7 @@ rgnn_status launch_wide(WgradK k, hipStream_t s)
     k.window = xcd_window(tiles);
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
-    hipLaunchKernelGGL((typed_wgrad_wide_kernel<T>), dim3((uint32_t)grid), dim3(256), 0, s, k);
+    hipLaunchKernelGGL((typed_wgrad_wide_kernel<T>), flat_grid(grid), dim3(256), 0, s, k);
     return RGNN_OK;
 }
 

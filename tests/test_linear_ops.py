@@ -986,3 +986,32 @@ def test_wide_tile_near_32_bits():
         rgnn.typed_linear(tail, torch.tensor([0, 1000], device="cuda"), w, first)
         assert (z.double() - first.double()).abs().max().item() <= 2 * (K * 2.0 ** -23 * size + 2.0 ** -8 * first.double().abs().max().item())
         del x, y, z
+
+
+def test_more_workgroups_than_a_launch_is_wide():
+    """2^24 workgroups and more: rows of one column, and rows in 8 bits."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    rows = (1 << 30) + 777
+    x = torch.empty(rows, 1, device="cuda")
+    part = torch.arange(1 << 20, device="cuda", dtype=torch.float32)
+    x[:1 << 30].view(1 << 10, 1 << 20).copy_(part)
+    x[1 << 30:, 0] = part[:777] + 5
+    cut = (1 << 30) + 100
+    y = torch.empty(rows, 1, device="cuda")
+    print("2^30 rows", flush=True)
+    rgnn.typed_linear(x, torch.tensor([0, cut, rows], device="cuda"), torch.tensor([2.0, -4.0], device="cuda").view(2, 1, 1), y)
+    x[:cut] *= 2
+    x[cut:] *= -4
+    assert torch.equal(x, y)
+    del x, y
+    rows = (1 << 26) + 9
+    x = torch.empty(rows, 8, dtype=torch.bfloat16, device="cuda")
+    x[:] = torch.tensor([1.0, -2, 3, 0.5, 0, 7, -448, 5], device="cuda").to(torch.bfloat16)
+    x[-9:] *= 2
+    print("2^26 rows in 8 bits", flush=True)
+    codes, scales = rgnn.fp8_quantize_rows(x)
+    first = codes[:1].view(torch.uint8)
+    assert (scales[:-9, 0] == 127).all() and (scales[-9:, 0] == 128).all() and (scales[:, 1:] == 127).all()
+    for at in range(0, rows, 1 << 24):
+        assert (codes[at:at + (1 << 24)].view(torch.uint8) == first).all()
