@@ -370,6 +370,8 @@ def _same_device(first, *others) -> int:
 def _stream_on(stream, device: int):
     """The stream's handle; None: the device's current stream, without making an object of it."""
     if stream is not None:
+        if getattr(stream, "device_index", device) != device:
+            raise ValueError(f"the stream is on device {stream.device_index}, the tensors on {device}")
         return _stream(stream)
     import torch
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -458,8 +460,14 @@ def fp8_widths(K: int):
     return -(-K // 128) * 128, -(-K // 512) * 4
 
 
-def _fp8_out(codes, scales, lead, blocks, K, device):
+def _fp8_out(codes, scales, lead, blocks, K, device, stream):
+    """The outputs, those that are not given in memory of the stream that writes them."""
     import torch
+    if stream is not None and (codes is None or scales is None) and device.type == "cuda":
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream):
+            return _fp8_out(codes, scales, lead, blocks, K, device, None)
     Kp, Ks = fp8_widths(K)
     if codes is None:
         codes = torch.empty(*lead, Kp, dtype=torch.float8_e4m3fn, device=device)
@@ -480,12 +488,13 @@ def _fp8_check(codes, scales, lead, blocks, K):
 
 def fp8_quantize_rows(X, codes=None, scales=None, stream=None):
     """X [rows, K] -> (codes float8_e4m3fn [rows, Kp], scales uint8 [rows, Ks]), a
-    power-of-two scale for each 128 columns of a row."""
+    power-of-two scale for each 128 columns of a row.  Outputs that are not given are
+    made in the memory of `stream`: to use them on another one, wait for it there."""
     if X.dim() != 2:
         raise ValueError("X must be a matrix")
     K = X.shape[1]
     xp, rows, ldx = _matrix(X, "X", K)
-    codes, scales = _fp8_out(codes, scales, (rows,), (rows,), K, X.device)
+    codes, scales = _fp8_out(codes, scales, (rows,), (rows,), K, X.device, stream)
     d = _same_device(X, codes, scales)
     _check(_lib.rgnn_fp8_quantize_rows(_dtype(X), xp, rows, ldx, K, codes.data_ptr(), scales.data_ptr(),
                                        _stream_on(stream, d)))
@@ -498,7 +507,7 @@ def fp8_quantize_weights(W, codes=None, scales=None, stream=None):
     if W.dim() != 3 or not W.is_contiguous():
         raise ValueError("W must be contiguous [types, K, N]")
     T, K, N = W.shape
-    codes, scales = _fp8_out(codes, scales, (T, N), (T, -(-N // 128)), K, W.device)
+    codes, scales = _fp8_out(codes, scales, (T, N), (T, -(-N // 128)), K, W.device, stream)
     d = _same_device(W, codes, scales)
     _check(_lib.rgnn_fp8_quantize_weights(_dtype(W), W.data_ptr(), T, K, N, codes.data_ptr(), scales.data_ptr(),
                                           _stream_on(stream, d)))

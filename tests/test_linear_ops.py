@@ -1015,3 +1015,24 @@ def test_more_workgroups_than_a_launch_is_wide():
     assert (scales[:-9, 0] == 127).all() and (scales[-9:, 0] == 128).all() and (scales[:, 1:] == 127).all()
     for at in range(0, rows, 1 << 24):
         assert (codes[at:at + (1 << 24)].view(torch.uint8) == first).all()
+
+
+def test_quantize_on_another_stream():
+    """Outputs made by the call belong to the stream that writes them: memory that the current stream has
+    given back with work still under way is not theirs."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    x = torch.randn(4096, 512, device="cuda").to(torch.bfloat16)
+    ref = rgnn.fp8_quantize_rows(x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    print("quantize on another stream", flush=True)
+    for stream in (side, side.cuda_stream, 0):
+        for _ in range(3):
+            busy = torch.empty(4096, 512, dtype=torch.uint8, device="cuda")   # the codes' size
+            for _ in range(20):
+                busy.fill_(3)                                                 # under way on the current stream
+            del busy
+            codes, scales = rgnn.fp8_quantize_rows(x, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(codes.view(torch.uint8), ref[0].view(torch.uint8)) and torch.equal(scales, ref[1])

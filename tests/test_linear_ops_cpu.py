@@ -164,3 +164,14 @@ def test_wrappers_refuse_cpu_tensors_and_bad_shapes():
         rgnn._matrix(x, "X", 7)
     assert rgnn._matrix(torch.zeros(9, 20)[:, 3:11], "X", 8)[1:] == (9, 20)
     assert rgnn.fp8_widths(1) == (128, 4) and rgnn.fp8_widths(513) == (640, 8)
+
+
+def test_stream_of_another_device_is_refused():
+    from paper_2301_06284_amd import rgnn
+
+    class Stream:
+        device_index, cuda_stream = 1, 64
+    with pytest.raises(ValueError, match="stream is on device 1"):
+        rgnn._stream_on(Stream(), 0)
+    assert rgnn._stream_on(Stream(), 1).value == 64
+    assert rgnn._stream_on(64, 0).value == 64
