@@ -573,7 +573,10 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
 
 // Which tile of 16 and 8 bits: each is priced by what it measured (us; 1 to 16384 rows, k of 512 to
 // 4096, one to 32 types) and the cheapest is taken.  `slots` workgroups fit the chip; a round of them
-// costs `each` and, for each KB of k of a row, `full`, down to `light` where few of the slots are taken.
+// costs `each` and, for each KB of k of a row, `full`, down to `light` where few of the slots are taken.  Where
+// a CU has several slots, rounds run into each other: a last one in part costs half as if it were apart and
+// half its share (8192 rows of 16 types, 1536 -> 2048, bf16: 128 x 128, 2.25 rounds, 68 us; 128 x 64, 3, 75; 256 x 256,
+// 1.25, 81).
 // The deep ones, with four stages, are for few tiles (64 rows, 4096 x 4096, bf16: 32 x 64 17 us, 64 x 64
 // 20, 128 x 64 with two stages 36; 1024 rows 76, 58 and 47).  Rows on any address wait for registers at
 // each step: theirs are priced apart (292 rows, 1561 -> 333: 32 x 64 16 us, 128 x 64 28, 128 x 128 36; 8192
@@ -582,10 +585,10 @@ struct TileCost {
     int bm, bn, slots;
     double each, light, full;
 };
-constexpr TileCost kCostWide = {256, 256, 256, 7.0, 12.5, 12.5};
+constexpr TileCost kCostWide = {256, 256, 256, 9.0, 7.0, 12.8};
 constexpr TileCost kCost128 = {128, 128, 512, 3.0, 6.0, 8.5};
-constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 3.7, 7.2};
-constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 3.0};
+constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 3.7, 7.5};
+constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 3.3};
 constexpr TileCost kCostDeepSmall = {32, 64, 768, 2.0, 1.6, 3.3};
 constexpr TileCost kAnyCost128 = {128, 128, 512, 3.0, 11.0, 14.0};
 constexpr TileCost kAnyCostNarrow = {128, 64, 768, 2.5, 8.5, 10.0};
@@ -603,7 +606,8 @@ double tile_cost(const TileArgs &k, const TileCost &c, int el)
 {
     const double tiles = tiles_of(k, c.bm, c.bn), kb = (double)k.K * el / 1024;
     const double rounds = std::floor(tiles / c.slots), rest = tiles / c.slots - rounds;
-    return rounds * (c.each + c.full * kb) + (rest > 0 ? c.each + (c.light + (c.full - c.light) * rest) * kb : 0);
+    const double round = c.each + c.full * kb, last = rest > 0 ? c.each + (c.light + (c.full - c.light) * rest) * kb : 0;
+    return rounds * round + (rounds > 0 && c.slots > 256 ? (last + rest * round) / 2 : last);
 }
 
 // fp32 is bound by its matrix cores, which take as long for a tile of few rows as for a full one: 64 x 64
