@@ -536,7 +536,11 @@ class AdamwTensors:
     """The tensors of adamw_step, checked once and kept: lists of parameters,
     gradients (the buffers that the backward calls write) and states m, v, fp32, or int8
     and uint8 with m_scale, v_scale (fp32, one for each 256 elements); copies: None, or a
-    tensor or None for each parameter, which takes the new value in its own type."""
+    tensor or None for each parameter, which takes the new value in its own type.
+
+    Their memory is kept too, and a step refuses a tensor that has been given other memory since
+    (`.data = `, `set_`, `resize_`): make the list again then.  Gradients that are new tensors after each
+    backward pass need a list of their own each time; a captured graph holds the addresses of its capture."""
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
         import torch
@@ -544,7 +548,7 @@ class AdamwTensors:
         m_scale, v_scale, copies = (x if x is not None else [None] * n for x in (m_scale, v_scale, copies))
         lists = (params, grads, m, v, m_scale, v_scale, copies)
         _need(all(len(x) == n for x in lists), "lists must have one length")
-        self._kept = [list(x) for x in lists]
+        self._kept = [(k, t) for k, x in enumerate(zip(*lists)) for t in x if t is not None]
         self._array = (AdamwTensor * max(n, 1))()
         self._n = n
         self.device = params[0].get_device() if n else None
@@ -572,6 +576,16 @@ class AdamwTensors:
                  0 if sa is None else sa.data_ptr(), 0 if sb is None else sb.data_ptr(),
                  0 if c is None else c.data_ptr(), size, *types, 8 if eight else 32)
             at += size_of
+        # with the storages kept, no other memory can come to lie at these addresses
+        self._storages = [t.untyped_storage() for _, t in self._kept]
+        self._where = [t.data_ptr for _, t in self._kept]
+        self._addresses = [where() for where in self._where]
+
+    def _check_addresses(self):
+        now = [where() for where in self._where]
+        if now != self._addresses:
+            k = next(k for (k, _), a, b in zip(self._kept, now, self._addresses) if a != b)
+            raise ValueError(f"tensor {k}: its memory has moved since the list was made; make the list again")
 
 
 def adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
@@ -584,6 +598,7 @@ def adamw_step(tensors: AdamwTensors, step, lr, beta1=0.9, beta2=0.999, eps=1e-8
         return
     if d != torch.cuda.current_device():
         raise ValueError(f"tensors are on device {d}, the current one is {torch.cuda.current_device()}")
+    tensors._check_addresses()
     step_dev = None
     if isinstance(step, torch.Tensor):
         if step.dtype != torch.int64 or step.numel() != 1 or step.get_device() != d:

@@ -175,3 +175,62 @@ def test_stream_of_another_device_is_refused():
         rgnn._stream_on(Stream(), 0)
     assert rgnn._stream_on(Stream(), 1).value == 64
     assert rgnn._stream_on(64, 0).value == 64
+
+
+def test_adamw_refuses_tensors_whose_memory_has_moved(monkeypatch):
+    """The addresses are kept from one step to the next: a tensor that has been given other memory
+    is refused before anything is enqueued, and the list made again is taken."""
+    import torch
+    rgnn, _ = lib()
+
+    class OnGpu(torch.Tensor):          # host memory that says it is on device 0: nothing is launched here
+        def get_device(self):
+            return 0
+
+    class Library:
+        calls = 0
+
+        def rgnn_adamw_step(self, *args):
+            Library.calls += 1
+            return 0
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(rgnn, "_lib", Library())
+    monkeypatch.setattr(rgnn, "_stream_on", lambda stream, device: None)
+
+    def make(n, dtype=torch.float32):
+        return torch.zeros(n, dtype=dtype).as_subclass(OnGpu)
+
+    def lists(bits):
+        d = dict(params=[make(600), make(0), make(7)], grads=[make(600), make(0), make(7)], copies=[make(600, torch.bfloat16), None, None])
+        if bits == 32:
+            return dict(d, m=[make(600), make(0), make(7)], v=[make(600), make(0), make(7)])
+        return dict(d, m=[make(n, torch.int8) for n in (600, 0, 7)], v=[make(n, torch.uint8) for n in (600, 0, 7)],
+                    m_scale=[make(3), make(0), make(1)], v_scale=[make(3), make(0), make(1)])
+
+    moves = {
+        "data": lambda t: setattr(t, "data", torch.zeros(t.numel(), dtype=t.dtype)),
+        "set_": lambda t: t.set_(torch.zeros(t.numel() + 5, dtype=t.dtype)[5:]),
+        "resize_": lambda t: t.resize_(1 << 20),
+        "storage": lambda t: t.untyped_storage().resize_(0),
+        "twice": lambda t: (setattr(t, "data", torch.zeros(1, dtype=t.dtype)), setattr(t, "data", torch.zeros(2, dtype=t.dtype))),
+    }
+    for bits in (32, 8):
+        for name in lists(bits):
+            for move in moves.values():
+                d = lists(bits)
+                kept = rgnn.AdamwTensors(**d)
+                before = Library.calls
+                rgnn.adamw_step(kept, 1, 1e-3)
+                rgnn.adamw_step(kept, 2, 1e-3)
+                assert Library.calls == before + 2
+                move(d[name][0])
+                with pytest.raises(ValueError, match="tensor 0.*moved"):
+                    rgnn.adamw_step(kept, 3, 1e-3)
+                assert Library.calls == before + 2
+        d = lists(bits)
+        kept = rgnn.AdamwTensors(**d)
+        moves["data"](d["grads"][2])
+        with pytest.raises(ValueError, match="tensor 2.*moved"):
+            rgnn.adamw_step(kept, 3, 1e-3)
+        rgnn.adamw_step(rgnn.AdamwTensors(**d), 3, 1e-3)
