@@ -404,6 +404,24 @@ rgnn_status rgnn_typed_linear_wgrad(int32_t dtype, const void *X, int64_t x_rows
 rgnn_status rgnn_typed_linear_wgrad_workspace_size(int32_t dtype, int64_t M, int32_t num_types,
                                                    int32_t K, int32_t N, size_t *bytes);
 
+/* The tile that a call takes, chosen from sizes, types and alignment (no launch, no device; X, W, dY
+ * and the index arrays are looked at as addresses only).  rows x cols: results of a workgroup (of the
+ * weight gradient: of K x N); stages: steps of k, or of rows, that LDS holds at a time, 1 where
+ * one step is all; any: rows that are no whole vectors of 16 bytes go through registers.
+ * rgnn_typed_linear_select_tile with RGNN_F8_E4M3 (trans_w = 1, ldx in bytes) tells that of
+ * rgnn_typed_linear_fp8. */
+typedef struct {
+    int32_t rows, cols, stages, any;
+} rgnn_tile_t;
+rgnn_status rgnn_typed_linear_select_tile(int32_t dtype, const void *X, int64_t x_rows, int64_t ldx,
+                                          const int32_t *gather, int32_t num_types, int64_t M,
+                                          const void *W, int32_t K, int32_t N, int32_t trans_w,
+                                          rgnn_tile_t *tile);
+rgnn_status rgnn_typed_linear_wgrad_select_tile(int32_t dtype, const void *X, int64_t x_rows, int64_t ldx,
+                                                const int32_t *gather, const void *dY, int64_t dy_rows,
+                                                int64_t lddy, const int32_t *dy_gather, int32_t num_types,
+                                                int64_t M, int32_t K, int32_t N, rgnn_tile_t *tile);
+
 /* 8-bit rows and weights with a scale for each block of 128.  A block's scale is the
  * least power of two s >= 2^-126 with max |x| <= 448 s, kept as the byte log2(s) + 127; its codes
  * are x / s (exact) rounded to the nearest e4m3 value, ties to even.  A block that holds

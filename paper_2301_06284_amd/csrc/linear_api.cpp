@@ -106,6 +106,46 @@ extern "C" rgnn_status rgnn_typed_linear_wgrad(int32_t dtype, const void *X, int
     return launch_typed_wgrad(a, (hipStream_t)stream);
 }
 
+extern "C" rgnn_status rgnn_typed_linear_select_tile(int32_t dtype, const void *X, int64_t x_rows, int64_t ldx,
+                                                     const int32_t *gather, int32_t num_types, int64_t M,
+                                                     const void *W, int32_t K, int32_t N, int32_t trans_w,
+                                                     rgnn_tile_t *tile)
+{
+    if (!tile) return fail(RGNN_EINVAL, "tile is NULL");
+    const bool fp8 = dtype == RGNN_F8_E4M3;
+    if (!fp8 && !float_type(dtype)) return fail(RGNN_EINVAL, "X and W must be fp32, bf16, fp16 or e4m3");
+    if (trans_w != (fp8 ? 1 : trans_w & 1)) return fail(RGNN_EINVAL, "trans_w must be 0 or 1, with 8 bits 1");
+    rgnn_status st = check_sizes(M, num_types, K, N);
+    if (st != RGNN_OK) return st;
+    if ((st = check_rows("X", X, dtype, x_rows, ldx, fp8 ? fp8_width(K) : K, gather, M)) != RGNN_OK) return st;
+    LinearArgs a;
+    a.dtype = dtype; a.y_dtype = RGNN_F32;
+    a.X = X; a.x_rows = x_rows; a.ldx = ldx; a.gather = gather;
+    a.T = num_types; a.M = M; a.W = W; a.K = K; a.N = N; a.trans_w = trans_w;
+    *tile = typed_linear_tile(a);
+    return RGNN_OK;
+}
+
+extern "C" rgnn_status rgnn_typed_linear_wgrad_select_tile(int32_t dtype, const void *X, int64_t x_rows, int64_t ldx,
+                                                           const int32_t *gather, const void *dY, int64_t dy_rows,
+                                                           int64_t lddy, const int32_t *dy_gather, int32_t num_types,
+                                                           int64_t M, int32_t K, int32_t N, rgnn_tile_t *tile)
+{
+    if (!tile) return fail(RGNN_EINVAL, "tile is NULL");
+    if (!float_type(dtype)) return fail(RGNN_EINVAL, "X and dY must be fp32, bf16 or fp16");
+    rgnn_status st = check_sizes(M, num_types, K, N);
+    if (st != RGNN_OK) return st;
+    if ((st = check_rows("X", X, dtype, x_rows, ldx, K, gather, M)) != RGNN_OK) return st;
+    if ((st = check_rows("dY", dY, dtype, dy_rows, lddy, N, dy_gather, M)) != RGNN_OK) return st;
+    WgradArgs a;
+    a.dtype = dtype; a.dw_dtype = dtype;
+    a.X = X; a.x_rows = x_rows; a.ldx = ldx; a.gather = gather;
+    a.dY = dY; a.dy_rows = dy_rows; a.lddy = lddy; a.dy_gather = dy_gather;
+    a.T = num_types; a.M = M; a.K = K; a.N = N;
+    *tile = typed_wgrad_tile(a);
+    return RGNN_OK;
+}
+
 extern "C" rgnn_status rgnn_fp8_quantize_rows(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t K,
                                               void *codes, uint8_t *scales, void *stream)
 {

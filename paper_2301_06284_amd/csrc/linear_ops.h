@@ -60,6 +60,8 @@ WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s);
+rgnn_tile_t typed_linear_tile(const LinearArgs &a);     // what the launchers take, for fp8 too
+rgnn_tile_t typed_wgrad_tile(const WgradArgs &a);
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_fp8_rows(int dtype, const void *X, int64_t rows, int64_t ldx, int K, void *codes, uint8_t *scales,

@@ -610,44 +610,58 @@ double tile_cost(const TileArgs &k, const TileCost &c, int el)
     return rounds * round + (rounds > 0 && c.slots > 256 ? (last + rest * round) / 2 : last);
 }
 
+// The tile of a call; el: bytes of an element, any: rows on any address.
+enum class Shape { k32x64, k32x64Deep, k64x64, k64x64Deep, k128x64, k128x128, kWide };
+
 // fp32 is bound by its matrix cores, which take as long for a tile of few rows as for a full one: 64 x 64
 // where those give every CU two, 32 x 64 below (33 rows of 7 types, 2624 -> 128: 38 us, 64 x 64 59,
 // 128 x 128 182; 600 000 rows 128 -> 128: 294, 253).  Four stages from 16 steps of k on (1816 -> 1192:
 // 26-29 us, with two 30; 5 steps 13, with two 11).
-template <bool TRANS, bool ANY>
-rgnn_status launch_shape_f32(const TileArgs &k, hipStream_t s)
+Shape choose_tile(const TileArgs &k, int el, bool any)
 {
-    if (tiles_of(k, 64, 64) >= 512) return launch_tile<F32, 64, 64, 2, 2, TRANS, ANY>(k, s);
-    if constexpr (!ANY)
-        if (k.K >= 512) return launch_tile<F32, 32, 64, 2, 2, TRANS, false, true>(k, s);
-    return launch_tile<F32, 32, 64, 2, 2, TRANS, ANY>(k, s);
+    if (el == 4) {
+        if (tiles_of(k, 64, 64) >= 512) return Shape::k64x64;
+        return !any && k.K >= 512 ? Shape::k32x64Deep : Shape::k32x64;
+    }
+    if (any) {
+        const double small = tile_cost(k, kAnyCostSmall, el), narrow = tile_cost(k, kAnyCostNarrow, el), c128 = tile_cost(k, kAnyCost128, el);
+        if (small < std::min(narrow, c128)) return Shape::k32x64;
+        return narrow <= c128 ? Shape::k128x64 : Shape::k128x128;
+    }
+    const double narrow = tile_cost(k, kCostNarrow, el), c128 = tile_cost(k, kCost128, el), wide = tile_cost(k, kCostWide, el);
+    const double best = std::min(narrow, c128);
+    // the wide tile's offsets have 32 bits
+    const bool near = k.x_rows > 0 && (k.gather ? k.x_rows : (int64_t)kWide) * k.ldx < (int64_t(1) << 32) &&
+                      kWide * k.w_row < (int64_t(1) << 32);
+    if (k.K * el > 128) {      // more than one step
+        const double deep = tile_cost(k, kCostDeep, el), small = tile_cost(k, kCostDeepSmall, el);
+        if (small < std::min(deep, best)) return Shape::k32x64Deep;
+        if (deep < best && !(near && wide < deep)) return Shape::k64x64Deep;
+    }
+    if (near && wide < best) return Shape::kWide;
+    return narrow <= c128 ? Shape::k128x64 : Shape::k128x128;
 }
 
 template <class T, bool TRANS, bool ANY>
 rgnn_status launch_shape(const TileArgs &k, hipStream_t s)
 {
     constexpr int el = sizeof(typename T::elem);
+    const Shape tile = choose_tile(k, el, ANY);
     if constexpr (el == 4) {
-        return launch_shape_f32<TRANS, ANY>(k, s);
-    } else if constexpr (ANY) {
-        const double small = tile_cost(k, kAnyCostSmall, el), narrow = tile_cost(k, kAnyCostNarrow, el), c128 = tile_cost(k, kAnyCost128, el);
-        if (small < std::min(narrow, c128)) return launch_tile<T, 32, 64, 2, 2, TRANS, true>(k, s);
-        if (narrow <= c128) return launch_tile<T, 128, 64, 4, 1, TRANS, true>(k, s);
-        return launch_tile<T, 128, 128, 2, 2, TRANS, true>(k, s);
+        if (tile == Shape::k64x64) return launch_tile<F32, 64, 64, 2, 2, TRANS, ANY>(k, s);
+        if constexpr (!ANY)
+            if (tile == Shape::k32x64Deep) return launch_tile<F32, 32, 64, 2, 2, TRANS, false, true>(k, s);
+        return launch_tile<F32, 32, 64, 2, 2, TRANS, ANY>(k, s);
     } else {
-        const double narrow = tile_cost(k, kCostNarrow, el), c128 = tile_cost(k, kCost128, el), wide = tile_cost(k, kCostWide, el);
-        const double best = std::min(narrow, c128);
-        // the wide tile's offsets have 32 bits
-        const bool near = k.x_rows > 0 && (k.gather ? k.x_rows : (int64_t)kWide) * k.ldx < (int64_t(1) << 32) &&
-                          kWide * k.w_row < (int64_t(1) << 32);
-        if (k.K * el > 128) {      // more than one step
-            const double deep = tile_cost(k, kCostDeep, el), small = tile_cost(k, kCostDeepSmall, el);
-            if (small < std::min(deep, best)) return launch_tile<T, 32, 64, 2, 2, TRANS, false, true>(k, s);
-            if (deep < best && !(near && wide < deep)) return launch_tile<T, 64, 64, 2, 2, TRANS, false, true>(k, s);
+        if constexpr (ANY) {
+            if (tile == Shape::k32x64) return launch_tile<T, 32, 64, 2, 2, TRANS, true>(k, s);
+        } else {
+            if (tile == Shape::k32x64Deep) return launch_tile<T, 32, 64, 2, 2, TRANS, false, true>(k, s);
+            if (tile == Shape::k64x64Deep) return launch_tile<T, 64, 64, 2, 2, TRANS, false, true>(k, s);
+            if (tile == Shape::kWide) return launch_wide<T, TRANS>(k, s);
         }
-        if (near && wide < best) return launch_wide<T, TRANS>(k, s);
-        if (narrow <= c128) return launch_tile<T, 128, 64, 4, 1, TRANS, false>(k, s);
-        return launch_tile<T, 128, 128, 2, 2, TRANS, false>(k, s);
+        if (tile == Shape::k128x64) return launch_tile<T, 128, 64, 4, 1, TRANS, ANY>(k, s);
+        return launch_tile<T, 128, 128, 2, 2, TRANS, ANY>(k, s);
     }
 }
 
@@ -667,6 +681,24 @@ TileArgs tile_args(const LinearArgs &a)
     return k;
 }
 
+// Whole vectors of 16 bytes in every row go straight to LDS.
+bool whole_rows(const LinearArgs &a)
+{
+    const int el = dtype_bytes(a.dtype);
+    return (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.W % 16 == 0 && a.ldx * el % 16 == 0 && (int64_t)a.K * el % 16 == 0 &&
+           (int64_t)a.N * el % 16 == 0;
+}
+
+TileArgs tile_args_fp8(const LinearArgs &a)
+{
+    TileArgs k = tile_args(a);
+    k.K = fp8_width(a.K);
+    k.w_row = k.K; k.w_type = (int64_t)k.K * a.N;
+    k.xs = a.x_scale; k.ws = a.w_scale; k.ks = fp8_scales(a.K); k.nb = (a.N + 127) / 128;
+    k.y_f16 = a.y_dtype == RGNN_F16;
+    return k;
+}
+
 template <class T>
 rgnn_status launch_type(const TileArgs &k, int trans, bool whole, hipStream_t s)
 {
@@ -676,12 +708,25 @@ rgnn_status launch_type(const TileArgs &k, int trans, bool whole, hipStream_t s)
 
 }  // namespace
 
+rgnn_tile_t typed_linear_tile(const LinearArgs &a)
+{
+    const bool fp8 = a.dtype == RGNN_F8_E4M3, any = !fp8 && !whole_rows(a);
+    const TileArgs k = fp8 ? tile_args_fp8(a) : tile_args(a);
+    const int el = dtype_bytes(a.dtype), one = k.K * el <= 128 ? 1 : 0;
+    switch (choose_tile(k, el, any)) {
+    case Shape::k32x64: return {32, 64, one ? 1 : 2, any};
+    case Shape::k32x64Deep: return {32, 64, one ? 1 : 4, any};
+    case Shape::k64x64: return {64, 64, one ? 1 : 2, any};
+    case Shape::k64x64Deep: return {64, 64, one ? 1 : 4, any};
+    case Shape::k128x64: return {128, 64, one ? 1 : 2, any};
+    case Shape::k128x128: return {128, 128, one ? 1 : 2, any};
+    default: return {kWide, kWide, 4, any};
+    }
+}
+
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s)
 {
-    const int el = dtype_bytes(a.dtype);
-    // whole vectors of 16 bytes in every row go straight to LDS
-    const bool whole = (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.W % 16 == 0 && a.ldx * el % 16 == 0 &&
-                       (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
+    const bool whole = whole_rows(a);
     const TileArgs k = tile_args(a);
     rgnn_status st;
     {
@@ -697,11 +742,7 @@ rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s)
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s)
 {
-    TileArgs k = tile_args(a);
-    k.K = fp8_width(a.K);
-    k.w_row = k.K; k.w_type = (int64_t)k.K * a.N;
-    k.xs = a.x_scale; k.ws = a.w_scale; k.ks = fp8_scales(a.K); k.nb = (a.N + 127) / 128;
-    k.y_f16 = a.y_dtype == RGNN_F16;
+    const TileArgs k = tile_args_fp8(a);
     rgnn_status st;
     {
         LaunchScope ls("typed_linear_fp8", s);

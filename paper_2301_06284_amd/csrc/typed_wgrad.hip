@@ -439,18 +439,27 @@ rgnn_status launch_wide(WgradK k, hipStream_t s)
     return RGNN_OK;
 }
 
+// The tile of a call with this plan; el: bytes of an element, any: rows on any address.
+struct WgradTile { int bk, bn; };
+WgradTile choose_tile(const WgradK &k, const WgradPlan &p, int el, bool any)
+{
+    // the wide tile takes rows as they are, at 32-bit offsets in a step
+    if (el == 2 && p.bk == 256 && (any || k.gather || k.dy_gather || std::max(k.ldx, k.lddy) * kWide >= (int64_t(1) << 32))) return {128, 128};
+    return {p.bk, p.bn};
+}
+
 template <class T, bool ANY>
 rgnn_status launch_shape(const WgradK &k, const WgradPlan &p, hipStream_t s)
 {
     if constexpr (sizeof(typename T::elem) == 4) {       // wgrad_plan
         return launch_tile<T, 64, 64, 2, 2, ANY>(k, s);
     } else {
-        // the wide tile takes rows as they are, at 32-bit offsets in a step
+        const WgradTile t = choose_tile(k, p, 2, ANY);
         if constexpr (!ANY)
-            if (p.bk == 256 && !k.gather && !k.dy_gather && std::max(k.ldx, k.lddy) * kWide < (int64_t(1) << 32)) return launch_wide<T>(k, s);
-        if (p.bk >= 128 && p.bn >= 128) return launch_tile<T, 128, 128, 2, 2, ANY>(k, s);
-        if (p.bk == 128) return launch_tile<T, 128, 64, 2, 2, ANY>(k, s);
-        if (p.bn == 128) return launch_tile<T, 64, 128, 2, 2, ANY>(k, s);
+            if (t.bk == 256) return launch_wide<T>(k, s);
+        if (t.bk == 128 && t.bn == 128) return launch_tile<T, 128, 128, 2, 2, ANY>(k, s);
+        if (t.bk == 128) return launch_tile<T, 128, 64, 2, 2, ANY>(k, s);
+        if (t.bn == 128) return launch_tile<T, 64, 128, 2, 2, ANY>(k, s);
         return launch_tile<T, 64, 64, 2, 2, ANY>(k, s);
     }
 }
@@ -496,12 +505,18 @@ size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N)
     return (size_t)wgrad_plan(dtype, M, T, K, N).slots * K * N * sizeof(float);
 }
 
-rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
+namespace {
+
+bool whole_rows(const WgradArgs &a)
 {
-    const WgradPlan plan = wgrad_plan(a.dtype, a.M, a.T, a.K, a.N);
     const int el = dtype_bytes(a.dtype);
-    const bool whole = (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.dY % 16 == 0 && a.ldx * el % 16 == 0 && a.lddy * el % 16 == 0 &&
-                       (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
+    return (uintptr_t)a.X % 16 == 0 && (uintptr_t)a.dY % 16 == 0 && a.ldx * el % 16 == 0 && a.lddy * el % 16 == 0 &&
+           (int64_t)a.K * el % 16 == 0 && (int64_t)a.N * el % 16 == 0;
+}
+
+WgradK wgrad_args(const WgradArgs &a, const WgradPlan &plan)
+{
+    const int el = dtype_bytes(a.dtype);
     WgradK k{};
     k.X = (const char *)a.X; k.x_rows = a.x_rows; k.ldx = a.ldx * el; k.gather = a.gather;
     k.dY = (const char *)a.dY; k.dy_rows = a.dy_rows; k.lddy = a.lddy * el; k.dy_gather = a.dy_gather;
@@ -510,6 +525,24 @@ rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
     k.ptr = a.type_ptr; k.T = a.T; k.M = a.M; k.K = a.K; k.N = a.N;
     k.dW = a.dW; k.f32 = a.dw_dtype == RGNN_F32;
     k.cut = Cut{plan.whole, plan.chunk}; k.slots = plan.slots; k.partial = (float *)a.ws;
+    return k;
+}
+
+}  // namespace
+
+rgnn_tile_t typed_wgrad_tile(const WgradArgs &a)
+{
+    const WgradPlan plan = wgrad_plan(a.dtype, a.M, a.T, a.K, a.N);
+    const bool any = !whole_rows(a);
+    const WgradTile t = choose_tile(wgrad_args(a, plan), plan, dtype_bytes(a.dtype), any);
+    return {t.bk, t.bn, t.bk == 256 ? 4 : 2, any};
+}
+
+rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s)
+{
+    const WgradPlan plan = wgrad_plan(a.dtype, a.M, a.T, a.K, a.N);
+    const bool whole = whole_rows(a);
+    const WgradK k = wgrad_args(a, plan);
     rgnn_status st;
     {
         LaunchScope ls("typed_wgrad", s);

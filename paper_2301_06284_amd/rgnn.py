@@ -39,7 +39,8 @@ EXPORTED = [
     "rgat_forward", "rgat_forward_noalloc", "hgt_forward", "rgat_backward", "rgcn_backward", "hgt_backward",
     "rgnn_segment_gemm",
     "rgnn_segment_gemm_workspace_size", "rgnn_typed_linear", "rgnn_typed_linear_wgrad",
-    "rgnn_typed_linear_wgrad_workspace_size", "rgnn_fp8_quantize_rows", "rgnn_fp8_quantize_weights",
+    "rgnn_typed_linear_wgrad_workspace_size", "rgnn_typed_linear_select_tile",
+    "rgnn_typed_linear_wgrad_select_tile", "rgnn_fp8_quantize_rows", "rgnn_fp8_quantize_weights",
     "rgnn_typed_linear_fp8", "rgnn_adamw_step", "rgnn_profile_enable", "rgnn_profile_count",
     "rgnn_profile_read", "rgnn_profile_reset", "rgnn_last_error", "rgnn_version",
 ]
@@ -59,6 +60,10 @@ class GraphInfo(ctypes.Structure):
                 ("num_vsegs", ctypes.c_int64), ("num_items", ctypes.c_int64),
                 ("num_split_dst", ctypes.c_int64), ("chunk_edges", ctypes.c_int32),
                 ("device", ctypes.c_int32)]
+
+
+class Tile(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "stages", "any")]
 
 
 class AdamwTensor(ctypes.Structure):
@@ -105,6 +110,8 @@ def _load():
         "rgnn_typed_linear_wgrad": [i32, vp, i64, i64, vp, vp, i64, i64, vp, vp, i32, i64, i32, i32, i32, vp, vp,
                                     sz, vp],
         "rgnn_typed_linear_wgrad_workspace_size": [i32, i64, i32, i32, i32, P(sz)],
+        "rgnn_typed_linear_select_tile": [i32, vp, i64, i64, vp, i32, i64, vp, i32, i32, i32, P(Tile)],
+        "rgnn_typed_linear_wgrad_select_tile": [i32, vp, i64, i64, vp, vp, i64, i64, vp, i32, i64, i32, i32, P(Tile)],
         "rgnn_fp8_quantize_rows": [i32, vp, i64, i64, i32, vp, vp, vp],
         "rgnn_fp8_quantize_weights": [i32, vp, i32, i32, i32, vp, vp, vp],
         "rgnn_typed_linear_fp8": [vp, vp, i64, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, i64, i64, vp, vp],
@@ -453,6 +460,40 @@ def typed_linear_wgrad(X, dY, type_ptr, dW, ws, gather=None, dy_gather=None, str
     _check(_lib.rgnn_typed_linear_wgrad(_dtype(X), xp, xr, ldx, gp, dp, dr, ldd, sp, type_ptr.data_ptr(), T, M, K, N,
                                         _dtype(dW), dW.data_ptr(), _ptr(ws),
                                         0 if ws is None else ws.numel() * ws.element_size(), _stream_on(stream, d)))
+
+
+def _tile(t: Tile):
+    return t.rows, t.cols, t.stages, bool(t.any)
+
+
+def typed_linear_select_tile(X, W, gather=None, scatter=None, trans_w=False):
+    """(rows, columns, stages, any address) of the tile that typed_linear takes for these tensors, or, for
+    float8_e4m3fn X and W, typed_linear_fp8."""
+    import torch
+    eight = X.dtype == torch.float8_e4m3fn
+    T, K, N = W.shape
+    if trans_w or eight:
+        K, N = N, K
+    xp, xr, ldx = _matrix(X, "X", K)
+    gp, _ = _index(gather), _index(scatter)
+    M = gather.shape[0] if gather is not None else scatter.shape[0] if scatter is not None else xr
+    t = Tile()
+    _check(_lib.rgnn_typed_linear_select_tile(F8_E4M3 if eight else _dtype(X), xp, xr, ldx, gp, T, M, W.data_ptr(), K, N,
+                                              1 if trans_w or eight else 0, ctypes.byref(t)))
+    return _tile(t)
+
+
+def typed_linear_wgrad_select_tile(X, dY, types: int, gather=None, dy_gather=None):
+    """(rows of k, columns of n, stages, any address) of the tile that typed_linear_wgrad takes."""
+    K, N = X.shape[1], dY.shape[1]
+    xp, xr, ldx = _matrix(X, "X", K)
+    dp, dr, ldd = _matrix(dY, "dY", N)
+    gp, sp = _index(gather), _index(dy_gather)
+    M = gather.shape[0] if gather is not None else dy_gather.shape[0] if dy_gather is not None else xr
+    t = Tile()
+    _check(_lib.rgnn_typed_linear_wgrad_select_tile(_dtype(X), xp, xr, ldx, gp, dp, dr, ldd, sp, types, M, K, N,
+                                                    ctypes.byref(t)))
+    return _tile(t)
 
 
 def fp8_widths(K: int):
