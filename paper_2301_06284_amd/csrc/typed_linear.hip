@@ -579,8 +579,8 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
 // 1.25, 81).
 // The deep ones, with four stages, are for few tiles (64 rows, 4096 x 4096, bf16: 32 x 64 17 us, 64 x 64
 // 20, 128 x 64 with two stages 36; 1024 rows 76, 58 and 47).  Rows on any address wait for registers at
-// each step: theirs are priced apart (292 rows, 1561 -> 333: 32 x 64 16 us, 128 x 64 28, 128 x 128 36; 8192
-// rows, 2047 -> 1535: 200, 138 and 105).
+// each step: theirs are priced apart (bf16; 292 rows, 1561 -> 333: 32 x 64 17 us, 128 x 64 30, 128 x 128 37; 8192
+// rows, 2047 -> 1535: 209, 119 and 93; 300 007 rows of 96 types, 61 -> 61: 27, 22 and 24).
 struct TileCost {
     int bm, bn, slots;
     double each, light, full;
@@ -590,9 +590,9 @@ constexpr TileCost kCost128 = {128, 128, 512, 3.0, 6.0, 8.5};
 constexpr TileCost kCostNarrow = {128, 64, 768, 2.5, 3.7, 7.5};
 constexpr TileCost kCostDeep = {64, 64, 512, 2.0, 1.9, 3.3};
 constexpr TileCost kCostDeepSmall = {32, 64, 768, 2.0, 1.6, 3.3};
-constexpr TileCost kAnyCost128 = {128, 128, 512, 3.0, 11.0, 14.0};
-constexpr TileCost kAnyCostNarrow = {128, 64, 768, 2.5, 8.5, 10.0};
-constexpr TileCost kAnyCostSmall = {32, 64, 768, 2.5, 4.6, 6.0};
+constexpr TileCost kAnyCost128 = {128, 128, 512, 4.0, 9.0, 14.0};
+constexpr TileCost kAnyCostNarrow = {128, 64, 768, 3.5, 8.5, 13.5};
+constexpr TileCost kAnyCostSmall = {32, 64, 768, 2.5, 4.6, 7.0};
 
 // Tiles that the rows make: every type that has some leaves half a tile, and has one at least.
 double tiles_of(const TileArgs &k, int bm, int bn)
