@@ -5,8 +5,8 @@
 // consecutive elements of one tensor, a wave 256 of them at a time (4 a lane), which is one block
 // of 8-bit states: its maximum is a reduction over one wave.
 // Bound by memory, small lists by their launches.  Measured: 201M fp32 values with bf16 gradients, bf16
-// copies and 8-bit states 637 us (4.9 TB/s), 24M bf16 values in 230 tensors with fp32 states 113 us in three
-// launches (4.7 TB/s), the 7 tensors of a small layer 4.9 us.  Every product and sum is rounded on its own (no fused multiply-add), so that a
+// copies and 8-bit states 629 us (5.1 TB/s), 24M bf16 values in 230 tensors with fp32 states 106 us in three
+// launches (5.0 TB/s), the 7 tensors of a small layer 4.8 us.  Every product and sum is rounded on its own (no fused multiply-add), so that a
 // state's code is the one that the same formula gives in any fp32 arithmetic.
 #include <algorithm>
 #include <cmath>

@@ -8,8 +8,8 @@
 // mantissa lies above 1.75 (0x600000), which adding 0x1FFFFF carries into it.  The maximum
 // is taken over bits as integers, where a NaN or an infinity is larger than any number.
 //
-// Bound by memory: every element is read once and a byte written.  Measured, bf16: rows 8192 x 4096 18.5
-// us (5.4 TB/s), weights 16 x 2048 x 1536 29 us (5.2 TB/s), 8 rows of 2048 2.7 us (a launch).
+// Bound by memory: every element is read once and a byte written.  Measured, bf16: rows 8192 x 4096 19
+// us (5.2 TB/s), weights 16 x 2048 x 1536 29 us (5.2 TB/s), 8 rows of 2048 2.8 us (a launch).
 #include <algorithm>
 
 #include "linear_ops.h"

@@ -21,13 +21,15 @@
 // row; 16-bit rows are turned in LDS and written in pieces as wide as a wave's columns.
 //
 // What bounds it, and what it measured (copies reach 5.2 TB/s here, large bf16 products 1.1 PFLOP/s):
-//   few rows: the weights' bytes, and the latency of the steps (16 rows of 2048 -> 1536, 16 of 32 types'
-//     weights read: 18 us, 5.4 TB/s; in 8 bits 10 us, 4.8 TB/s);
-//   many rows of narrow weights: memory (300 007 rows 64 -> 64, fp16: 16 us, 4.7 TB/s; 1 000 003
-//     gathered and scattered rows 64 -> 128, bf16: 98 us, 3.9 TB/s of rows at random);
+//   few rows: the weights' bytes, and the latency of the steps (16 rows of 2048 -> 1536, 13 of 32 types'
+//     weights read: 19 us, 4.3 TB/s; in 8 bits 10 us, 4.0 TB/s);
+//   many rows of narrow weights: memory (300 007 rows 64 -> 64, fp16: 16 us, 5.0 TB/s; 1 000 003
+//     gathered and scattered rows 64 -> 128, bf16: 95 us, 4.1 TB/s of rows at random, each counted as often as it is read);
 //   many rows of wide weights: the matrix cores, at the rate of the whole tiles that the types' sizes
-//     leave (16 384 rows of 32 types, 2048 -> 4096, bf16: 300 us, 0.92 PFLOP/s; one type 233 us, 1.18; 8
-//     bits, 8192 rows 4096 -> 4096: 150 us, 1.83 PFLOP/s).
+//     leave (16 384 rows of 32 types, 2048 -> 4096, bf16: 322 us, 0.85 PFLOP/s; one type 242 us, 1.14; 8
+//     bits, 8192 rows 4096 -> 4096: 156 us, 1.76 PFLOP/s);
+//   thousands of types: the search for a tile, which every workgroup makes from the first offset on (bf16, 65 535
+//     rows, 64 -> 64: 1024 types 10 us, 4096 42, 16 384 380, 65 535 5.1 ms).
 #include <algorithm>
 #include <cmath>
 
@@ -571,8 +573,10 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
     return RGNN_OK;
 }
 
-// Which tile of 16 and 8 bits: each is priced by what it measured (us; 1 to 16384 rows, k of 512 to
-// 4096, one to 32 types) and the cheapest is taken.  `slots` workgroups fit the chip; a round of them
+// Which tile of 16 and 8 bits: each is priced and the cheapest is taken.  The prices were fitted to times in us (1 to
+// 16384 rows, k of 512 to 4096, one to 32 types, mostly 16 bits) and tell which tile is faster, not how long
+// it takes: kernels take 1.05 to 1.6 times theirs (16 rows of 32 types, 2048 -> 1536: priced 11.8, takes 18.8; in 8 bits 6.9
+// and 10.2; 8192 rows, 4096 -> 4096, 8 bits: 120 and 156).  `slots` workgroups fit the chip; a round of them
 // costs `each` and, for each KB of k of a row, `full`, down to `light` where few of the slots are taken.  Where
 // a CU has several slots, rounds run into each other: a last one in part costs half as if it were apart and
 // half its share (8192 rows of 16 types, 1536 -> 2048, bf16: 128 x 128, 2.25 rounds, 68 us; 128 x 64, 3, 75; 256 x 256,

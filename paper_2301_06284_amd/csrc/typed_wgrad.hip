@@ -13,7 +13,7 @@
 //
 // What bounds it, and what it measured: memory at narrow widths (300 007 rows, 64 x 64, fp16: 17 us, 4.5
 // TB/s, and 7 us for the join), the matrix cores and the gradients' bytes at wide ones (8192 rows of 16
-// types, 2048 x 1536, bf16: 88 us, 0.59 PFLOP/s and 100 MB written; tiles of different types take as
+// types, 2048 x 1536, bf16: 87 us, 0.59 PFLOP/s and 100 MB written; tiles of different types take as
 // different times as these have rows), launches below (10 007 rows, 100 x 77, fp32: 13 us and 4).
 #include <algorithm>
 
@@ -443,7 +443,9 @@ rgnn_status launch_wide(WgradK k, hipStream_t s)
 struct WgradTile { int bk, bn; };
 WgradTile choose_tile(const WgradK &k, const WgradPlan &p, int el, bool any)
 {
-    // the wide tile takes rows as they are, at 32-bit offsets in a step
+    // The wide tile takes rows as they are, at 32-bit offsets in a step.  Where it is not to be had, 128 x 128 walks the
+    // pieces that the plan made for it (bf16, rows as they are and gathered, with the join: 8192 rows of 16 types, 2048 x 1536 97
+    // and 192 us; 8192 rows of one type, 4096 x 4096 332 and 804; 4099 rows of 16 types, 1000 x 1040 41 and 62).
     if (el == 2 && p.bk == 256 && (any || k.gather || k.dy_gather || std::max(k.ldx, k.lddy) * kWide >= (int64_t(1) << 32))) return {128, 128};
     return {p.bk, p.bn};
 }

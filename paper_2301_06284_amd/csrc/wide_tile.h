@@ -8,8 +8,8 @@
 // in advance: steps of 64 bytes of k in four LDS stages, the fragments of the next step read
 // while this step's are multiplied, three more steps on their way from memory.
 //
-// Measured: 4096 columns, 16 384 rows, bf16, k of 2048 233 us (1.18 PFLOP/s), of 8192 1.33 to 1.36 PFLOP/s; 8
-// bits, k of 4096 1.83, of 8192 2.13.  64 steps take 83 000 cycles, 65 500 of them the matrix cores'; a
+// Measured, calls queued one after another: 4096 columns, bf16, 16 384 rows, k of 2048 242 us (1.14 PFLOP/s), of 8192
+// 1.36 PFLOP/s; 8 bits, 8192 rows, k of 4096 1.93, of 8192 2.2.  64 steps take 83 000 cycles, 65 500 of them the matrix cores'; a
 // tile's outputs 13 000 to 16 000 more, as all CUs write at once.
 #pragma once
 
