@@ -209,8 +209,9 @@ def _e4m3_rows(x):
 
 
 def _int8(x, dim):
-    """Codes of x (32 bits) and their scales along `dim`: x times the 32-bit inverse of the scale, rounded once."""
-    scale = (x.abs().amax(dim=dim, keepdim=True) / 127.0).clamp(min=LEAST)
+    """Codes of x (32 bits) and their scales along `dim`: x times the 32-bit inverse of the scale, rounded once.
+    (The quotient in 64 bits: in 32, torch multiplies by the rounded inverse of 127.)"""
+    scale = (x.abs().amax(dim=dim, keepdim=True).double() / 127.0).float().clamp(min=LEAST)
     return torch.round(x.double() * (1.0 / scale).double()).to(torch.int8), scale
 
 
@@ -438,7 +439,7 @@ def _exact_drop(s, v):
 
 def _exact_int8(x):
     """(codes, scale) of rows of x; the scale and its inverse are numbers of 32 bits by definition."""
-    scale = torch.maximum(x.abs().max(dim=-1).values.float() / 127, torch.full((), LEAST, device=x.device))
+    scale = torch.maximum((x.abs().max(dim=-1).values / 127).float(), torch.full((), LEAST, device=x.device))
     return torch.round(x * scale.reciprocal().double()[..., None]), scale.double()
 
 
