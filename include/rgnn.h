@@ -1,7 +1,8 @@
 /*
  * rgnn.h -- C ABI of librgnn.so: RGCN, RGAT and HGT layers and their backward
  * passes on one MI355X (gfx950), in fp32, and the typed linear for training and
- * serving (fp32, 16 and 8 bits) with the AdamW step.
+ * serving (fp32, 16 and 8 bits) with what stands between two such products (norm,
+ * residual, dropout, rows in 8 bits) and the AdamW step.
  *
  * The layers follow the definitions of Hector (ASPLOS '24, arXiv 2301.06284):
  *   RGCN  -- the RGCN equation of Section "RGNN Formulation and Operators";
@@ -379,7 +380,8 @@ typedef enum {
     RGNN_F32 = 0,
     RGNN_BF16 = 1,
     RGNN_F16 = 2,
-    RGNN_F8_E4M3 = 3      /* 1 sign, 4 exponent, 3 mantissa bits, largest 448, no infinities */
+    RGNN_F8_E4M3 = 3,     /* 1 sign, 4 exponent, 3 mantissa bits, largest 448, no infinities */
+    RGNN_I8 = 4           /* 8-bit integers with scales apart */
 } rgnn_dtype;
 
 /* Y[scatter[i]] = X[gather[i]] W[t(i)] for every position i that a type owns.
@@ -412,8 +414,8 @@ rgnn_status rgnn_typed_linear_wgrad_workspace_size(int32_t dtype, int64_t M, int
  * and the index arrays are looked at as addresses only).  rows x cols: results of a workgroup (of the
  * weight gradient: of K x N); stages: steps of k, or of rows, that LDS holds at a time, 1 where
  * one step is all; any: rows that are no whole vectors of 16 bytes go through registers.
- * rgnn_typed_linear_select_tile with RGNN_F8_E4M3 (trans_w = 1, ldx in bytes) tells that of
- * rgnn_typed_linear_fp8. */
+ * rgnn_typed_linear_select_tile with RGNN_F8_E4M3 or RGNN_I8 (trans_w = 1, ldx in bytes) tells that of
+ * rgnn_typed_linear_fp8 and rgnn_typed_linear_int8. */
 typedef struct {
     int32_t rows, cols, stages, any;
 } rgnn_tile_t;
@@ -455,6 +457,97 @@ rgnn_status rgnn_typed_linear_fp8(const void *X, const uint8_t *x_scales, int64_
                                   int64_t M, const void *W, const uint8_t *w_scales, int32_t K,
                                   int32_t N, int32_t y_dtype, void *Y, int64_t y_rows, int64_t ldy,
                                   const int32_t *scatter, void *stream);
+
+/* Rows and weights as 8-bit integers, with an fp32 scale for each row (token) and for each output of a
+ * type's weight (channel):
+ *   scale = max |x| / 127, at least 2^-126;  code = x times fp32(1 / scale), rounded once to the nearest
+ *   whole number, ties to even; it lies in [-127, 127].
+ * A row or channel that holds an infinity or a NaN has a NaN scale and codes of 0.
+ *   Kp = K rounded up to 128.
+ *   rows:    X [rows, K] -> codes int8 [rows, Kp], scales [rows].
+ *   weights: W [num_types, K, N] -> codes int8 [num_types, N, Kp] (each output's k side by side), scales
+ *            [num_types, N].
+ *   Codes behind K are 0.  dtype of X and W: RGNN_F32, RGNN_BF16 or RGNN_F16.  codes on a 16-byte address,
+ *   which rows of X need not have. */
+rgnn_status rgnn_int8_quantize_rows(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t K,
+                                    void *codes, float *scales, void *stream);
+rgnn_status rgnn_int8_quantize_weights(int32_t dtype, const void *W, int32_t num_types, int32_t K,
+                                       int32_t N, void *codes, float *scales, void *stream);
+
+/* rgnn_typed_linear on such rows and weights:
+ *   Y[scatter[i]][n] = x_scales[gather[i]] w_scales[t(i)][n] sum_k X[gather[i]][k] W[t(i)][n][k].
+ * X codes [x_rows, Kp] and scales [x_rows], W codes [num_types, N, Kp] and scales [num_types, N], codes on 16-byte
+ * addresses; any codes, -128 among them; those behind K must be 0.  Y RGNN_F32, RGNN_BF16 or RGNN_F16.
+ * The sum is exact in 32 bits (K <= 130944, RGNN_ERANGE beyond); it is rounded to fp32, times the row's
+ * scale, times the output's, and to Y's type.  A NaN scale makes its row's or column's outputs NaN. */
+rgnn_status rgnn_typed_linear_int8(const void *X, const float *x_scales, int64_t x_rows,
+                                   const int32_t *gather, const int64_t *type_ptr, int32_t num_types,
+                                   int64_t M, const void *W, const float *w_scales, int32_t K,
+                                   int32_t N, int32_t y_dtype, void *Y, int64_t y_rows, int64_t ldy,
+                                   const int32_t *scatter, void *stream);
+
+/* ------------------------------------------------------------------ norm, residual, dropout
+ *
+ * What stands between two products of a layer, on matrices of `rows` rows and `cols` columns:
+ *   r = residual + D(x);   y = r / rms(r) * weight,   for training and, with y in 8 bits, for serving.
+ * What these calls share, besides the conventions above:
+ *   - Types (rgnn_dtype): each matrix and vector RGNN_F32 or 16-bit; a call's 16-bit ones all RGNN_BF16 or all
+ *     RGNN_F16.  Arithmetic in fp32, sums over a row in fp64, each output rounded once, to nearest.
+ *   - ld...: elements from one row to the next, at least cols; any address of an element (fastest on 16 bytes).
+ *   - 0 <= rows < 2^31 - 1, 1 <= cols <= 2^24; RGNN_ERANGE beyond.  Rows are independent.
+ *   - An output may be one of the inputs if it has its address, type and leading dimension (Y on X, sum on
+ *     residual); otherwise outputs overlap nothing.
+ *   - Results are reproducible: no atomics, sums in a fixed order, whatever the launch.
+ *   - A row stays in registers up to 32768 columns; longer ones are read twice or, into 8-bit integers, three times,
+ *     by one workgroup.
+ */
+
+/* Dropout.  D(x)[i][j] = x[i][j] times fp32(1 / (1 - p)) where the number of row i, column j is at least
+ * floor(p 2^32), else 0, whatever x holds there.  The number is word j % 4 of Philox4x32-10 (Salmon et al., 2011) with the
+ * counter (j / 4, i, o mod 2^32, o / 2^32) and the key (seed mod 2^32, seed / 2^32), o = offset + call mod 2^64.
+ *   rng: DEVICE int64 [2], seed and offset, read when the kernels run, so that a captured graph draws anew
+ *   when the program has moved the offset on.  call: the number of the call within a step, so that two
+ *   dropouts of a step are apart while rng stays as it is; the backward pass takes the forward's rng and call.
+ *   0 <= p <= 1; p = 1 drops all. */
+typedef struct {
+    const int64_t *rng;
+    int64_t call;
+    double p;
+} rgnn_dropout_t;
+
+/* Y = [residual +] D(X), the kept product and the sum rounded once; residual: of Y's type, or NULL.  With the output's gradient as X and
+ * no residual the call is the gradient of x; that of the residual is the output's. */
+rgnn_status rgnn_dropout(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t cols,
+                         const rgnn_dropout_t *dropout, int32_t y_dtype, const void *residual, int64_t ldr,
+                         void *Y, int64_t ldy, void *stream);
+
+/* r = [residual +] D(X), rounded to sum_dtype; s = 1 / sqrt(mean(r^2) + eps); Y = (r s) weight.
+ *   dropout: NULL for D(x) = x.  residual: [rows, cols] of sum_dtype, or NULL.  sum: where r is kept, or NULL.
+ *   weight: [cols], or NULL for ones.  rstd: fp32 [rows], takes s, or NULL.  r (X itself without residual and dropout) and
+ *   rstd are what the backward call needs.
+ *   y_dtype: fp32 or 16-bit, scales then unused; or RGNN_F8_E4M3: Y codes [rows, Kp] and scales uint8 [rows, Ks] as
+ *   rgnn_fp8_quantize_rows makes them of y in fp32; or RGNN_I8: Y codes [rows, Kp] and scales fp32 [rows] as
+ *   rgnn_int8_quantize_rows does (codes on a 16-byte address, scales on a 4-byte one; ldy unused).
+ * A NaN or an infinity in a row spoils that row alone; a row of zeros gives zeros where eps > 0. */
+rgnn_status rgnn_rms_norm(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t cols,
+                          const rgnn_dropout_t *dropout, int32_t sum_dtype, const void *residual, int64_t ldr,
+                          void *sum, int64_t lds, int32_t w_dtype, const void *weight, double eps,
+                          int32_t y_dtype, void *Y, int64_t ldy, void *scales, float *rstd, void *stream);
+
+/* Its gradients: with n = r s, g = dY weight:
+ *   dr = s (g - n mean(g n)) + d_sum;  d_residual = dr;  dX = D'(dr) (kept values times the factor);
+ *   dW = sum over the rows of dY n  (zero without rows).
+ *   sum, rstd: the forward's r and s.  d_sum: the gradient that reaches r by other ways, of sum_dtype, or NULL.
+ *   d_residual (of sum_dtype), dX, dW [cols]: each may be NULL.  ws: needed with dW.
+ *   d_residual may be d_sum, and dX dY, with the same address, type and leading dimension. */
+rgnn_status rgnn_rms_norm_backward(int32_t dy_dtype, const void *dY, int64_t rows, int64_t lddy, int32_t cols,
+                                   int32_t sum_dtype, const void *sum, int64_t lds, const float *rstd,
+                                   int32_t w_dtype, const void *weight, const void *d_sum, int64_t ldds,
+                                   const rgnn_dropout_t *dropout, void *d_residual, int64_t lddr,
+                                   int32_t dx_dtype, void *dX, int64_t lddx, int32_t dw_dtype, void *dW,
+                                   void *ws, size_t ws_bytes, void *stream);
+/* Grows with the rows, so that a workspace for the most rows serves fewer of the same columns. */
+rgnn_status rgnn_rms_norm_backward_workspace_size(int64_t rows, int32_t cols, size_t *bytes);
 
 /* ------------------------------------------------------------------ AdamW
  *

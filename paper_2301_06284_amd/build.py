@@ -21,7 +21,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["status.cpp", "graph.cpp", "api.cpp", "gemm.hip", "traverse.hip", "reduce.hip", "hgt.hip",
            "backward.hip", "fused.hip",
            "rgcn_backward.hip", "hgt_backward.hip", "noalloc.hip", "backward_heads.hip",
-           "linear_api.cpp", "typed_linear.hip", "typed_wgrad.hip", "fp8_quantize.hip", "adamw.hip"]
+           "linear_api.cpp", "typed_linear.hip", "typed_wgrad.hip", "fp8_quantize.hip", "adamw.hip",
+           "rows_api.cpp", "rms_norm.hip", "rms_norm_backward.hip", "dropout.hip", "int8_quantize.hip"]
 
 COMMON = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,5 +1,5 @@
 // linear_api.cpp -- C ABI entry points of the typed linear over device offsets (with its
-// gradients and its 8-bit form) and of the AdamW step: argument checks, then the launchers.
+// gradients and its 8-bit forms) and of the AdamW step: argument checks, then the launchers.
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -13,6 +13,8 @@ namespace {
 
 constexpr int64_t kMostRows = (int64_t(1) << 31) - 1;
 constexpr int32_t kMostTypes = 65535, kMostWidth = 1 << 24;
+// Whole blocks of 128 whose products of 8-bit integers, 2^14 at most each (-128 squared), stay below 2^31.
+constexpr int32_t kMostInt8 = ((1 << 17) - 1) / 128 * 128;
 
 bool float_type(int32_t d) { return d == RGNN_F32 || d == RGNN_BF16 || d == RGNN_F16; }
 bool on(const void *p, size_t b) { return (uintptr_t)p % b == 0; }
@@ -112,12 +114,12 @@ extern "C" rgnn_status rgnn_typed_linear_select_tile(int32_t dtype, const void *
                                                      rgnn_tile_t *tile)
 {
     if (!tile) return fail(RGNN_EINVAL, "tile is NULL");
-    const bool fp8 = dtype == RGNN_F8_E4M3;
-    if (!fp8 && !float_type(dtype)) return fail(RGNN_EINVAL, "X and W must be fp32, bf16, fp16 or e4m3");
-    if (trans_w != (fp8 ? 1 : trans_w & 1)) return fail(RGNN_EINVAL, "trans_w must be 0 or 1, with 8 bits 1");
+    const bool eight = dtype_eight(dtype);
+    if (!eight && !float_type(dtype)) return fail(RGNN_EINVAL, "X and W must be fp32, bf16, fp16, e4m3 or int8");
+    if (trans_w != (eight ? 1 : trans_w & 1)) return fail(RGNN_EINVAL, "trans_w must be 0 or 1, with 8 bits 1");
     rgnn_status st = check_sizes(M, num_types, K, N);
     if (st != RGNN_OK) return st;
-    if ((st = check_rows("X", X, dtype, x_rows, ldx, fp8 ? fp8_width(K) : K, gather, M)) != RGNN_OK) return st;
+    if ((st = check_rows("X", X, dtype, x_rows, ldx, eight ? fp8_width(K) : K, gather, M)) != RGNN_OK) return st;
     LinearArgs a;
     a.dtype = dtype; a.y_dtype = RGNN_F32;
     a.X = X; a.x_rows = x_rows; a.ldx = ldx; a.gather = gather;
@@ -193,6 +195,56 @@ extern "C" rgnn_status rgnn_typed_linear_fp8(const void *X, const uint8_t *x_sca
     a.type_ptr = type_ptr; a.T = num_types; a.M = M; a.W = W; a.w_scale = w_scales; a.K = K; a.N = N; a.trans_w = 1;
     a.Y = Y; a.y_rows = y_rows; a.ldy = ldy; a.scatter = scatter;
     return launch_typed_fp8(a, (hipStream_t)stream);
+}
+
+extern "C" rgnn_status rgnn_int8_quantize_rows(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t K,
+                                               void *codes, float *scales, void *stream)
+{
+    if (!float_type(dtype)) return fail(RGNN_EINVAL, "X must be fp32, bf16 or fp16");
+    if (rows < 0 || K <= 0) return fail(RGNN_EINVAL, "rows must not be negative, K must be positive");
+    if (rows >= kMostRows || K > kMostWidth) return fail(RGNN_ERANGE, "too many rows, or K beyond 2^24");
+    if (ldx < K) return fail(RGNN_EINVAL, "leading dimension too small");
+    if (rows == 0) return RGNN_OK;
+    if (!X || !codes || !scales) return fail(RGNN_EINVAL, "NULL pointer");
+    if (!on(X, dtype_bytes(dtype)) || !on(codes, 16) || !on(scales, 4))
+        return fail(RGNN_EINVAL, "X, codes or scales on a bad boundary");
+    return launch_int8_rows(dtype, X, rows, ldx, K, codes, scales, (hipStream_t)stream);
+}
+
+extern "C" rgnn_status rgnn_int8_quantize_weights(int32_t dtype, const void *W, int32_t num_types, int32_t K, int32_t N,
+                                                  void *codes, float *scales, void *stream)
+{
+    if (!float_type(dtype)) return fail(RGNN_EINVAL, "W must be fp32, bf16 or fp16");
+    rgnn_status st = check_sizes(0, num_types, K, N);
+    if (st != RGNN_OK) return st;
+    if (!W || !codes || !scales) return fail(RGNN_EINVAL, "NULL pointer");
+    if (!on(W, dtype_bytes(dtype)) || !on(codes, 16) || !on(scales, 4))
+        return fail(RGNN_EINVAL, "W, codes or scales on a bad boundary");
+    return launch_int8_weights(dtype, W, num_types, K, N, codes, scales, (hipStream_t)stream);
+}
+
+extern "C" rgnn_status rgnn_typed_linear_int8(const void *X, const float *x_scales, int64_t x_rows,
+                                              const int32_t *gather, const int64_t *type_ptr, int32_t num_types,
+                                              int64_t M, const void *W, const float *w_scales, int32_t K, int32_t N,
+                                              int32_t y_dtype, void *Y, int64_t y_rows, int64_t ldy,
+                                              const int32_t *scatter, void *stream)
+{
+    if (!float_type(y_dtype)) return fail(RGNN_EINVAL, "Y must be fp32, bf16 or fp16");
+    rgnn_status st = check_sizes(M, num_types, K, N);
+    if (st != RGNN_OK) return st;
+    if (K > kMostInt8) return fail(RGNN_ERANGE, "K beyond 130944: sums of 8-bit products could leave 32 bits");
+    if ((st = check_rows("X", X, RGNN_I8, x_rows, fp8_width(K), K, gather, M)) != RGNN_OK) return st;
+    if ((st = check_rows("Y", Y, y_dtype, y_rows, ldy, N, scatter, M)) != RGNN_OK) return st;
+    if (!type_ptr || !W || !w_scales || (!x_scales && M > 0 && x_rows > 0)) return fail(RGNN_EINVAL, "NULL pointer");
+    if (!on(X, 16) || !on(W, 16)) return fail(RGNN_EINVAL, "codes must be on 16-byte boundaries");
+    if (!on(x_scales, 4) || !on(w_scales, 4)) return fail(RGNN_EINVAL, "scales are not on an element's boundary");
+    if (M == 0) return RGNN_OK;
+    LinearArgs a;
+    a.dtype = RGNN_I8; a.y_dtype = y_dtype;
+    a.X = X; a.x_factor = x_scales; a.x_rows = x_rows; a.ldx = fp8_width(K); a.gather = gather;
+    a.type_ptr = type_ptr; a.T = num_types; a.M = M; a.W = W; a.w_factor = w_scales; a.K = K; a.N = N; a.trans_w = 1;
+    a.Y = Y; a.y_rows = y_rows; a.ldy = ldy; a.scatter = scatter;
+    return launch_typed_int8(a, (hipStream_t)stream);
 }
 
 extern "C" rgnn_status rgnn_adamw_step(const rgnn_adamw_tensor_t *tensors, int32_t num_tensors,

@@ -20,7 +20,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // ---------------------------------------------------------------- arguments
 
 struct LinearArgs {
-    int dtype = 0;                       // rgnn_dtype of X and W (fp8: RGNN_F8_E4M3)
+    int dtype = 0;                       // rgnn_dtype of X and W (8 bits: RGNN_F8_E4M3, RGNN_I8)
     int y_dtype = 0;
     const void *X = nullptr;   int64_t x_rows = 0, ldx = 0;
     const int32_t *gather = nullptr;
@@ -34,6 +34,8 @@ struct LinearArgs {
     const int32_t *scatter = nullptr;
     // fp8: scale bytes of X [x_rows, ks] and of W [T, ceil(N/128), ks]
     const uint8_t *x_scale = nullptr, *w_scale = nullptr;
+    // int8: scales of X [x_rows] and of W [T, N]
+    const float *x_factor = nullptr, *w_factor = nullptr;
 };
 
 struct WgradArgs {
@@ -60,13 +62,16 @@ WgradPlan wgrad_plan(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 size_t wgrad_workspace(int dtype, int64_t M, int32_t T, int32_t K, int32_t N);
 rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_typed_wgrad(const WgradArgs &a, hipStream_t s);
-rgnn_tile_t typed_linear_tile(const LinearArgs &a);     // what the launchers take, for fp8 too
+rgnn_tile_t typed_linear_tile(const LinearArgs &a);     // what the launchers take, for 8 bits too
 rgnn_tile_t typed_wgrad_tile(const WgradArgs &a);
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s);
+rgnn_status launch_typed_int8(const LinearArgs &a, hipStream_t s);
 rgnn_status launch_fp8_rows(int dtype, const void *X, int64_t rows, int64_t ldx, int K, void *codes, uint8_t *scales,
                             hipStream_t s);
 rgnn_status launch_fp8_weights(int dtype, const void *W, int T, int K, int N, void *codes, uint8_t *scales, hipStream_t s);
+rgnn_status launch_int8_rows(int dtype, const void *X, int64_t rows, int64_t ldx, int K, void *codes, float *scales, hipStream_t s);
+rgnn_status launch_int8_weights(int dtype, const void *W, int T, int K, int N, void *codes, float *scales, hipStream_t s);
 rgnn_status launch_adamw(const rgnn_adamw_tensor_t *t, int32_t count, const rgnn_adamw_t &h, int64_t step,
                          const int64_t *step_dev, const float *grad_scale, hipStream_t s);
 
@@ -74,7 +79,8 @@ rgnn_status launch_adamw(const rgnn_adamw_tensor_t *t, int32_t count, const rgnn
 constexpr int32_t fp8_width(int32_t K) { return (K + 127) / 128 * 128; }
 constexpr int32_t fp8_scales(int32_t K) { return (K + 511) / 512 * 4; }
 
-constexpr int dtype_bytes(int d) { return d == RGNN_F32 ? 4 : d == RGNN_F8_E4M3 ? 1 : 2; }
+constexpr bool dtype_eight(int d) { return d == RGNN_F8_E4M3 || d == RGNN_I8; }
+constexpr int dtype_bytes(int d) { return d == RGNN_F32 ? 4 : dtype_eight(d) ? 1 : 2; }
 
 // Row tiles of `rows` rows that M rows of T types can make, at most: every type that
 // has rows can leave one tile partly filled.
@@ -99,6 +105,7 @@ __device__ __forceinline__ uint32_t flat_block() { return blockIdx.y * gridDim.x
 struct F32 { typedef float elem; };
 struct BF16 { typedef __bf16 elem; };
 struct F16 { typedef _Float16 elem; };
+struct I8 { typedef int8_t elem; };
 
 // D[n][m] += sum_k a[n][k] b[m][k] over 16 bytes of k a lane: lane l holds row l % 16
 // of both, 16-byte chunk l / 16 of the step's k.  The order of k within a step is the
@@ -116,6 +123,12 @@ template <>
 __device__ __forceinline__ f32x4 mma16<F16>(i32x4 a, i32x4 b, f32x4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// 8-bit integers: the sums are whole numbers of 32 bits, kept in the registers of the others' fp32 sums.
+template <>
+__device__ __forceinline__ f32x4 mma16<I8>(i32x4 a, i32x4 b, f32x4 c)
+{
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, __builtin_bit_cast(i32x4, c), 0, 0, 0));
 }
 template <>
 __device__ __forceinline__ f32x4 mma16<F32>(i32x4 a, i32x4 b, f32x4 c)

@@ -1,0 +1,257 @@
+// rms_norm_backward.hip -- gradients of the root-mean-square norm with residual and dropout.
+//
+// With n = r s and g = dY w: dr = s (g - n mean(g n)) + dsum, the residual's gradient; dX = D'(dr), whose kept
+// values the generator tells again; dw = sum over the rows of dY n.  A row is read once and stays in registers.
+// A workgroup takes every G-th group of rows and keeps dw of its columns in registers to the end, then
+// writes it to the workspace; a second launch adds the G rows there in 64 bits, in their order, so that results are
+// reproducible.
+#include <algorithm>
+
+#include "rows.h"
+
+namespace rgnn {
+
+namespace {
+
+constexpr int kLong = 32768;         // columns that registers hold
+
+struct Shape {
+    int lanes, vectors, per;         // threads of a row, vectors of a thread, rows of a workgroup
+};
+Shape shape_of(int cols)
+{
+    if (cols <= 64) return {8, 1, 32};
+    if (cols <= 128) return {16, 1, 16};
+    if (cols <= 256) return {32, 1, 8};
+    if (cols <= 512) return {64, 1, 4};
+    if (cols <= 1024) return {64, 2, 4};
+    if (cols <= 2048) return {256, 1, 1};
+    if (cols <= 4096) return {256, 2, 1};
+    if (cols <= 8192) return {256, 4, 1};
+    if (cols <= 16384) return {1024, 2, 1};
+    if (cols <= kLong) return {1024, 4, 1};
+    return {1024, 0, 1};
+}
+int64_t groups_of(int64_t rows, int cols)
+{
+    const Shape s = shape_of(cols);
+    return std::min<int64_t>((rows + s.per - 1) / s.per, s.lanes > 256 ? 256 : 1024);
+}
+
+template <class H>
+__device__ __forceinline__ void store_typed(void *base, bool f32, int64_t at, const float (&x)[8], int left)
+{
+    if (f32) store8<float>(base, at, x, left);
+    else store8<H>(base, at, x, left);
+}
+
+// dX of eight columns from dr, and both stored.
+template <class H, class RT>
+__device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const Philox &gen, int64_t row, int c, float (&dr)[8])
+{
+    if (a.dres) store8<RT>(a.dres, row * a.lddr + c, dr, a.cols - c);
+    if (!a.dX) return;
+    if (a.drop.rng) {
+        uint32_t word[8];
+        gen.eight(c, row, word);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dr[i] = word[i] > a.drop.below ? dr[i] * a.drop.factor : 0.0f;
+    }
+    store_typed<H>(a.dX, a.dx32, row * a.lddx + c, dr, a.cols - c);
+}
+
+template <class H, bool DY32, bool R32, int L, int NV>
+__global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(NormBackwardArgs a)
+{
+#pragma clang fp contract(off)
+    typedef typename std::conditional<DY32, float, H>::type YT;
+    typedef typename std::conditional<R32, float, H>::type RT;
+    constexpr int PER = L >= 256 ? 1 : 256 / L;
+    __shared__ double sums[2][L > 64 ? L / 64 : 1];
+    __shared__ float part[PER > 1 ? 256 * NV * 8 : 1];
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    Philox gen;
+    if (a.drop.rng) gen.init(a.drop);
+    float w[NV][8], dw[NV][8] = {};
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load_weight<H>(a.w, a.w32, (v * L + lane) * 8, a.cols - (v * L + lane) * 8, w[v]);
+    int turn = 0;
+    for (int64_t row = blockIdx.x * (int64_t)PER + group; row < a.rows; row += gridDim.x * (int64_t)PER, turn ^= 1) {
+        Eight<YT> dy[NV];
+        Eight<RT> r[NV], ds[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * L + lane) * 8;
+            dy[v].load((const YT *)a.dY + row * a.lddy + c, a.cols - c);
+            r[v].load((const RT *)a.r + row * a.ldr + c, a.cols - c);
+        }
+        if (a.dsum)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * L + lane) * 8;
+                ds[v].load((const RT *)a.dsum + row * a.ldds + c, a.cols - c);
+            }
+        const float s = a.rstd[row];
+        double dot = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = (float)dy[v].v[i], n = (float)r[v].v[i] * s;
+                dw[v][i] = __builtin_fmaf(d, n, dw[v][i]);
+                dot += (double)(d * w[v][i] * n);
+            }
+        const float mean = (float)(row_sum<L>(dot, sums[turn]) / a.cols);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float dr[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = (float)dy[v].v[i] * w[v][i], n = (float)r[v].v[i] * s;
+                dr[i] = s * (g - n * mean);
+                if (a.dsum) dr[i] += (float)ds[v].v[i];
+            }
+            store_gradients<H, RT>(a, gen, row, (v * L + lane) * 8, dr);
+        }
+    }
+    if (!a.dW) return;
+    float *out = a.ws + blockIdx.x * (int64_t)a.cols;
+    if constexpr (PER == 1) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) store8<float>(out, (v * L + lane) * 8, dw[v], a.cols - (v * L + lane) * 8);
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float *to = part + group * (L * NV * 8) + (v * L + lane) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i] = dw[v][i];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.cols; c += 256) {
+            float x = 0;
+            for (int g = 0; g < PER; ++g) x += part[g * (L * NV * 8) + c];
+            out[c] = x;
+        }
+    }
+}
+
+// Rows that registers do not hold: a workgroup of 1024 goes over each of its rows twice and keeps its dw in
+// the workspace, each thread its own columns.
+template <class H, bool DY32, bool R32>
+__global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwardArgs a)
+{
+#pragma clang fp contract(off)
+    typedef typename std::conditional<DY32, float, H>::type YT;
+    typedef typename std::conditional<R32, float, H>::type RT;
+    __shared__ double sums[2][16];
+    Philox gen;
+    if (a.drop.rng) gen.init(a.drop);
+    float *out = a.dW ? a.ws + blockIdx.x * (int64_t)a.cols : nullptr;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const float s = a.rstd[row];
+        double dot = 0;
+        for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
+            Eight<YT> dy;
+            Eight<RT> r;
+            float w[8];
+            dy.load((const YT *)a.dY + row * a.lddy + c, a.cols - c);
+            r.load((const RT *)a.r + row * a.ldr + c, a.cols - c);
+            load_weight<H>(a.w, a.w32, c, a.cols - c, w);
+            for (int i = 0; i < 8 && c + i < a.cols; ++i) {
+                const float d = (float)dy.v[i], n = (float)r.v[i] * s;
+                dot += (double)(d * w[i] * n);
+                if (out) out[c + i] = row == (int64_t)blockIdx.x ? d * n : __builtin_fmaf(d, n, out[c + i]);
+            }
+        }
+        const float mean = (float)(row_sum<1024>(dot, sums[turn]) / a.cols);
+        for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
+            Eight<YT> dy;
+            Eight<RT> r, ds;
+            float w[8], dr[8];
+            dy.load((const YT *)a.dY + row * a.lddy + c, a.cols - c);
+            r.load((const RT *)a.r + row * a.ldr + c, a.cols - c);
+            if (a.dsum) ds.load((const RT *)a.dsum + row * a.ldds + c, a.cols - c);
+            load_weight<H>(a.w, a.w32, c, a.cols - c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float g = (float)dy.v[i] * w[i], n = (float)r.v[i] * s;
+                dr[i] = s * (g - n * mean);
+                if (a.dsum) dr[i] += (float)ds.v[i];
+            }
+            store_gradients<H, RT>(a, gen, row, c, dr);
+        }
+    }
+}
+
+// dw of 16 columns: 64 threads a column over the workspace's rows, then over each other's sums.
+template <class H>
+__global__ __launch_bounds__(1024) void rms_norm_join_kernel(const float *ws, int64_t groups, int cols, void *dW, bool f32)
+{
+    __shared__ double part[64][17];
+    const int at = threadIdx.x & 15, slice = threadIdx.x >> 4, c = blockIdx.x * 16 + at;
+    double x = 0;
+    if (c < cols)
+#pragma unroll 4
+        for (int64_t g = slice; g < groups; g += 64) x += (double)ws[g * cols + c];
+    part[slice][at] = x;
+    __syncthreads();
+    if (threadIdx.x >= 16 || c >= cols) return;
+    x = 0;
+    for (int i = 0; i < 64; ++i) x += part[i][at];
+    if (f32) ((float *)dW)[c] = (float)x;
+    else ((H *)dW)[c] = (H)(float)x;
+}
+
+template <class H, bool DY32, bool R32, int L, int NV>
+void launch_shape(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
+{
+    hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, L, NV>), dim3((uint32_t)groups), dim3(L > 256 ? L : 256), 0, s, a);
+}
+
+template <class H, bool DY32, bool R32>
+void launch_types(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
+{
+    if (a.cols <= 64) launch_shape<H, DY32, R32, 8, 1>(a, groups, s);
+    else if (a.cols <= 128) launch_shape<H, DY32, R32, 16, 1>(a, groups, s);
+    else if (a.cols <= 256) launch_shape<H, DY32, R32, 32, 1>(a, groups, s);
+    else if (a.cols <= 512) launch_shape<H, DY32, R32, 64, 1>(a, groups, s);
+    else if (a.cols <= 1024) launch_shape<H, DY32, R32, 64, 2>(a, groups, s);
+    else if (a.cols <= 2048) launch_shape<H, DY32, R32, 256, 1>(a, groups, s);
+    else if (a.cols <= 4096) launch_shape<H, DY32, R32, 256, 2>(a, groups, s);
+    else if (a.cols <= 8192) launch_shape<H, DY32, R32, 256, 4>(a, groups, s);
+    else if (a.cols <= 16384) launch_shape<H, DY32, R32, 1024, 2>(a, groups, s);
+    else if (a.cols <= kLong) launch_shape<H, DY32, R32, 1024, 4>(a, groups, s);
+    else hipLaunchKernelGGL((rms_norm_backward_long_kernel<H, DY32, R32>), dim3((uint32_t)groups), dim3(1024), 0, s, a);
+}
+
+template <class H>
+void launch_half(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
+{
+    if (a.dy32) a.r32 ? launch_types<H, true, true>(a, groups, s) : launch_types<H, true, false>(a, groups, s);
+    else a.r32 ? launch_types<H, false, true>(a, groups, s) : launch_types<H, false, false>(a, groups, s);
+}
+
+}  // namespace
+
+size_t rms_norm_backward_workspace(int64_t rows, int32_t cols) { return (size_t)groups_of(rows, cols) * cols * sizeof(float); }
+
+rgnn_status launch_rms_norm_backward(const NormBackwardArgs &a, hipStream_t s)
+{
+    const int64_t groups = groups_of(a.rows, a.cols);
+    if (groups) {
+        LaunchScope ls("rms_norm_backward", s);
+        if (a.half == RGNN_F16) launch_half<_Float16>(a, groups, s);
+        else launch_half<__bf16>(a, groups, s);
+    }
+    if (a.dW) {
+        LaunchScope ls("rms_norm_join", s);
+        const dim3 g((uint32_t)((a.cols + 15) / 16));
+        if (a.half == RGNN_F16) hipLaunchKernelGGL((rms_norm_join_kernel<_Float16>), g, dim3(1024), 0, s, a.ws, groups, a.cols, a.dW, a.dw32);
+        else hipLaunchKernelGGL((rms_norm_join_kernel<__bf16>), g, dim3(1024), 0, s, a.ws, groups, a.cols, a.dW, a.dw32);
+    }
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? RGNN_OK : hip_fail(e, "rms_norm_backward launch");
+}
+
+}  // namespace rgnn

@@ -57,6 +57,7 @@ struct TileArgs {
     int window;                  // workgroups dealt to the XCDs at a time, over 8
     const uint8_t *xs, *ws;      // fp8: scale bytes
     int ks, nb;                  // bytes of a row's scales; 128-blocks of n
+    const float *xf, *wf;        // int8: scales of rows and of outputs
 };
 
 struct F8 { typedef uint8_t elem; };
@@ -74,6 +75,14 @@ __device__ __forceinline__ void tile_row(const TileArgs &a, int64_t i, int64_t e
     if (!in && to >= 0) to = -2 - to;
 }
 
+// int8: the scales of four outputs side by side, of those that the weight has.
+__device__ __forceinline__ void output_scales(const TileArgs &a, int type, int j, float (&out)[4])
+{
+    const float *wf = a.wf + (int64_t)type * a.N;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = wf[min(j + i, a.N - 1)];
+}
+
 // ANY: rows on any address.  Loads go through registers (16 bytes from any address; at the end of
 // k and of the matrix by elements) and are written to LDS a step later.  STAGES: 1 where all of k is
 // one step, which leaves LDS and registers for more workgroups on a CU; 4 where a CU has few of them and
@@ -83,7 +92,7 @@ template <class T, int BM, int BN, int WM, int WN, bool TRANS, bool ANY, int STA
 __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear_kernel(TileArgs a)
 {
     typedef typename T::elem E;
-    constexpr bool FP8 = sizeof(E) == 1;
+    constexpr bool FP8 = std::is_same<T, F8>::value, INT8 = std::is_same<T, I8>::value;
     constexpr int NW = WM * WN, KE = 128 / sizeof(E);
     constexpr int FM = BM / WM / 16, FN = BN / WN / 16;     // fragments of a wave
     constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;       // KB that a wave loads each step
@@ -370,6 +379,20 @@ __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear
     // ---- write
     const int *out = to + wm * FM * 16;
     const int j1 = j0 + wn * FN * 16;               // this wave's first column
+    if constexpr (INT8) {                           // whole numbers to fp32, times the scales
+        float wf[FN][4];
+#pragma unroll
+        for (int f = 0; f < FN; ++f) output_scales(a, p.type, j1 + f * 16 + g * 4, wf[f]);
+#pragma unroll
+        for (int m = 0; m < FM; ++m) {
+            const int row = from[(wm * FM + m) * 16 + r16];
+            const float xf = row >= 0 ? a.xf[row] : 0.0f;
+#pragma unroll
+            for (int f = 0; f < FN; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][f][i] = (float)__float_as_int(acc[m][f][i]) * xf * wf[f][i];
+        }
+    }
     if (sizeof(E) == 4 || a.y_f32) {
 #pragma unroll
         for (int m = 0; m < FM; ++m) {
@@ -387,7 +410,7 @@ __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear
     }
     step_barrier<0>();                              // the stages may be used again
     char *mine = s0 + wave * (FM * FN * 512);
-    if (FP8 && a.y_f16) write_rows<_Float16, FM, FN>(mine, acc, (_Float16 *)a.Y + j1, a.ldy, a.N - j1, lane, out);
+    if (sizeof(E) == 1 && a.y_f16) write_rows<_Float16, FM, FN>(mine, acc, (_Float16 *)a.Y + j1, a.ldy, a.N - j1, lane, out);
     else write_rows<typename std::conditional<sizeof(E) != 2, __bf16, E>::type, FM, FN>(
         mine, acc, (typename std::conditional<sizeof(E) != 2, __bf16, E>::type *)a.Y + j1, a.ldy, a.N - j1, lane, out);
 }
@@ -397,7 +420,7 @@ template <class T, bool TRANS>
 __global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
 {
     typedef typename T::elem E;
-    constexpr bool FP8 = sizeof(E) == 1;
+    constexpr bool FP8 = std::is_same<T, F8>::value, INT8 = std::is_same<T, I8>::value;
     constexpr int KE = kWideKB / sizeof(E);
     __shared__ __attribute__((aligned(1024))) char s0[2 * kWideStage], s1[2 * kWideStage], s2[2 * kWideStage], s3[2 * kWideStage];
     char *a0 = s0, *b0 = s0 + kWideStage, *a1 = s1, *b1 = s1 + kWideStage;
@@ -520,11 +543,29 @@ __global__ __launch_bounds__(256, 1) void typed_linear_wide_kernel(TileArgs a)
         };
         wide_walk<FMV, false, !TRANS, LA + kWideLoads>(a0, b0, a1, b1, a2, b2, a3, b3, fa, fb, steps, whole, load, edge, multiply,
                                                        shift, acc);
-        typedef typename std::conditional<FP8, __bf16, E>::type O;
+        if constexpr (INT8) {
+            const float *xf = a.gather ? a.xf : a.xf + i0;
+            float x[FMV];
+#pragma unroll
+            for (int m = 0; m < FMV; ++m) x[m] = xf[from[(wm * FMV + m) * 32 + (lane & 31)]];
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float wf[4];
+                    output_scales(a, p.type, j0 + wn * 128 + n * 32 + q * 8 + (lane >> 5) * 4, wf);
+#pragma unroll
+                    for (int m = 0; m < FMV; ++m)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            acc[m][n][q * 4 + i] = (float)__float_as_int(acc[m][n][q * 4 + i]) * x[m] * wf[i];
+                }
+        }
+        typedef typename std::conditional<sizeof(E) == 1, __bf16, E>::type O;
         const int *out = to + wm * FMV * 32;
         char *mine = wave == 0 ? s0 : wave == 1 ? s1 : wave == 2 ? s2 : s3;
         const int cols = a.N - j0 - wn * 128;
-        if (FP8 && a.y_f16) return wide_write<_Float16, FMV>(mine, acc, (_Float16 *)a.Y + j0 + wn * 128, a.ldy, cols, lane, out);
+        if (sizeof(E) == 1 && a.y_f16) return wide_write<_Float16, FMV>(mine, acc, (_Float16 *)a.Y + j0 + wn * 128, a.ldy, cols, lane, out);
         if (!a.y_f32) return wide_write<O, FMV>(mine, acc, (O *)a.Y + j0 + wn * 128, a.ldy, cols, lane, out);
 #pragma unroll
         for (int m = 0; m < FMV; ++m) {
@@ -693,12 +734,13 @@ bool whole_rows(const LinearArgs &a)
            (int64_t)a.N * el % 16 == 0;
 }
 
-TileArgs tile_args_fp8(const LinearArgs &a)
+TileArgs tile_args_eight(const LinearArgs &a)
 {
     TileArgs k = tile_args(a);
     k.K = fp8_width(a.K);
     k.w_row = k.K; k.w_type = (int64_t)k.K * a.N;
     k.xs = a.x_scale; k.ws = a.w_scale; k.ks = fp8_scales(a.K); k.nb = (a.N + 127) / 128;
+    k.xf = a.x_factor; k.wf = a.w_factor;
     k.y_f16 = a.y_dtype == RGNN_F16;
     return k;
 }
@@ -714,8 +756,8 @@ rgnn_status launch_type(const TileArgs &k, int trans, bool whole, hipStream_t s)
 
 rgnn_tile_t typed_linear_tile(const LinearArgs &a)
 {
-    const bool fp8 = a.dtype == RGNN_F8_E4M3, any = !fp8 && !whole_rows(a);
-    const TileArgs k = fp8 ? tile_args_fp8(a) : tile_args(a);
+    const bool eight = dtype_eight(a.dtype), any = !eight && !whole_rows(a);
+    const TileArgs k = eight ? tile_args_eight(a) : tile_args(a);
     const int el = dtype_bytes(a.dtype), one = k.K * el <= 128 ? 1 : 0;
     switch (choose_tile(k, el, any)) {
     case Shape::k32x64: return {32, 64, one ? 1 : 2, any};
@@ -746,7 +788,7 @@ rgnn_status launch_typed_linear(const LinearArgs &a, hipStream_t s)
 
 rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s)
 {
-    const TileArgs k = tile_args_fp8(a);
+    const TileArgs k = tile_args_eight(a);
     rgnn_status st;
     {
         LaunchScope ls("typed_linear_fp8", s);
@@ -755,6 +797,19 @@ rgnn_status launch_typed_fp8(const LinearArgs &a, hipStream_t s)
     if (st != RGNN_OK) return st;
     hipError_t e = hipGetLastError();
     return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_linear_fp8 launch");
+}
+
+rgnn_status launch_typed_int8(const LinearArgs &a, hipStream_t s)
+{
+    const TileArgs k = tile_args_eight(a);
+    rgnn_status st;
+    {
+        LaunchScope ls("typed_linear_int8", s);
+        st = launch_shape<I8, true, false>(k, s);
+    }
+    if (st != RGNN_OK) return st;
+    hipError_t e = hipGetLastError();
+    return e == hipSuccess ? RGNN_OK : hip_fail(e, "typed_linear_int8 launch");
 }
 
 }  // namespace rgnn

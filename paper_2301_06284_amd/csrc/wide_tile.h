@@ -18,13 +18,14 @@
 namespace rgnn {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kWide = 256, kWideKB = 64;             // tile, bytes of k of a step
 constexpr int kWideStage = kWide * kWideKB;          // bytes of one operand's stage
 constexpr int kWideLoads = kWideStage / 1024 / 4;    // loads of a wave and operand each step
 
 // D[n][m] += a[n][k] b[m][k] over 32 rows each: lane l holds row l % 32, chunks l / 32 and
-// l / 32 + 2 of the 64 bytes of k (16-bit: an instruction each; 8-bit: one of both).  The
+// l / 32 + 2 of the 64 bytes of k (16-bit and 8-bit integers: an instruction each; e4m3: one of both).  The
 // result's lane holds m = l % 32 and n = 8 (i / 4) + 4 (l / 32) + i % 4, i = 0 .. 15.
 template <class T>
 __device__ __forceinline__ f32x16 mma32(i32x4 a, i32x4 b, f32x16 c);
@@ -37,6 +38,12 @@ template <>
 __device__ __forceinline__ f32x16 mma32<F16>(i32x4 a, i32x4 b, f32x16 c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+template <>
+__device__ __forceinline__ f32x16 mma32<I8>(i32x4 a, i32x4 b, f32x16 c)
+{
+    return __builtin_bit_cast(f32x16, __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, __builtin_bit_cast(i32x16, c), 0, 0, 0));
 }
 
 // Chunk q of a fragment.

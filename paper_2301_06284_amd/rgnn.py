@@ -25,7 +25,7 @@ LAYER_RGCN_BACKWARD, LAYER_HGT_BACKWARD = 5, 6
 SOFTMAX_PER_DST, SOFTMAX_PER_DST_REL = 0, 1
 FLAG_RELU, FLAG_RESIDUAL, FLAG_A_LINEAR = 1, 2, 4
 GRAPH_HOST_ONLY, GRAPH_NO_COMPACT = 1, 2
-F32, BF16, F16, F8_E4M3 = 0, 1, 2, 3
+F32, BF16, F16, F8_E4M3, I8 = 0, 1, 2, 3, 4
 
 INDEX_KINDS = {
     "dst_rowptr": 0, "in_src": 1, "in_rel": 2, "in_eid": 3, "seg_ptr": 4, "seg_rel": 5,
@@ -41,7 +41,8 @@ EXPORTED = [
     "rgnn_segment_gemm_workspace_size", "rgnn_typed_linear", "rgnn_typed_linear_wgrad",
     "rgnn_typed_linear_wgrad_workspace_size", "rgnn_typed_linear_select_tile",
     "rgnn_typed_linear_wgrad_select_tile", "rgnn_fp8_quantize_rows", "rgnn_fp8_quantize_weights",
-    "rgnn_typed_linear_fp8", "rgnn_adamw_step", "rgnn_profile_enable", "rgnn_profile_count",
+    "rgnn_typed_linear_fp8", "rgnn_int8_quantize_rows", "rgnn_int8_quantize_weights", "rgnn_typed_linear_int8",
+    "rgnn_dropout", "rgnn_rms_norm", "rgnn_rms_norm_backward", "rgnn_rms_norm_backward_workspace_size", "rgnn_adamw_step", "rgnn_profile_enable", "rgnn_profile_count",
     "rgnn_profile_read", "rgnn_profile_reset", "rgnn_last_error", "rgnn_version",
 ]
 
@@ -64,6 +65,10 @@ class GraphInfo(ctypes.Structure):
 
 class Tile(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "stages", "any")]
+
+
+class DropoutArgs(ctypes.Structure):
+    _fields_ = [("rng", ctypes.c_void_p), ("call", ctypes.c_int64), ("p", ctypes.c_double)]
 
 
 class AdamwTensor(ctypes.Structure):
@@ -115,6 +120,15 @@ def _load():
         "rgnn_fp8_quantize_rows": [i32, vp, i64, i64, i32, vp, vp, vp],
         "rgnn_fp8_quantize_weights": [i32, vp, i32, i32, i32, vp, vp, vp],
         "rgnn_typed_linear_fp8": [vp, vp, i64, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, i64, i64, vp, vp],
+        "rgnn_int8_quantize_rows": [i32, vp, i64, i64, i32, vp, vp, vp],
+        "rgnn_int8_quantize_weights": [i32, vp, i32, i32, i32, vp, vp, vp],
+        "rgnn_typed_linear_int8": [vp, vp, i64, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, i64, i64, vp, vp],
+        "rgnn_dropout": [i32, vp, i64, i64, i32, P(DropoutArgs), i32, vp, i64, vp, i64, vp],
+        "rgnn_rms_norm": [i32, vp, i64, i64, i32, P(DropoutArgs), i32, vp, i64, vp, i64, i32, vp, ctypes.c_double, i32, vp,
+                          i64, vp, vp, vp],
+        "rgnn_rms_norm_backward": [i32, vp, i64, i64, i32, i32, vp, i64, vp, i32, vp, vp, i64, P(DropoutArgs), vp, i64, i32,
+                                   vp, i64, i32, vp, vp, sz, vp],
+        "rgnn_rms_norm_backward_workspace_size": [i64, i32, P(sz)],
         "rgnn_adamw_step": [P(AdamwTensor), i32, P(AdamwHyper), i64, vp, vp, vp],
         "rgnn_profile_enable": [i32],
         "rgnn_profile_count": [P(i32)],
@@ -468,18 +482,18 @@ def _tile(t: Tile):
 
 def typed_linear_select_tile(X, W, gather=None, scatter=None, trans_w=False):
     """(rows, columns, stages, any address) of the tile that typed_linear takes for these tensors, or, for
-    float8_e4m3fn X and W, typed_linear_fp8."""
+    float8_e4m3fn X and W, typed_linear_fp8, for int8 typed_linear_int8."""
     import torch
-    eight = X.dtype == torch.float8_e4m3fn
+    eight = {torch.float8_e4m3fn: F8_E4M3, torch.int8: I8}.get(X.dtype)
     T, K, N = W.shape
-    if trans_w or eight:
+    if trans_w or eight is not None:
         K, N = N, K
     xp, xr, ldx = _matrix(X, "X", K)
     gp, _ = _index(gather), _index(scatter)
     M = gather.shape[0] if gather is not None else scatter.shape[0] if scatter is not None else xr
     t = Tile()
-    _check(_lib.rgnn_typed_linear_select_tile(F8_E4M3 if eight else _dtype(X), xp, xr, ldx, gp, T, M, W.data_ptr(), K, N,
-                                              1 if trans_w or eight else 0, ctypes.byref(t)))
+    _check(_lib.rgnn_typed_linear_select_tile(_dtype(X) if eight is None else eight, xp, xr, ldx, gp, T, M, W.data_ptr(),
+                                              K, N, 1 if trans_w or eight is not None else 0, ctypes.byref(t)))
     return _tile(t)
 
 
@@ -501,14 +515,22 @@ def fp8_widths(K: int):
     return -(-K // 128) * 128, -(-K // 512) * 4
 
 
+def _on_stream(stream, device, make):
+    """make() with the allocator on `stream`."""
+    import torch
+    if stream is None or device.type != "cuda":
+        return make()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return make()
+
+
 def _fp8_out(codes, scales, lead, blocks, K, device, stream):
     """The outputs, those that are not given in memory of the stream that writes them."""
     import torch
-    if stream is not None and (codes is None or scales is None) and device.type == "cuda":
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
-        with torch.cuda.stream(stream):
-            return _fp8_out(codes, scales, lead, blocks, K, device, None)
+    if stream is not None and (codes is None or scales is None):
+        return _on_stream(stream, device, lambda: _fp8_out(codes, scales, lead, blocks, K, device, None))
     Kp, Ks = fp8_widths(K)
     if codes is None:
         codes = torch.empty(*lead, Kp, dtype=torch.float8_e4m3fn, device=device)
@@ -571,6 +593,180 @@ def typed_linear_fp8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatter
     _check(_lib.rgnn_typed_linear_fp8(X.data_ptr(), x_scales.data_ptr(), rows, gp, type_ptr.data_ptr(), T, M,
                                       W.data_ptr(), w_scales.data_ptr(), K, N, _dtype(Y), yp, yr, ldy, sp,
                                       _stream_on(stream, d)))
+
+
+def _int8_out(codes, scales, lead, K, device, stream):
+    """The outputs, those that are not given in memory of the stream that writes them."""
+    import torch
+    if stream is not None and (codes is None or scales is None):
+        return _on_stream(stream, device, lambda: _int8_out(codes, scales, lead, K, device, None))
+    if codes is None:
+        codes = torch.empty(*lead, fp8_widths(K)[0], dtype=torch.int8, device=device)
+    if scales is None:
+        scales = torch.empty(lead, dtype=torch.float32, device=device)
+    _int8_check(codes, scales, lead, K)
+    return codes, scales
+
+
+def _int8_check(codes, scales, lead, K):
+    import torch
+    Kp = fp8_widths(K)[0]
+    if codes.dtype != torch.int8 or codes.shape != (*lead, Kp) or not codes.is_contiguous():
+        raise ValueError(f"codes must be contiguous int8 {(*lead, Kp)}")
+    if scales.dtype != torch.float32 or scales.shape != lead or not scales.is_contiguous():
+        raise ValueError(f"scales must be contiguous float32 {lead}")
+
+
+def int8_quantize_rows(X, codes=None, scales=None, stream=None):
+    """X [rows, K] -> (codes int8 [rows, Kp], scales float32 [rows]), a scale for each row.  Outputs that
+    are not given are made in the memory of `stream`: to use them on another one, wait for it there."""
+    if X.dim() != 2:
+        raise ValueError("X must be a matrix")
+    K = X.shape[1]
+    xp, rows, ldx = _matrix(X, "X", K)
+    codes, scales = _int8_out(codes, scales, (rows,), K, X.device, stream)
+    d = _same_device(X, codes, scales)
+    _check(_lib.rgnn_int8_quantize_rows(_dtype(X), xp, rows, ldx, K, codes.data_ptr(), scales.data_ptr(),
+                                        _stream_on(stream, d)))
+    return codes, scales
+
+
+def int8_quantize_weights(W, codes=None, scales=None, stream=None):
+    """W [types, K, N] -> (codes int8 [types, N, Kp], scales float32 [types, N]), a scale for each output."""
+    if W.dim() != 3 or not W.is_contiguous():
+        raise ValueError("W must be contiguous [types, K, N]")
+    T, K, N = W.shape
+    codes, scales = _int8_out(codes, scales, (T, N), K, W.device, stream)
+    d = _same_device(W, codes, scales)
+    _check(_lib.rgnn_int8_quantize_weights(_dtype(W), W.data_ptr(), T, K, N, codes.data_ptr(), scales.data_ptr(),
+                                           _stream_on(stream, d)))
+    return codes, scales
+
+
+def typed_linear_int8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatter=None, stream=None):
+    """typed_linear on the codes and scales of int8_quantize_rows (or rms_norm) and
+    int8_quantize_weights; Y fp32, bf16 or fp16."""
+    d = _same_device(X, x_scales, type_ptr, W, w_scales, Y, gather, scatter)
+    if W.dim() != 3 or X.dim() != 2:
+        raise ValueError("X must be [rows, Kp], W [types, N, Kp]")
+    T, N, K = W.shape
+    rows = X.shape[0]
+    _int8_check(X, x_scales, (rows,), K)
+    _int8_check(W, w_scales, (T, N), K)
+    yp, yr, ldy = _matrix(Y, "Y", N)
+    gp, sp = _index(gather), _index(scatter)
+    M = _positions(type_ptr, T, gather, scatter, rows)
+    _check(_lib.rgnn_typed_linear_int8(X.data_ptr(), x_scales.data_ptr(), rows, gp, type_ptr.data_ptr(), T, M,
+                                       W.data_ptr(), w_scales.data_ptr(), K, N, _dtype(Y), yp, yr, ldy, sp,
+                                       _stream_on(stream, d)))
+
+
+class Dropout:
+    """What rms_norm, its backward and dropout drop: a value with probability p, by the numbers of a
+    counter-based generator.  rng: device int64 [2], seed and offset, read when the kernels run; call: the number
+    of the call within a step.  The backward pass takes the forward's Dropout and the same rng."""
+
+    def __init__(self, p: float, rng, call: int = 0):
+        import torch
+        if rng.dtype != torch.int64 or rng.dim() != 1 or rng.shape[0] != 2 or not rng.is_contiguous():
+            raise ValueError("rng must be contiguous int64 [2]")
+        if not 0 <= p <= 1:
+            raise ValueError("p must lie in [0, 1]")
+        self.p, self.rng, self.call = float(p), rng, int(call)
+
+    def _args(self):
+        return DropoutArgs(self.rng.data_ptr(), self.call, self.p)
+
+
+def _rows(t, name: str, rows: int, cols: int, dtype=None):
+    """(pointer, leading dimension) of a matrix of that size."""
+    p, r, ld = _matrix(t, name, cols)
+    if r != rows or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be [{rows}, {cols}]" + (f" of {dtype}" if dtype is not None else ""))
+    return p, ld
+
+
+def _vector(t, name: str, n: int, dtype=None):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be contiguous [{n}]" + (f" of {dtype}" if dtype is not None else ""))
+    return t.data_ptr()
+
+
+def _drop(dropout):
+    return None if dropout is None else ctypes.byref(dropout._args())
+
+
+def dropout(X, Y, dropout: Dropout, residual=None, stream=None):
+    """Y = [residual +] D(X); X, Y fp32, bf16 or fp16, residual of Y's type.  Y may be X or residual.  With the
+    output's gradient as X and no residual: the gradient of x."""
+    d = _same_device(X, Y, dropout.rng, residual)
+    if X.dim() != 2:
+        raise ValueError("X must be a matrix")
+    rows, cols = X.shape
+    xp, ldx = _rows(X, "X", rows, cols)
+    yp, ldy = _rows(Y, "Y", rows, cols)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", rows, cols, Y.dtype)
+    _check(_lib.rgnn_dropout(_dtype(X), xp, rows, ldx, cols, _drop(dropout), _dtype(Y), rp, ldr, yp, ldy,
+                             _stream_on(stream, d)))
+
+
+def rms_norm(X, weight, Y, eps=1e-6, residual=None, sum=None, scales=None, rstd=None, dropout=None, stream=None):
+    """r = [residual +] D(X), Y = r / sqrt(mean(r^2) + eps) * weight for each row; weight [cols] or None.
+    sum: takes r (of residual's type; X's without one); rstd: float32 [rows], takes the root's inverse.  Y fp32,
+    bf16 or fp16; or float8_e4m3fn codes [rows, Kp] with scales uint8 [rows, Ks] for typed_linear_fp8; or int8 codes
+    [rows, Kp] with scales float32 [rows] for typed_linear_int8.  Y may be X, sum may be residual."""
+    import torch
+    d = _same_device(X, weight, Y, residual, sum, scales, rstd, None if dropout is None else dropout.rng)
+    if X.dim() != 2:
+        raise ValueError("X must be a matrix")
+    rows, cols = X.shape
+    xp, ldx = _rows(X, "X", rows, cols)
+    kept = residual if residual is not None else sum if sum is not None else X
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", rows, cols)
+    sp, lds = (None, 0) if sum is None else _rows(sum, "sum", rows, cols, kept.dtype)
+    if Y.dtype == torch.float8_e4m3fn or Y.dtype == torch.int8:
+        if scales is None:
+            raise ValueError("8-bit codes need scales")
+        code = F8_E4M3 if Y.dtype == torch.float8_e4m3fn else I8
+        _fp8_check(Y, scales, (rows,), (rows,), cols) if code == F8_E4M3 else _int8_check(Y, scales, (rows,), cols)
+        yp, ldy, scp = Y.data_ptr(), 0, scales.data_ptr()
+    else:
+        if scales is not None:
+            raise ValueError("scales are for 8-bit codes")
+        (yp, ldy), code, scp = _rows(Y, "Y", rows, cols), _dtype(Y), None
+    _check(_lib.rgnn_rms_norm(_dtype(X), xp, rows, ldx, cols, _drop(dropout), _dtype(kept), rp, ldr, sp, lds,
+                              F32 if weight is None else _dtype(weight), _vector(weight, "weight", cols), eps, code, yp, ldy,
+                              scp, _vector(rstd, "rstd", rows, torch.float32), _stream_on(stream, d)))
+
+
+def rms_norm_backward_workspace_size(rows: int, cols: int) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.rgnn_rms_norm_backward_workspace_size(rows, cols, ctypes.byref(n)))
+    return n.value
+
+
+def rms_norm_backward(dY, sum, rstd, weight, d_sum=None, d_residual=None, dX=None, dW=None, ws=None, dropout=None,
+                      stream=None):
+    """The gradients of rms_norm: sum and rstd as it wrote them (sum: X itself without residual and dropout), d_sum
+    the gradient that reaches the sum by other ways.  d_residual (sum's type), dX and dW [cols] are written where
+    given; dW needs the workspace ws.  d_residual may be d_sum, dX may be dY."""
+    import torch
+    d = _same_device(dY, sum, rstd, weight, d_sum, d_residual, dX, dW, ws, None if dropout is None else dropout.rng)
+    if dY.dim() != 2:
+        raise ValueError("dY must be a matrix")
+    rows, cols = dY.shape
+    yp, ldy = _rows(dY, "dY", rows, cols)
+    sp, lds = _rows(sum, "sum", rows, cols)
+    gp, ldg = (None, 0) if d_sum is None else _rows(d_sum, "d_sum", rows, cols, sum.dtype)
+    rp, ldr = (None, 0) if d_residual is None else _rows(d_residual, "d_residual", rows, cols, sum.dtype)
+    xp, ldx = (None, 0) if dX is None else _rows(dX, "dX", rows, cols)
+    _check(_lib.rgnn_rms_norm_backward(
+        _dtype(dY), yp, rows, ldy, cols, _dtype(sum), sp, lds, _vector(rstd, "rstd", rows, torch.float32),
+        F32 if weight is None else _dtype(weight), _vector(weight, "weight", cols), gp, ldg, _drop(dropout), rp, ldr,
+        F32 if dX is None else _dtype(dX), xp, ldx, F32 if dW is None else _dtype(dW), _vector(dW, "dW", cols), _ptr(ws),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream_on(stream, d)))
 
 
 class AdamwTensors:
