@@ -20,55 +20,72 @@ struct Cut {
     uint32_t inverse;    // ceil(2^32 / wide)
 };
 
-template <class H, bool X32, bool Y32>
+// RES: with a residual.  DROP: p is not 0.
+template <class H, bool X32, bool Y32, bool WHOLE, bool RES, bool DROP>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, Cut cut)
 {
 #pragma clang fp contract(off)
     typedef typename std::conditional<X32, float, H>::type XT;
     typedef typename std::conditional<Y32, float, H>::type YT;
-    const uint32_t block = flat_block(), down = block / (uint32_t)cut.across;
+    const uint32_t block = flat_block(), down = cut.across == 1 ? block : block / (uint32_t)cut.across;
     const int first = (int)(block - down * cut.across) * cut.wide;
     const int64_t row0 = (int64_t)down * cut.tall;
-    Philox gen;
-    if (a.drop.rng) gen.init(a.drop);
-    Eight<XT> x[kVectors];
-    Eight<YT> in[kVectors];
+    // Every thread loads all its vectors, those outside from inside: no branch stands between the loads.
+    Eight<XT, WHOLE> x[kVectors];
+    Eight<YT, WHOLE> in[RES ? kVectors : 1];
     int64_t row[kVectors];
     int col[kVectors];
 #pragma unroll
     for (int u = 0; u < kVectors; ++u) {
         const uint32_t i = threadIdx.x + u * 256;
         const uint32_t r = cut.wide == 1 ? i : __umulhi(i, cut.inverse);
-        row[u] = row0 + r;
+        row[u] = (int)r < cut.tall ? row0 + r : a.rows;
         col[u] = (first + (int)(i - r * cut.wide)) * 8;
-        if ((int)r >= cut.tall || row[u] >= a.rows || col[u] >= a.cols) row[u] = -1;
-        if (row[u] < 0) continue;
-        x[u].load((const XT *)a.X + row[u] * a.ldx + col[u], a.cols - col[u]);
-        if (a.res) in[u].load((const YT *)a.res + row[u] * a.ldr + col[u], a.cols - col[u]);
+        const int64_t from = min(row[u], a.rows - 1);
+        x[u].load((const XT *)a.X + from * a.ldx, col[u], a.cols);
+        if constexpr (RES) in[u].load((const YT *)a.res + from * a.ldr, col[u], a.cols);
     }
+    Philox gen;
+    if constexpr (DROP) gen.init(a.drop);
 #pragma unroll
     for (int u = 0; u < kVectors; ++u) {
-        if (row[u] < 0) continue;
+        if (row[u] >= a.rows || col[u] >= a.cols) continue;
+        x[u].settle(col[u], a.cols);
+        if constexpr (RES) in[u].settle(col[u], a.cols);
         float y[8];
         uint32_t word[8];
-        if (a.drop.rng) gen.eight(col[u], row[u], word);
+        if constexpr (DROP) gen.eight(col[u], row[u], word);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float res = a.res ? (float)in[u].v[i] : 0.0f, v = (float)x[u].v[i];
-            const float kept = a.res ? __builtin_fmaf(v, a.drop.factor, res) : v * a.drop.factor;
-            y[i] = !a.drop.rng || word[i] > a.drop.below ? kept : res;
+            const float res = RES ? in[RES ? u : 0].at(i) : 0.0f, v = x[u].at(i);
+            const float kept = RES ? __builtin_fmaf(v, a.drop.factor, res) : v * a.drop.factor;
+            y[i] = !DROP || word[i] > a.drop.below ? kept : res;
         }
-        store8<YT>(a.Y, row[u] * a.ldy + col[u], y, a.cols - col[u]);
+        store8<YT, WHOLE>(a.Y, row[u] * a.ldy, y, col[u], a.cols);
     }
+}
+
+template <class H, bool X32, bool Y32>
+void launch_types(const DropoutArgs &a, const Cut &cut, dim3 grid, hipStream_t s)
+{
+    auto go = [&](auto whole, auto res, auto drop) {
+        hipLaunchKernelGGL((dropout_kernel<H, X32, Y32, decltype(whole)::value, decltype(res)::value, decltype(drop)::value>), grid, dim3(256),
+                           0, s, a, cut);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    auto with = [&](auto whole) {
+        if (a.drop.rng) a.res ? go(whole, yes, yes) : go(whole, no, yes);
+        else a.res ? go(whole, yes, no) : go(whole, no, no);
+    };
+    whole_vectors(a.cols) ? with(yes) : with(no);
 }
 
 template <class H>
 void launch_half(const DropoutArgs &a, const Cut &cut, dim3 grid, hipStream_t s)
 {
-    if (a.x32 && a.y32) hipLaunchKernelGGL((dropout_kernel<H, true, true>), grid, dim3(256), 0, s, a, cut);
-    else if (a.x32) hipLaunchKernelGGL((dropout_kernel<H, true, false>), grid, dim3(256), 0, s, a, cut);
-    else if (a.y32) hipLaunchKernelGGL((dropout_kernel<H, false, true>), grid, dim3(256), 0, s, a, cut);
-    else hipLaunchKernelGGL((dropout_kernel<H, false, false>), grid, dim3(256), 0, s, a, cut);
+    if (a.x32) a.y32 ? launch_types<H, true, true>(a, cut, grid, s) : launch_types<H, true, false>(a, cut, grid, s);
+    else a.y32 ? launch_types<H, false, true>(a, cut, grid, s) : launch_types<H, false, false>(a, cut, grid, s);
 }
 
 }  // namespace

@@ -11,7 +11,7 @@ namespace rgnn {
 
 namespace {
 
-template <class E, int L, int NV>
+template <class E, bool WHOLE, int L, int NV>
 __global__ __launch_bounds__(L > 256 ? L : 256) void int8_rows_kernel(const E *X, int64_t rows, int64_t ldx, int K, uint8_t *codes,
                                                                       float *scales)
 {
@@ -20,14 +20,16 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void int8_rows_kernel(const E *X
     const int64_t row = flat_block() * (int64_t)PER + (PER > 1 ? threadIdx.x / L : 0);
     if (row >= rows) return;
     const int lane = threadIdx.x % L, kp = fp8_width(K);
-    Eight<E> x[NV];
+    Eight<E, WHOLE> x[NV];
     uint32_t top = 0;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) x[v].load(X + row * ldx + (v * L + lane) * 8, K - (v * L + lane) * 8);
+    for (int v = 0; v < NV; ++v) x[v].load(X + row * ldx, (v * L + lane) * 8, K);
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+    for (int v = 0; v < NV; ++v) {
+        x[v].settle((v * L + lane) * 8, K);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits((float)x[v].v[i]));
+        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(x[v].at(i)));
+    }
     const float scale = int8_scale(row_max<L>(top, tops)), inverse = 1.0f / scale;
     if (lane == 0) scales[row] = scale;
 #pragma unroll
@@ -35,7 +37,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void int8_rows_kernel(const E *X
         const int c = (v * L + lane) * 8;
         float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (float)x[v].v[i];
+        for (int i = 0; i < 8; ++i) f[i] = x[v].at(i);
         if (c < kp) store_int8(codes + row * kp + c, f, inverse, scale != scale);
     }
 }
@@ -50,26 +52,28 @@ __global__ __launch_bounds__(1024) void int8_long_rows_kernel(const E *X, int64_
     const int kp = fp8_width(K);
     uint32_t top = 0;
     for (int c = threadIdx.x * 8; c < K; c += 8192) {
-        Eight<E> x;
-        x.load(X + row * ldx + c, K - c);
+        Eight<E, false> x;
+        x.load(X + row * ldx, c, K);
+        x.settle(c, K);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits((float)x.v[i]));
+        for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(x.at(i)));
     }
     const float scale = int8_scale(row_max<1024>(top, tops)), inverse = 1.0f / scale;
     if (threadIdx.x == 0) scales[row] = scale;
     for (int c = threadIdx.x * 8; c < kp; c += 8192) {
-        Eight<E> x;
+        Eight<E, false> x;
         float f[8];
-        x.load(X + row * ldx + c, K - c);
+        x.load(X + row * ldx, c, K);
+        x.settle(c, K);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (float)x.v[i];
+        for (int i = 0; i < 8; ++i) f[i] = x.at(i);
         store_int8(codes + row * kp + c, f, inverse, scale != scale);
     }
 }
 
 // A workgroup takes 64 outputs of one type: eight threads across, 32 rows of k at a time for the maxima, then 128 for
 // the codes.
-template <class E>
+template <class E, bool WHOLE>
 __global__ __launch_bounds__(256) void int8_weights_kernel(const E *W, int K, int N, int kp, uint8_t *codes, float *scales)
 {
     __shared__ __attribute__((aligned(16))) uint8_t turn[64 * 144];
@@ -77,15 +81,16 @@ __global__ __launch_bounds__(256) void int8_weights_kernel(const E *W, int K, in
     __shared__ float inverse[64];
     const int tid = threadIdx.x, across = (tid & 7) * 8, down = tid >> 3;
     const int64_t t = blockIdx.y;
-    const int n0 = blockIdx.x * 64, n = n0 + across, left = N - n;
-    const E *w = W + t * K * N + n;
+    const int n0 = blockIdx.x * 64, n = n0 + across;
+    const E *w = W + t * K * N;
     uint32_t top[8] = {};
 #pragma unroll 4
     for (int k = down; k < K; k += 32) {
-        Eight<E> x;
-        x.load(w + (int64_t)k * N, left);
+        Eight<E, WHOLE> x;
+        x.load(w + (int64_t)k * N, n, N);
+        x.settle(n, N);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top[i] = max(top[i], magnitude_bits((float)x.v[i]));
+        for (int i = 0; i < 8; ++i) top[i] = max(top[i], magnitude_bits(x.at(i)));
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) tops[down][across + i] = top[i];
@@ -102,14 +107,16 @@ __global__ __launch_bounds__(256) void int8_weights_kernel(const E *W, int K, in
 #pragma unroll
     for (int i = 0; i < 8; ++i) inv[i] = inverse[across + i];
     for (int k0 = 0; k0 < kp; k0 += 128) {
-        Eight<E> x[4];                    // four k side by side
+        Eight<E, WHOLE> x[4];                    // four k side by side
 #pragma unroll
-        for (int q = 0; q < 4; ++q) x[q].load(w + (int64_t)min(k0 + down * 4 + q, K - 1) * N, k0 + down * 4 + q < K ? left : 0);
+        for (int q = 0; q < 4; ++q) x[q].load(w + (int64_t)min(k0 + down * 4 + q, K - 1) * N, n, N);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) x[q].settle(n, N);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             uint32_t b[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) b[q] = inv[i] == 0.0f ? 0 : __float_as_uint(__builtin_fmaf((float)x[q].v[i], inv[i], 12582912.0f));
+            for (int q = 0; q < 4; ++q) b[q] = inv[i] == 0.0f || k0 + down * 4 + q >= K ? 0 : __float_as_uint(__builtin_fmaf(x[q].at(i), inv[i], 12582912.0f));
             *(uint32_t *)(turn + (across + i) * 144 + down * 4) = (b[0] & 0xFF) | (b[1] & 0xFF) << 8 | (b[2] & 0xFF) << 16 | b[3] << 24;
         }
         __syncthreads();
@@ -125,7 +132,9 @@ template <class E, int L, int NV>
 void launch_shape(const E *X, int64_t rows, int64_t ldx, int K, uint8_t *codes, float *scales, hipStream_t s)
 {
     constexpr int PER = L >= 256 ? 1 : 256 / L;
-    hipLaunchKernelGGL((int8_rows_kernel<E, L, NV>), flat_grid((rows + PER - 1) / PER), dim3(L > 256 ? L : 256), 0, s, X, rows, ldx, K, codes, scales);
+    const dim3 g = flat_grid((rows + PER - 1) / PER), b(L > 256 ? L : 256);
+    if (whole_vectors(K)) hipLaunchKernelGGL((int8_rows_kernel<E, true, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
+    else hipLaunchKernelGGL((int8_rows_kernel<E, false, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
 }
 
 template <class E>
@@ -147,8 +156,9 @@ void rows_of(const void *p, int64_t rows, int64_t ldx, int K, void *c, float *sc
 template <class E>
 void weights_of(const void *W, int T, int K, int N, void *codes, float *scales, hipStream_t s)
 {
-    hipLaunchKernelGGL((int8_weights_kernel<E>), dim3((uint32_t)((N + 63) / 64), (uint32_t)T), dim3(256), 0, s, (const E *)W, K, N, fp8_width(K),
-                       (uint8_t *)codes, scales);
+    const dim3 g((uint32_t)((N + 63) / 64), (uint32_t)T);
+    if (whole_vectors(N)) hipLaunchKernelGGL((int8_weights_kernel<E, true>), g, dim3(256), 0, s, (const E *)W, K, N, fp8_width(K), (uint8_t *)codes, scales);
+    else hipLaunchKernelGGL((int8_weights_kernel<E, false>), g, dim3(256), 0, s, (const E *)W, K, N, fp8_width(K), (uint8_t *)codes, scales);
 }
 
 }  // namespace

@@ -55,7 +55,7 @@ __device__ __forceinline__ float inverse_rms(double squares, int cols, double ep
 }
 
 // L threads hold a row, NV vectors of eight columns each.
-template <class H, bool X32, bool R32, int L, int NV>
+template <class H, bool X32, bool R32, bool WHOLE, int L, int NV>
 __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_kernel(NormArgs a)
 {
 #pragma clang fp contract(off)
@@ -68,36 +68,38 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_kernel(NormArgs a)
     if (row >= a.rows) return;                       // all lanes of a row
     const int lane = threadIdx.x % L;
 
-    Eight<XT> x[NV];
-    Eight<RT> in[NV];
+    Eight<XT, WHOLE> x[NV];
+    Eight<RT, WHOLE> in[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * L + lane) * 8;
-        x[v].load((const XT *)a.X + row * a.ldx + c, a.cols - c);
+        x[v].load((const XT *)a.X + row * a.ldx, c, a.cols);
     }
     if (a.res)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * L + lane) * 8;
-            in[v].load((const RT *)a.res + row * a.ldr + c, a.cols - c);
+            in[v].load((const RT *)a.res + row * a.ldr, c, a.cols);
         }
     Philox gen;
     if (a.drop.rng) gen.init(a.drop);
     float r[NV][8], w[NV][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight<H>(a.w, a.w32, (v * L + lane) * 8, a.cols - (v * L + lane) * 8, w[v]);
+    for (int v = 0; v < NV; ++v) load_weight<H, WHOLE>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
     double squares = 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * L + lane) * 8;
         float f[8], res[8];
+        x[v].settle(c, a.cols);
+        if (a.res) in[v].settle(c, a.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            f[i] = (float)x[v].v[i];
-            res[i] = a.res ? (float)in[v].v[i] : 0.0f;
+            f[i] = x[v].at(i);
+            res[i] = a.res ? in[v].at(i) : 0.0f;
         }
         sum8<RT>(a, gen, row, c, f, res, r[v]);
-        if (a.sum) store8<RT>(a.sum, row * a.lds + c, r[v], a.cols - c);
+        if (a.sum) store8<RT, WHOLE>(a.sum, row * a.lds, r[v], c, a.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)r[v][i], (double)r[v][i], squares);
     }
@@ -112,8 +114,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * L + lane) * 8;
-            if (a.out == kRowsF32) store8<float>(a.Y, row * a.ldy + c, r[v], a.cols - c);
-            else store8<H>(a.Y, row * a.ldy + c, r[v], a.cols - c);
+            if (a.out == kRowsF32) store8<float, WHOLE>(a.Y, row * a.ldy, r[v], c, a.cols);
+            else store8<H, WHOLE>(a.Y, row * a.ldy, r[v], c, a.cols);
         }
         return;
     }
@@ -171,29 +173,32 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     Philox gen;
     if (a.drop.rng) gen.init(a.drop);
     auto sum = [&](int c, float (&r)[8]) {
-        Eight<XT> x;
-        Eight<RT> in;
-        x.load((const XT *)a.X + row * a.ldx + c, a.cols - c);
-        if (a.res) in.load((const RT *)a.res + row * a.ldr + c, a.cols - c);
+        Eight<XT, false> x;
+        Eight<RT, false> in;
+        x.load((const XT *)a.X + row * a.ldx, c, a.cols);
+        if (a.res) in.load((const RT *)a.res + row * a.ldr, c, a.cols);
+        x.settle(c, a.cols);
+        if (a.res) in.settle(c, a.cols);
         float f[8], res[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            f[i] = (float)x.v[i];
-            res[i] = a.res ? (float)in.v[i] : 0.0f;
+            f[i] = x.at(i);
+            res[i] = a.res ? in.at(i) : 0.0f;
         }
         sum8<RT>(a, gen, row, c, f, res, r);
     };
     auto again = [&](int c, float s, float (&y)[8]) {       // the norm's output in fp32, zero behind the columns
         float w[8];
         if (a.sum) {
-            Eight<RT> in;
-            in.load((const RT *)a.sum + row * a.lds + c, a.cols - c);
+            Eight<RT, false> in;
+            in.load((const RT *)a.sum + row * a.lds, c, a.cols);
+            in.settle(c, a.cols);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = (float)in.v[i];
+            for (int i = 0; i < 8; ++i) y[i] = in.at(i);
         } else {
             sum(c, y);
         }
-        load_weight<H>(a.w, a.w32, c, a.cols - c, w);
+        load_weight<H, false>(a.w, a.w32, c, a.cols, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = c + i < a.cols ? y[i] * s * w[i] : 0.0f;
     };
@@ -201,7 +206,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
         float r[8];
         sum(c, r);
-        if (a.sum) store8<RT>(a.sum, row * a.lds + c, r, a.cols - c);
+        if (a.sum) store8<RT, false>(a.sum, row * a.lds, r, c, a.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)r[i], (double)r[i], squares);
     }
@@ -225,8 +230,8 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     for (int c = threadIdx.x * 8; c < kp; c += 8192) {
         float y[8];
         again(c, s, y);
-        if (a.out == kRowsHalf) store8<H>(a.Y, row * a.ldy + c, y, a.cols - c);
-        else if (a.out == kRowsF32) store8<float>(a.Y, row * a.ldy + c, y, a.cols - c);
+        if (a.out == kRowsHalf) store8<H, false>(a.Y, row * a.ldy, y, c, a.cols);
+        else if (a.out == kRowsF32) store8<float, false>(a.Y, row * a.ldy, y, c, a.cols);
         else if (a.out == kRowsInt8) store_int8(codes + c, y, inverse, scale != scale);
         else {      // kp is whole blocks: the 16 lanes of a block are here together
             uint32_t top = 0;
@@ -244,7 +249,9 @@ template <class H, bool X32, bool R32, int L, int NV>
 void launch_rows(const NormArgs &a, hipStream_t s)
 {
     constexpr int PER = L >= 256 ? 1 : 256 / L;
-    hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, L, NV>), flat_grid((a.rows + PER - 1) / PER), dim3(L > 256 ? L : 256), 0, s, a);
+    const dim3 g = flat_grid((a.rows + PER - 1) / PER), b(L > 256 ? L : 256);
+    if (whole_vectors(a.cols)) hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, true, L, NV>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, false, L, NV>), g, b, 0, s, a);
 }
 
 template <class H, bool X32, bool R32>

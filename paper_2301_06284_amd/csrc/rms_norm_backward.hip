@@ -13,7 +13,7 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kLong = 32768;         // columns that registers hold
+constexpr int kLong = 16384;         // columns that registers hold
 
 struct Shape {
     int lanes, vectors, per;         // threads of a row, vectors of a thread, rows of a workgroup
@@ -28,28 +28,27 @@ Shape shape_of(int cols)
     if (cols <= 2048) return {256, 1, 1};
     if (cols <= 4096) return {256, 2, 1};
     if (cols <= 8192) return {256, 4, 1};
-    if (cols <= 16384) return {1024, 2, 1};
-    if (cols <= kLong) return {1024, 4, 1};
+    if (cols <= kLong) return {512, 4, 1};
     return {1024, 0, 1};
 }
 int64_t groups_of(int64_t rows, int cols)
 {
     const Shape s = shape_of(cols);
-    return std::min<int64_t>((rows + s.per - 1) / s.per, s.lanes > 256 ? 256 : 1024);
+    return std::min<int64_t>((rows + s.per - 1) / s.per, s.lanes > 256 ? 512 : 1024);
 }
 
-template <class H>
-__device__ __forceinline__ void store_typed(void *base, bool f32, int64_t at, const float (&x)[8], int left)
+template <class H, bool WHOLE>
+__device__ __forceinline__ void store_typed(void *base, bool f32, int64_t row, const float (&x)[8], int c, int cols)
 {
-    if (f32) store8<float>(base, at, x, left);
-    else store8<H>(base, at, x, left);
+    if (f32) store8<float, WHOLE>(base, row, x, c, cols);
+    else store8<H, WHOLE>(base, row, x, c, cols);
 }
 
 // dX of eight columns from dr, and both stored.
-template <class H, class RT>
+template <class H, class RT, bool WHOLE>
 __device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const Philox &gen, int64_t row, int c, float (&dr)[8])
 {
-    if (a.dres) store8<RT>(a.dres, row * a.lddr + c, dr, a.cols - c);
+    if (a.dres) store8<RT, WHOLE>(a.dres, row * a.lddr, dr, c, a.cols);
     if (!a.dX) return;
     if (a.drop.rng) {
         uint32_t word[8];
@@ -57,10 +56,10 @@ __device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const
 #pragma unroll
         for (int i = 0; i < 8; ++i) dr[i] = word[i] > a.drop.below ? dr[i] * a.drop.factor : 0.0f;
     }
-    store_typed<H>(a.dX, a.dx32, row * a.lddx + c, dr, a.cols - c);
+    store_typed<H, WHOLE>(a.dX, a.dx32, row * a.lddx, dr, c, a.cols);
 }
 
-template <class H, bool DY32, bool R32, int L, int NV>
+template <class H, bool DY32, bool R32, bool WHOLE, int L, int NV>
 __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(NormBackwardArgs a)
 {
 #pragma clang fp contract(off)
@@ -74,51 +73,56 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
     if (a.drop.rng) gen.init(a.drop);
     float w[NV][8], dw[NV][8] = {};
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight<H>(a.w, a.w32, (v * L + lane) * 8, a.cols - (v * L + lane) * 8, w[v]);
+    for (int v = 0; v < NV; ++v) load_weight<H, WHOLE>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
     int turn = 0;
     for (int64_t row = blockIdx.x * (int64_t)PER + group; row < a.rows; row += gridDim.x * (int64_t)PER, turn ^= 1) {
-        Eight<YT> dy[NV];
-        Eight<RT> r[NV], ds[NV];
+        Eight<YT, WHOLE> dy[NV];
+        Eight<RT, WHOLE> r[NV], ds[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * L + lane) * 8;
-            dy[v].load((const YT *)a.dY + row * a.lddy + c, a.cols - c);
-            r[v].load((const RT *)a.r + row * a.ldr + c, a.cols - c);
+            dy[v].load((const YT *)a.dY + row * a.lddy, c, a.cols);
+            r[v].load((const RT *)a.r + row * a.ldr, c, a.cols);
         }
         if (a.dsum)
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int c = (v * L + lane) * 8;
-                ds[v].load((const RT *)a.dsum + row * a.ldds + c, a.cols - c);
+                ds[v].load((const RT *)a.dsum + row * a.ldds, c, a.cols);
             }
         const float s = a.rstd[row];
         double dot = 0;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * L + lane) * 8;
+            dy[v].settle(c, a.cols);
+            r[v].settle(c, a.cols);
+            if (a.dsum) ds[v].settle(c, a.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float d = (float)dy[v].v[i], n = (float)r[v].v[i] * s;
+                const float d = dy[v].at(i), n = r[v].at(i) * s;
                 dw[v][i] = __builtin_fmaf(d, n, dw[v][i]);
                 dot += (double)(d * w[v][i] * n);
             }
+        }
         const float mean = (float)(row_sum<L>(dot, sums[turn]) / a.cols);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             float dr[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float g = (float)dy[v].v[i] * w[v][i], n = (float)r[v].v[i] * s;
+                const float g = dy[v].at(i) * w[v][i], n = r[v].at(i) * s;
                 dr[i] = s * (g - n * mean);
-                if (a.dsum) dr[i] += (float)ds[v].v[i];
+                if (a.dsum) dr[i] += ds[v].at(i);
             }
-            store_gradients<H, RT>(a, gen, row, (v * L + lane) * 8, dr);
+            store_gradients<H, RT, WHOLE>(a, gen, row, (v * L + lane) * 8, dr);
         }
     }
     if (!a.dW) return;
     float *out = a.ws + blockIdx.x * (int64_t)a.cols;
     if constexpr (PER == 1) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) store8<float>(out, (v * L + lane) * 8, dw[v], a.cols - (v * L + lane) * 8);
+        for (int v = 0; v < NV; ++v) store8<float, WHOLE>(out, 0, dw[v], (v * L + lane) * 8, a.cols);
     } else {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -152,34 +156,41 @@ __global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwa
         const float s = a.rstd[row];
         double dot = 0;
         for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
-            Eight<YT> dy;
-            Eight<RT> r;
+            Eight<YT, false> dy;
+            Eight<RT, false> r;
             float w[8];
-            dy.load((const YT *)a.dY + row * a.lddy + c, a.cols - c);
-            r.load((const RT *)a.r + row * a.ldr + c, a.cols - c);
-            load_weight<H>(a.w, a.w32, c, a.cols - c, w);
+            dy.load((const YT *)a.dY + row * a.lddy, c, a.cols);
+            r.load((const RT *)a.r + row * a.ldr, c, a.cols);
+            dy.settle(c, a.cols);
+            r.settle(c, a.cols);
+            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
             for (int i = 0; i < 8 && c + i < a.cols; ++i) {
-                const float d = (float)dy.v[i], n = (float)r.v[i] * s;
+                const float d = dy.at(i), n = r.at(i) * s;
                 dot += (double)(d * w[i] * n);
                 if (out) out[c + i] = row == (int64_t)blockIdx.x ? d * n : __builtin_fmaf(d, n, out[c + i]);
             }
         }
         const float mean = (float)(row_sum<1024>(dot, sums[turn]) / a.cols);
         for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
-            Eight<YT> dy;
-            Eight<RT> r, ds;
+            Eight<YT, false> dy;
+            Eight<RT, false> r, ds;
             float w[8], dr[8];
-            dy.load((const YT *)a.dY + row * a.lddy + c, a.cols - c);
-            r.load((const RT *)a.r + row * a.ldr + c, a.cols - c);
-            if (a.dsum) ds.load((const RT *)a.dsum + row * a.ldds + c, a.cols - c);
-            load_weight<H>(a.w, a.w32, c, a.cols - c, w);
+            dy.load((const YT *)a.dY + row * a.lddy, c, a.cols);
+            r.load((const RT *)a.r + row * a.ldr, c, a.cols);
+            dy.settle(c, a.cols);
+            r.settle(c, a.cols);
+            if (a.dsum) {
+                ds.load((const RT *)a.dsum + row * a.ldds, c, a.cols);
+                ds.settle(c, a.cols);
+            }
+            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float g = (float)dy.v[i] * w[i], n = (float)r.v[i] * s;
+                const float g = dy.at(i) * w[i], n = r.at(i) * s;
                 dr[i] = s * (g - n * mean);
-                if (a.dsum) dr[i] += (float)ds.v[i];
+                if (a.dsum) dr[i] += ds.at(i);
             }
-            store_gradients<H, RT>(a, gen, row, c, dr);
+            store_gradients<H, RT, false>(a, gen, row, c, dr);
         }
     }
 }
@@ -206,7 +217,9 @@ __global__ __launch_bounds__(1024) void rms_norm_join_kernel(const float *ws, in
 template <class H, bool DY32, bool R32, int L, int NV>
 void launch_shape(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
 {
-    hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, L, NV>), dim3((uint32_t)groups), dim3(L > 256 ? L : 256), 0, s, a);
+    const dim3 g((uint32_t)groups), b(L > 256 ? L : 256);
+    if (whole_vectors(a.cols)) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, true, L, NV>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, false, L, NV>), g, b, 0, s, a);
 }
 
 template <class H, bool DY32, bool R32>
@@ -220,8 +233,7 @@ void launch_types(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
     else if (a.cols <= 2048) launch_shape<H, DY32, R32, 256, 1>(a, groups, s);
     else if (a.cols <= 4096) launch_shape<H, DY32, R32, 256, 2>(a, groups, s);
     else if (a.cols <= 8192) launch_shape<H, DY32, R32, 256, 4>(a, groups, s);
-    else if (a.cols <= 16384) launch_shape<H, DY32, R32, 1024, 2>(a, groups, s);
-    else if (a.cols <= kLong) launch_shape<H, DY32, R32, 1024, 4>(a, groups, s);
+    else if (a.cols <= kLong) launch_shape<H, DY32, R32, 512, 4>(a, groups, s);
     else hipLaunchKernelGGL((rms_norm_backward_long_kernel<H, DY32, R32>), dim3((uint32_t)groups), dim3(1024), 0, s, a);
 }
 

@@ -73,58 +73,130 @@ rgnn_status launch_dropout(const DropoutArgs &a, hipStream_t s);
 
 // ---------------------------------------------------------------- eight columns
 
-// Eight values side by side, or the first `left` of them and zeros, from any address of an element: a vector
-// load takes any address, at full speed where it is a multiple of its size.
-template <class E>
+inline bool whole_vectors(int cols) { return cols % 8 == 0; }
+
+// Eight values of a row from column c on, those behind its `cols` columns zero, from any address of an element: a
+// vector load takes any address, at full speed where it is a multiple of its size.  load() only asks for them,
+// so that many loads are under way together; settle() comes before their use.  A vector that
+// the row does not fill is read as the row's last eight and moved down.  WHOLE: a row is whole vectors, and only
+// those behind its end are to be cleared.
+template <class E, bool WHOLE>
 struct Eight {
-    E v[8];
-    __device__ __forceinline__ void load(const E *p, int left)
+    static constexpr int words = sizeof(E) * 2;
+    uint32_t raw[words];
+    __device__ __forceinline__ void load(const E *row, int c, int cols)
     {
-        if (left >= 8) {
-            __builtin_memcpy(v, p, sizeof(v));
+        if (WHOLE || cols >= 8) {
+            __builtin_memcpy(raw, row + min(c, cols - 8), sizeof(raw));
             return;
         }
+        E e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (E)0.0f;
+        for (int i = 0; i < 8; ++i) e[i] = row[min(i, cols - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? e[i] : (E)0.0f;
+        __builtin_memcpy(raw, e, sizeof(raw));
     }
-    __device__ __forceinline__ void store(E *p, int left) const
+    __device__ __forceinline__ void settle(int c, int cols)
     {
-        if (left >= 8) {
-            __builtin_memcpy(p, v, sizeof(v));
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int i = 0; i < words; ++i) raw[i] = c < cols ? raw[i] : 0;
             return;
         }
+        const int by = c + 8 - cols;
+        if (by <= 0 || cols < 8) return;
+        if constexpr (sizeof(E) == 2) {
+            uint64_t lo = (uint64_t)raw[1] << 32 | raw[0], hi = (uint64_t)raw[3] << 32 | raw[2];
+            const int bits = (by & 3) * 16;
+            if (by & 4) { lo = hi; hi = 0; }
+            if (bits) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+            if (by >= 8) lo = hi = 0;
+            raw[0] = (uint32_t)lo; raw[1] = (uint32_t)(lo >> 32);
+            raw[2] = (uint32_t)hi; raw[3] = (uint32_t)(hi >> 32);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < left) p[i] = v[i];
+            for (int step = 1; step < 8; step *= 2)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[i] = by & step ? (i + step < 8 ? raw[i + step] : 0) : raw[i];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) raw[i] = by >= 8 ? 0 : raw[i];
+        }
+    }
+    __device__ __forceinline__ float at(int i) const
+    {
+        if constexpr (sizeof(E) == 4) return __uint_as_float(raw[i]);
+        else if constexpr (std::is_same<E, __bf16>::value) return __uint_as_float(i & 1 ? raw[i >> 1] & 0xFFFF0000u : raw[i >> 1] << 16);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)(raw[i >> 1] >> (i & 1) * 16));
     }
 };
 
-template <class E>
-__device__ __forceinline__ void store8(void *base, int64_t at, const float (&x)[8], int left)
+// Eight results to a row from column c on, those that it has: the last ones in pieces of four, two and one, by whole
+// words (selected as elements, they would go through memory).
+template <class E, bool WHOLE>
+__device__ __forceinline__ void store8(void *base, int64_t row, const float (&x)[8], int c, int cols)
 {
-    Eight<E> o;
+    typedef E vec __attribute__((ext_vector_type(8)));
+    vec v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.v[i] = (E)x[i];
-    o.store((E *)base + at, left);
+    for (int i = 0; i < 8; ++i) v[i] = (E)x[i];
+    E *p = (E *)base + row + c;
+    const int left = cols - c;
+    if (left >= 8) {
+        __builtin_memcpy(p, &v, sizeof(v));
+    } else if (!WHOLE && left > 0) {
+        if constexpr (sizeof(E) == 2) {
+            i32x4 w = __builtin_bit_cast(i32x4, v);
+            if (left & 4) {
+                const int2 q = make_int2(w[0], w[1]);
+                __builtin_memcpy(p, &q, 8);
+                p += 4;
+            }
+            const int w0 = left & 4 ? w[2] : w[0], w1 = left & 4 ? w[3] : w[1];
+            if (left & 2) {
+                __builtin_memcpy(p, &w0, 4);
+                p += 2;
+            }
+            const uint16_t last = (uint16_t)(left & 2 ? w1 : w0);
+            if (left & 1) __builtin_memcpy(p, &last, 2);
+        } else {
+            i32x8 w = __builtin_bit_cast(i32x8, v);
+            if (left & 4) {
+                const i32x4 q = {w[0], w[1], w[2], w[3]};
+                __builtin_memcpy(p, &q, 16);
+                p += 4;
+            }
+            const int w0 = left & 4 ? w[4] : w[0], w1 = left & 4 ? w[5] : w[1], w2 = left & 4 ? w[6] : w[2];
+            if (left & 2) {
+                const int2 q = make_int2(w0, w1);
+                __builtin_memcpy(p, &q, 8);
+                p += 2;
+            }
+            const int last = left & 2 ? w2 : w0;
+            if (left & 1) __builtin_memcpy(p, &last, 4);
+        }
+    }
 }
 
 // Eight weights as fp32, in either type.
-template <class H>
-__device__ __forceinline__ void load_weight(const void *w, bool w32, int at, int left, float (&out)[8])
+template <class H, bool WHOLE>
+__device__ __forceinline__ void load_weight(const void *w, bool w32, int c, int cols, float (&out)[8])
 {
     if (!w) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) out[i] = 1.0f;
     } else if (w32) {
-        Eight<float> e;
-        e.load((const float *)w + at, left);
+        Eight<float, WHOLE> e;
+        e.load((const float *)w, c, cols);
+        e.settle(c, cols);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = e.v[i];
+        for (int i = 0; i < 8; ++i) out[i] = e.at(i);
     } else {
-        Eight<H> e;
-        e.load((const H *)w + at, left);
+        Eight<H, WHOLE> e;
+        e.load((const H *)w, c, cols);
+        e.settle(c, cols);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) out[i] = (float)e.v[i];
+        for (int i = 0; i < 8; ++i) out[i] = e.at(i);
     }
 }
 
