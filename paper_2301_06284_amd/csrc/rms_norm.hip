@@ -261,7 +261,7 @@ void launch_types(const NormArgs &a, hipStream_t s)
     if (cols <= 64) launch_rows<H, X32, R32, 8, 1>(a, s);
     else if (cols <= 128) launch_rows<H, X32, R32, 16, 1>(a, s);
     else if (cols <= 256) launch_rows<H, X32, R32, 32, 1>(a, s);
-    else if (cols <= 512) launch_rows<H, X32, R32, 64, 1>(a, s);
+    else if (cols <= 512) launch_rows<H, X32, R32, 32, 2>(a, s);
     else if (cols <= 1024) launch_rows<H, X32, R32, 64, 2>(a, s);
     else if (cols <= 2048) launch_rows<H, X32, R32, 256, 1>(a, s);
     else if (cols <= 4096) launch_rows<H, X32, R32, 256, 2>(a, s);

@@ -13,28 +13,14 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kLong = 16384;         // columns that registers hold
+constexpr int kLong = 32768;         // columns whose dw LDS holds
 
-struct Shape {
-    int lanes, vectors, per;         // threads of a row, vectors of a thread, rows of a workgroup
-};
-Shape shape_of(int cols)
-{
-    if (cols <= 64) return {8, 1, 32};
-    if (cols <= 128) return {16, 1, 16};
-    if (cols <= 256) return {32, 1, 8};
-    if (cols <= 512) return {64, 1, 4};
-    if (cols <= 1024) return {64, 2, 4};
-    if (cols <= 2048) return {256, 1, 1};
-    if (cols <= 4096) return {256, 2, 1};
-    if (cols <= 8192) return {256, 4, 1};
-    if (cols <= kLong) return {512, 4, 1};
-    return {1024, 0, 1};
-}
+// Rows of a workgroup: several short ones, of 8 to 64 lanes each.
+int rows_of_group(int cols) { return cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
 int64_t groups_of(int64_t rows, int cols)
 {
-    const Shape s = shape_of(cols);
-    return std::min<int64_t>((rows + s.per - 1) / s.per, s.lanes > 256 ? 512 : 1024);
+    const int per = rows_of_group(cols);
+    return std::min<int64_t>((rows + per - 1) / per, cols <= 2048 ? 1024 : cols <= 4096 ? 512 : 256);
 }
 
 template <class H, bool WHOLE>
@@ -45,12 +31,12 @@ __device__ __forceinline__ void store_typed(void *base, bool f32, int64_t row, c
 }
 
 // dX of eight columns from dr, and both stored.
-template <class H, class RT, bool WHOLE>
+template <class H, class RT, bool WHOLE, bool DROP>
 __device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const Philox &gen, int64_t row, int c, float (&dr)[8])
 {
     if (a.dres) store8<RT, WHOLE>(a.dres, row * a.lddr, dr, c, a.cols);
     if (!a.dX) return;
-    if (a.drop.rng) {
+    if constexpr (DROP) {
         uint32_t word[8];
         gen.eight(c, row, word);
 #pragma unroll
@@ -59,7 +45,7 @@ __device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const
     store_typed<H, WHOLE>(a.dX, a.dx32, row * a.lddx, dr, c, a.cols);
 }
 
-template <class H, bool DY32, bool R32, bool WHOLE, int L, int NV>
+template <class H, bool DY32, bool R32, bool WHOLE, bool DROP, int L, int NV>
 __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(NormBackwardArgs a)
 {
 #pragma clang fp contract(off)
@@ -70,7 +56,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
     __shared__ float part[PER > 1 ? 256 * NV * 8 : 1];
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     Philox gen;
-    if (a.drop.rng) gen.init(a.drop);
+    if (DROP) gen.init(a.drop);
     float w[NV][8], dw[NV][8] = {};
 #pragma unroll
     for (int v = 0; v < NV; ++v) load_weight<H, WHOLE>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
@@ -86,10 +72,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
         }
         if (a.dsum)
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = (v * L + lane) * 8;
-                ds[v].load((const RT *)a.dsum + row * a.ldds, c, a.cols);
-            }
+            for (int v = 0; v < NV; ++v) ds[v].load((const RT *)a.dsum + row * a.ldds, (v * L + lane) * 8, a.cols);
         const float s = a.rstd[row];
         double dot = 0;
 #pragma unroll
@@ -97,17 +80,25 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
             const int c = (v * L + lane) * 8;
             dy[v].settle(c, a.cols);
             r[v].settle(c, a.cols);
-            if (a.dsum) ds[v].settle(c, a.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = dy[v].at(i), n = r[v].at(i) * s;
                 dw[v][i] = __builtin_fmaf(d, n, dw[v][i]);
                 dot += (double)(d * w[v][i] * n);
             }
+            // Where registers are short, the words are kept as they came over the sum (16 bits: 8 registers in place
+            // of 24), and dw is done with them (2000 rows of 16 000, bf16: 71 us, 131 from LDS and L2).
+            if constexpr (L * NV > 1024) {
+                opaque(dw[v]);
+                opaque(dy[v].raw);
+                opaque(r[v].raw);
+            }
         }
         const float mean = (float)(row_sum<L>(dot, sums[turn]) / a.cols);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
+            const int c = (v * L + lane) * 8;
+            if (a.dsum) ds[v].settle(c, a.cols);
             float dr[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -115,7 +106,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
                 dr[i] = s * (g - n * mean);
                 if (a.dsum) dr[i] += ds[v].at(i);
             }
-            store_gradients<H, RT, WHOLE>(a, gen, row, (v * L + lane) * 8, dr);
+            store_gradients<H, RT, WHOLE, DROP>(a, gen, row, c, dr);
         }
     }
     if (!a.dW) return;
@@ -139,35 +130,51 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
     }
 }
 
-// Rows that registers do not hold: a workgroup of 1024 goes over each of its rows twice and keeps its dw in
-// the workspace, each thread its own columns.
-template <class H, bool DY32, bool R32>
+// Rows that registers do not hold: a workgroup of 1024 goes over each of its rows twice (again from L2) and keeps its
+// dw in LDS, or beyond that in the workspace, each thread its own columns.
+template <class H, bool DY32, bool R32, bool DROP, bool IN_LDS>
 __global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwardArgs a)
 {
 #pragma clang fp contract(off)
     typedef typename std::conditional<DY32, float, H>::type YT;
     typedef typename std::conditional<R32, float, H>::type RT;
     __shared__ double sums[2][16];
+    __shared__ __attribute__((aligned(16))) float held[IN_LDS ? kLong : 4];
     Philox gen;
-    if (a.drop.rng) gen.init(a.drop);
+    if (DROP) gen.init(a.drop);
     float *out = a.dW ? a.ws + blockIdx.x * (int64_t)a.cols : nullptr;
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const bool first = row == (int64_t)blockIdx.x, last = row + gridDim.x >= a.rows;
         const float s = a.rstd[row];
         double dot = 0;
         for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
             Eight<YT, false> dy;
             Eight<RT, false> r;
-            float w[8];
+            float w[8], dw[8];
             dy.load((const YT *)a.dY + row * a.lddy, c, a.cols);
             r.load((const RT *)a.r + row * a.ldr, c, a.cols);
+            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
             dy.settle(c, a.cols);
             r.settle(c, a.cols);
-            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
-            for (int i = 0; i < 8 && c + i < a.cols; ++i) {
+            if (IN_LDS) {
+                *(f32x4 *)dw = *(const f32x4 *)(held + c);
+                *(f32x4 *)(dw + 4) = *(const f32x4 *)(held + c + 4);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dw[i] = out && !first && c + i < a.cols ? out[c + i] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
                 const float d = dy.at(i), n = r.at(i) * s;
                 dot += (double)(d * w[i] * n);
-                if (out) out[c + i] = row == (int64_t)blockIdx.x ? d * n : __builtin_fmaf(d, n, out[c + i]);
+                dw[i] = __builtin_fmaf(d, n, first ? 0.0f : dw[i]);
+            }
+            if (IN_LDS && !last) {
+                *(f32x4 *)(held + c) = *(const f32x4 *)dw;
+                *(f32x4 *)(held + c + 4) = *(const f32x4 *)(dw + 4);
+            } else if (out) {
+                store8<float, false>(out, 0, dw, c, a.cols);
             }
         }
         const float mean = (float)(row_sum<1024>(dot, sums[turn]) / a.cols);
@@ -177,20 +184,18 @@ __global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwa
             float w[8], dr[8];
             dy.load((const YT *)a.dY + row * a.lddy, c, a.cols);
             r.load((const RT *)a.r + row * a.ldr, c, a.cols);
+            if (a.dsum) ds.load((const RT *)a.dsum + row * a.ldds, c, a.cols);
+            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
             dy.settle(c, a.cols);
             r.settle(c, a.cols);
-            if (a.dsum) {
-                ds.load((const RT *)a.dsum + row * a.ldds, c, a.cols);
-                ds.settle(c, a.cols);
-            }
-            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
+            if (a.dsum) ds.settle(c, a.cols);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float g = dy.at(i) * w[i], n = r.at(i) * s;
                 dr[i] = s * (g - n * mean);
                 if (a.dsum) dr[i] += ds.at(i);
             }
-            store_gradients<H, RT, false>(a, gen, row, c, dr);
+            store_gradients<H, RT, false, DROP>(a, gen, row, c, dr);
         }
     }
 }
@@ -214,27 +219,34 @@ __global__ __launch_bounds__(1024) void rms_norm_join_kernel(const float *ws, in
     else ((H *)dW)[c] = (H)(float)x;
 }
 
-template <class H, bool DY32, bool R32, int L, int NV>
+template <class H, bool DY32, bool R32, bool DROP, int L, int NV>
 void launch_shape(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
 {
     const dim3 g((uint32_t)groups), b(L > 256 ? L : 256);
-    if (whole_vectors(a.cols)) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, true, L, NV>), g, b, 0, s, a);
-    else hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, false, L, NV>), g, b, 0, s, a);
+    if (whole_vectors(a.cols)) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, true, DROP, L, NV>), g, b, 0, s, a);
+    else hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, false, DROP, L, NV>), g, b, 0, s, a);
+}
+
+template <class H, bool DY32, bool R32, bool DROP>
+void launch_cols(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
+{
+    if (a.cols <= 64) launch_shape<H, DY32, R32, DROP, 8, 1>(a, groups, s);
+    else if (a.cols <= 128) launch_shape<H, DY32, R32, DROP, 16, 1>(a, groups, s);
+    else if (a.cols <= 256) launch_shape<H, DY32, R32, DROP, 32, 1>(a, groups, s);
+    else if (a.cols <= 512) launch_shape<H, DY32, R32, DROP, 64, 1>(a, groups, s);
+    else if (a.cols <= 1024) launch_shape<H, DY32, R32, DROP, 64, 2>(a, groups, s);
+    else if (a.cols <= 2048) launch_shape<H, DY32, R32, DROP, 256, 1>(a, groups, s);
+    else if (a.cols <= 4096) launch_shape<H, DY32, R32, DROP, 512, 1>(a, groups, s);
+    else if (a.cols <= 8192) launch_shape<H, DY32, R32, DROP, 1024, 1>(a, groups, s);
+    else if (a.cols <= 16384) launch_shape<H, DY32, R32, DROP, 1024, 2>(a, groups, s);
+    else if (a.cols <= kLong) hipLaunchKernelGGL((rms_norm_backward_long_kernel<H, DY32, R32, DROP, true>), dim3((uint32_t)groups), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((rms_norm_backward_long_kernel<H, DY32, R32, DROP, false>), dim3((uint32_t)groups), dim3(1024), 0, s, a);
 }
 
 template <class H, bool DY32, bool R32>
 void launch_types(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
 {
-    if (a.cols <= 64) launch_shape<H, DY32, R32, 8, 1>(a, groups, s);
-    else if (a.cols <= 128) launch_shape<H, DY32, R32, 16, 1>(a, groups, s);
-    else if (a.cols <= 256) launch_shape<H, DY32, R32, 32, 1>(a, groups, s);
-    else if (a.cols <= 512) launch_shape<H, DY32, R32, 64, 1>(a, groups, s);
-    else if (a.cols <= 1024) launch_shape<H, DY32, R32, 64, 2>(a, groups, s);
-    else if (a.cols <= 2048) launch_shape<H, DY32, R32, 256, 1>(a, groups, s);
-    else if (a.cols <= 4096) launch_shape<H, DY32, R32, 256, 2>(a, groups, s);
-    else if (a.cols <= 8192) launch_shape<H, DY32, R32, 256, 4>(a, groups, s);
-    else if (a.cols <= kLong) launch_shape<H, DY32, R32, 512, 4>(a, groups, s);
-    else hipLaunchKernelGGL((rms_norm_backward_long_kernel<H, DY32, R32>), dim3((uint32_t)groups), dim3(1024), 0, s, a);
+    a.drop.rng ? launch_cols<H, DY32, R32, true>(a, groups, s) : launch_cols<H, DY32, R32, false>(a, groups, s);
 }
 
 template <class H>

@@ -75,6 +75,14 @@ rgnn_status launch_dropout(const DropoutArgs &a, hipStream_t s);
 
 inline bool whole_vectors(int cols) { return cols % 8 == 0; }
 
+// The compiler takes these values as new: it keeps them and nothing that it made of them before.
+template <class T, int N>
+__device__ __forceinline__ void opaque(T (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
 // Eight values of a row from column c on, those behind its `cols` columns zero, from any address of an element: a
 // vector load takes any address, at full speed where it is a multiple of its size.  load() only asks for them,
 // so that many loads are under way together; settle() comes before their use.  A vector that
