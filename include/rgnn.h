@@ -508,44 +508,65 @@ rgnn_status rgnn_typed_linear_int8(const void *X, const float *x_scales, int64_t
  *   rng: DEVICE int64 [2], seed and offset, read when the kernels run, so that a captured graph draws anew
  *   when the program has moved the offset on.  call: the number of the call within a step, so that two
  *   dropouts of a step are apart while rng stays as it is; the backward pass takes the forward's rng and call.
- *   0 <= p <= 1; p = 1 drops all. */
+ *   0 <= p <= 1; p = 1 drops all.  In the calls below rng NULL means that nothing is dropped, D(x) = x. */
 typedef struct {
     const int64_t *rng;
     int64_t call;
     double p;
 } rgnn_dropout_t;
 
-/* Y = [residual +] D(X), the kept product and the sum rounded once; residual: of Y's type, or NULL.  With the output's gradient as X and
- * no residual the call is the gradient of x; that of the residual is the output's. */
-rgnn_status rgnn_dropout(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t cols,
-                         const rgnn_dropout_t *dropout, int32_t y_dtype, const void *residual, int64_t ldr,
-                         void *Y, int64_t ldy, void *stream);
+/* Y = [residual +] D(X), the kept product and the sum rounded once.  With the output's gradient as X and no residual the call
+ * is the gradient of x; that of the residual is the output's. */
+typedef struct {
+    const void *X;             /* [rows, cols] of dtype                       */
+    const void *residual;      /* [rows, cols] of y_dtype, or NULL            */
+    void *Y;                   /* [rows, cols] of y_dtype                     */
+    int64_t rows, ldx, ldr, ldy;
+    rgnn_dropout_t dropout;
+    int32_t cols, dtype, y_dtype;
+} rgnn_dropout_rows_t;
+rgnn_status rgnn_dropout(const rgnn_dropout_rows_t *args, void *stream);
 
 /* r = [residual +] D(X), rounded to sum_dtype; s = 1 / sqrt(mean(r^2) + eps); Y = (r s) weight.
- *   dropout: NULL for D(x) = x.  residual: [rows, cols] of sum_dtype, or NULL.  sum: where r is kept, or NULL.
- *   weight: [cols], or NULL for ones.  rstd: fp32 [rows], takes s, or NULL.  r (X itself without residual and dropout) and
- *   rstd are what the backward call needs.
+ *   r (X itself without residual and dropout, where sum_dtype is X's) and rstd are what the backward call needs.
  *   y_dtype: fp32 or 16-bit, scales then unused; or RGNN_F8_E4M3: Y codes [rows, Kp] and scales uint8 [rows, Ks] as
  *   rgnn_fp8_quantize_rows makes them of y in fp32; or RGNN_I8: Y codes [rows, Kp] and scales fp32 [rows] as
  *   rgnn_int8_quantize_rows does (codes on a 16-byte address, scales on a 4-byte one; ldy unused).
  * A NaN or an infinity in a row spoils that row alone; a row of zeros gives zeros where eps > 0. */
-rgnn_status rgnn_rms_norm(int32_t dtype, const void *X, int64_t rows, int64_t ldx, int32_t cols,
-                          const rgnn_dropout_t *dropout, int32_t sum_dtype, const void *residual, int64_t ldr,
-                          void *sum, int64_t lds, int32_t w_dtype, const void *weight, double eps,
-                          int32_t y_dtype, void *Y, int64_t ldy, void *scales, float *rstd, void *stream);
+typedef struct {
+    const void *X;             /* [rows, cols] of dtype                       */
+    const void *residual;      /* [rows, cols] of sum_dtype, or NULL          */
+    void *sum;                 /* takes r, [rows, cols] of sum_dtype, or NULL */
+    const void *weight;        /* [cols] of w_dtype, or NULL for ones         */
+    void *Y, *scales;
+    float *rstd;               /* takes s, [rows], or NULL                    */
+    int64_t rows, ldx, ldr, lds, ldy;
+    double eps;
+    rgnn_dropout_t dropout;
+    int32_t cols, dtype, sum_dtype, w_dtype, y_dtype;
+} rgnn_rms_norm_t;
+rgnn_status rgnn_rms_norm(const rgnn_rms_norm_t *args, void *stream);
 
 /* Its gradients: with n = r s, g = dY weight:
  *   dr = s (g - n mean(g n)) + d_sum;  d_residual = dr;  dX = D'(dr) (kept values times the factor);
  *   dW = sum over the rows of dY n  (zero without rows).
- *   sum, rstd: the forward's r and s.  d_sum: the gradient that reaches r by other ways, of sum_dtype, or NULL.
- *   d_residual (of sum_dtype), dX, dW [cols]: each may be NULL.  ws: needed with dW.
- *   d_residual may be d_sum, and dX dY, with the same address, type and leading dimension. */
-rgnn_status rgnn_rms_norm_backward(int32_t dy_dtype, const void *dY, int64_t rows, int64_t lddy, int32_t cols,
-                                   int32_t sum_dtype, const void *sum, int64_t lds, const float *rstd,
-                                   int32_t w_dtype, const void *weight, const void *d_sum, int64_t ldds,
-                                   const rgnn_dropout_t *dropout, void *d_residual, int64_t lddr,
-                                   int32_t dx_dtype, void *dX, int64_t lddx, int32_t dw_dtype, void *dW,
-                                   void *ws, size_t ws_bytes, void *stream);
+ *   d_residual may be d_sum, and dX dY, with the same address, type and leading dimension.  ws: needed with dW. */
+typedef struct {
+    const void *dY;            /* [rows, cols] of dy_dtype                    */
+    const void *sum;           /* the forward's r, of sum_dtype               */
+    const float *rstd;         /* the forward's s, [rows]                     */
+    const void *weight;        /* [cols] of w_dtype, or NULL for ones         */
+    const void *d_sum;         /* the gradient that reaches r by other ways, of sum_dtype, or NULL */
+    void *d_residual;          /* of sum_dtype, or NULL                       */
+    void *dX;                  /* of dx_dtype, or NULL                        */
+    void *dW;                  /* [cols] of dw_dtype, or NULL                 */
+    void *ws;
+    int64_t rows, lddy, lds, ldds, lddr, lddx;
+    size_t ws_bytes;
+    rgnn_dropout_t dropout;
+    int32_t cols, dy_dtype, sum_dtype, w_dtype, dx_dtype, dw_dtype;
+} rgnn_rms_norm_backward_t;
+rgnn_status rgnn_rms_norm_backward(const rgnn_rms_norm_backward_t *args, void *stream);
 /* Grows with the rows, so that a workspace for the most rows serves fewer of the same columns. */
 rgnn_status rgnn_rms_norm_backward_workspace_size(int64_t rows, int32_t cols, size_t *bytes);
 

@@ -67,8 +67,12 @@ class Tile(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("rows", "cols", "stages", "any")]
 
 
-class DropoutArgs(ctypes.Structure):
-    _fields_ = [("rng", ctypes.c_void_p), ("call", ctypes.c_int64), ("p", ctypes.c_double)]
+# The arguments of dropout, rms_norm and rms_norm_backward as the header lays them out, packed at once: a call
+# with one pointer costs the host a microsecond less than one with twenty arguments.
+_DROPOUT_PACK = struct.Struct("3Q4QQqd3i4x").pack
+_NORM_PACK = struct.Struct("7Q5QdQqd5i4x").pack
+_NORM_BACKWARD_PACK = struct.Struct("9Q6QQQqd6i").pack
+_NO_DROPOUT = (0, 0, 0.0)
 
 
 class AdamwTensor(ctypes.Structure):
@@ -123,11 +127,9 @@ def _load():
         "rgnn_int8_quantize_rows": [i32, vp, i64, i64, i32, vp, vp, vp],
         "rgnn_int8_quantize_weights": [i32, vp, i32, i32, i32, vp, vp, vp],
         "rgnn_typed_linear_int8": [vp, vp, i64, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, i64, i64, vp, vp],
-        "rgnn_dropout": [i32, vp, i64, i64, i32, P(DropoutArgs), i32, vp, i64, vp, i64, vp],
-        "rgnn_rms_norm": [i32, vp, i64, i64, i32, P(DropoutArgs), i32, vp, i64, vp, i64, i32, vp, ctypes.c_double, i32, vp,
-                          i64, vp, vp, vp],
-        "rgnn_rms_norm_backward": [i32, vp, i64, i64, i32, i32, vp, i64, vp, i32, vp, vp, i64, P(DropoutArgs), vp, i64, i32,
-                                   vp, i64, i32, vp, vp, sz, vp],
+        "rgnn_dropout": [ctypes.c_char_p, vp],
+        "rgnn_rms_norm": [ctypes.c_char_p, vp],
+        "rgnn_rms_norm_backward": [ctypes.c_char_p, vp],
         "rgnn_rms_norm_backward_workspace_size": [i64, i32, P(sz)],
         "rgnn_adamw_step": [P(AdamwTensor), i32, P(AdamwHyper), i64, vp, vp, vp],
         "rgnn_profile_enable": [i32],
@@ -595,70 +597,128 @@ def typed_linear_fp8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatter
                                       _stream_on(stream, d)))
 
 
+class _Torch:
+    """What these calls take from torch, looked up once."""
+
+    def __init__(self):
+        import torch
+        self.current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.empty, self.int8, self.float32, self.uint8, self.e4m3 = torch.empty, torch.int8, torch.float32, torch.uint8, torch.float8_e4m3fn
+
+        class Floats(dict):
+            def __missing__(self, dtype):
+                raise ValueError(f"tensors must be fp32, bf16 or fp16, not {dtype}")
+        self.floats = Floats(_dtype_codes())
+
+
+_torch_cache: list = []
+
+
+def _torch() -> _Torch:
+    if not _torch_cache:
+        _torch_cache.append(_Torch())
+    return _torch_cache[0]
+
+
+def _device_of(X, t: _Torch) -> int:
+    """The device of a call, which is that of X and the current one."""
+    d = X.get_device()
+    if d < 0:
+        raise ValueError("tensors must be on a GPU")
+    if d != t.current():
+        raise ValueError(f"tensors are on device {d}, the current one is {t.current()}")
+    return d
+
+
+def _stream_of(stream, device: int, t: _Torch):
+    """The stream's handle; None: the device's current stream."""
+    return t.raw_stream(device) if stream is None and t.raw_stream is not None else _stream_on(stream, device)
+
+
+def _rows(t, name: str, shape, device: int):
+    """(pointer, leading dimension) of a matrix of that shape and device."""
+    if t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{name} must be {tuple(shape)}, on device {device}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    p, _, ld = _matrix(t, name, shape[1])
+    return p, ld
+
+
+def _flat(t, name: str, shape, device: int, dtype=None) -> int:
+    """Pointer of a contiguous tensor of that shape, type and device."""
+    if t.shape != shape or t.get_device() != device or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be contiguous {tuple(shape)}" + (f" of {dtype}" if dtype is not None else "") +
+                         f", on device {device}")
+    return t.data_ptr()
+
+
 def _int8_out(codes, scales, lead, K, device, stream):
     """The outputs, those that are not given in memory of the stream that writes them."""
-    import torch
-    if stream is not None and (codes is None or scales is None):
+    if codes is not None and scales is not None:
+        return codes, scales
+    if stream is not None:
         return _on_stream(stream, device, lambda: _int8_out(codes, scales, lead, K, device, None))
+    t = _torch()
     if codes is None:
-        codes = torch.empty(*lead, fp8_widths(K)[0], dtype=torch.int8, device=device)
+        codes = t.empty((*lead, -(-K // 128) * 128), dtype=t.int8, device=device)
     if scales is None:
-        scales = torch.empty(lead, dtype=torch.float32, device=device)
-    _int8_check(codes, scales, lead, K)
+        scales = t.empty(lead, dtype=t.float32, device=device)
     return codes, scales
-
-
-def _int8_check(codes, scales, lead, K):
-    import torch
-    Kp = fp8_widths(K)[0]
-    if codes.dtype != torch.int8 or codes.shape != (*lead, Kp) or not codes.is_contiguous():
-        raise ValueError(f"codes must be contiguous int8 {(*lead, Kp)}")
-    if scales.dtype != torch.float32 or scales.shape != lead or not scales.is_contiguous():
-        raise ValueError(f"scales must be contiguous float32 {lead}")
 
 
 def int8_quantize_rows(X, codes=None, scales=None, stream=None):
     """X [rows, K] -> (codes int8 [rows, Kp], scales float32 [rows]), a scale for each row.  Outputs that
     are not given are made in the memory of `stream`: to use them on another one, wait for it there."""
+    t = _torch()
+    d = _device_of(X, t)
     if X.dim() != 2:
         raise ValueError("X must be a matrix")
-    K = X.shape[1]
-    xp, rows, ldx = _matrix(X, "X", K)
+    rows, K = shape = X.shape
+    xp, ldx = _rows(X, "X", shape, d)
+    made = codes is None, scales is None
     codes, scales = _int8_out(codes, scales, (rows,), K, X.device, stream)
-    d = _same_device(X, codes, scales)
-    _check(_lib.rgnn_int8_quantize_rows(_dtype(X), xp, rows, ldx, K, codes.data_ptr(), scales.data_ptr(),
-                                        _stream_on(stream, d)))
+    cp = codes.data_ptr() if made[0] else _flat(codes, "codes", (rows, -(-K // 128) * 128), d, t.int8)
+    sp = scales.data_ptr() if made[1] else _flat(scales, "scales", (rows,), d, t.float32)
+    _check(_lib.rgnn_int8_quantize_rows(t.floats[X.dtype], xp, rows, ldx, K, cp, sp, _stream_of(stream, d, t)))
     return codes, scales
 
 
 def int8_quantize_weights(W, codes=None, scales=None, stream=None):
     """W [types, K, N] -> (codes int8 [types, N, Kp], scales float32 [types, N]), a scale for each output."""
+    t = _torch()
+    d = _device_of(W, t)
     if W.dim() != 3 or not W.is_contiguous():
         raise ValueError("W must be contiguous [types, K, N]")
     T, K, N = W.shape
     codes, scales = _int8_out(codes, scales, (T, N), K, W.device, stream)
-    d = _same_device(W, codes, scales)
-    _check(_lib.rgnn_int8_quantize_weights(_dtype(W), W.data_ptr(), T, K, N, codes.data_ptr(), scales.data_ptr(),
-                                           _stream_on(stream, d)))
+    _check(_lib.rgnn_int8_quantize_weights(t.floats[W.dtype], W.data_ptr(), T, K, N,
+                                           _flat(codes, "codes", (T, N, -(-K // 128) * 128), d, t.int8),
+                                           _flat(scales, "scales", (T, N), d, t.float32), _stream_of(stream, d, t)))
     return codes, scales
 
 
 def typed_linear_int8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatter=None, stream=None):
     """typed_linear on the codes and scales of int8_quantize_rows (or rms_norm) and
     int8_quantize_weights; Y fp32, bf16 or fp16."""
-    d = _same_device(X, x_scales, type_ptr, W, w_scales, Y, gather, scatter)
-    if W.dim() != 3 or X.dim() != 2:
-        raise ValueError("X must be [rows, Kp], W [types, N, Kp]")
-    T, N, K = W.shape
-    rows = X.shape[0]
-    _int8_check(X, x_scales, (rows,), K)
-    _int8_check(W, w_scales, (T, N), K)
-    yp, yr, ldy = _matrix(Y, "Y", N)
+    t = _torch()
+    d = _device_of(X, t)
+    if W.dim() != 3 or X.dim() != 2 or Y.dim() != 2:
+        raise ValueError("X must be [rows, Kp], W [types, N, Kp], Y [y_rows, N]")
+    (T, N, K), rows, y_rows = W.shape, X.shape[0], Y.shape[0]
+    if K % 128:
+        raise ValueError("codes lie in rows of whole blocks of 128")
+    yp, ldy = _rows(Y, "Y", (y_rows, N), d)
+    for index in (gather, scatter):
+        if index is not None and index.get_device() != d:
+            raise ValueError("tensors must be on one device")
     gp, sp = _index(gather), _index(scatter)
     M = _positions(type_ptr, T, gather, scatter, rows)
-    _check(_lib.rgnn_typed_linear_int8(X.data_ptr(), x_scales.data_ptr(), rows, gp, type_ptr.data_ptr(), T, M,
-                                       W.data_ptr(), w_scales.data_ptr(), K, N, _dtype(Y), yp, yr, ldy, sp,
-                                       _stream_on(stream, d)))
+    _check(_lib.rgnn_typed_linear_int8(
+        _flat(X, "X", (rows, K), d, t.int8), _flat(x_scales, "x_scales", (rows,), d, t.float32), rows, gp,
+        _flat(type_ptr, "type_ptr", (T + 1,), d), T, M, _flat(W, "W", (T, N, K), d, t.int8),
+        _flat(w_scales, "w_scales", (T, N), d, t.float32), K, N, t.floats[Y.dtype], yp, y_rows, ldy, sp, _stream_of(stream, d, t)))
 
 
 class Dropout:
@@ -672,73 +732,83 @@ class Dropout:
             raise ValueError("rng must be contiguous int64 [2]")
         if not 0 <= p <= 1:
             raise ValueError("p must lie in [0, 1]")
+        if not -2 ** 63 <= call < 2 ** 63:
+            raise ValueError("call must be a 64-bit number")
         self.p, self.rng, self.call = float(p), rng, int(call)
 
-    def _args(self):
-        return DropoutArgs(self.rng.data_ptr(), self.call, self.p)
-
-
-def _rows(t, name: str, rows: int, cols: int, dtype=None):
-    """(pointer, leading dimension) of a matrix of that size."""
-    p, r, ld = _matrix(t, name, cols)
-    if r != rows or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} must be [{rows}, {cols}]" + (f" of {dtype}" if dtype is not None else ""))
-    return p, ld
-
-
-def _vector(t, name: str, n: int, dtype=None):
-    if t is None:
-        return None
-    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} must be contiguous [{n}]" + (f" of {dtype}" if dtype is not None else ""))
-    return t.data_ptr()
-
-
-def _drop(dropout):
-    return None if dropout is None else ctypes.byref(dropout._args())
+    def _args(self, device: int):
+        rng = self.rng
+        if rng.get_device() != device:
+            raise ValueError("rng must be on the tensors' device")
+        return rng.data_ptr(), self.call, self.p
 
 
 def dropout(X, Y, dropout: Dropout, residual=None, stream=None):
     """Y = [residual +] D(X); X, Y fp32, bf16 or fp16, residual of Y's type.  Y may be X or residual.  With the
     output's gradient as X and no residual: the gradient of x."""
-    d = _same_device(X, Y, dropout.rng, residual)
+    t = _torch()
+    floats = t.floats
+    d = _device_of(X, t)
     if X.dim() != 2:
         raise ValueError("X must be a matrix")
-    rows, cols = X.shape
-    xp, ldx = _rows(X, "X", rows, cols)
-    yp, ldy = _rows(Y, "Y", rows, cols)
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", rows, cols, Y.dtype)
-    _check(_lib.rgnn_dropout(_dtype(X), xp, rows, ldx, cols, _drop(dropout), _dtype(Y), rp, ldr, yp, ldy,
-                             _stream_on(stream, d)))
+    rows, cols = shape = X.shape
+    xp, ldx = _rows(X, "X", shape, d)
+    yp, ldy = _rows(Y, "Y", shape, d)
+    rp = ldr = 0
+    if residual is not None:
+        if residual.dtype != Y.dtype:
+            raise ValueError("residual must be of Y's type")
+        rp, ldr = _rows(residual, "residual", shape, d)
+    _check(_lib.rgnn_dropout(_DROPOUT_PACK(xp, rp, yp, rows, ldx, ldr, ldy, *dropout._args(d), cols, floats[X.dtype], floats[Y.dtype]),
+                             _stream_of(stream, d, t)))
 
 
 def rms_norm(X, weight, Y, eps=1e-6, residual=None, sum=None, scales=None, rstd=None, dropout=None, stream=None):
     """r = [residual +] D(X), Y = r / sqrt(mean(r^2) + eps) * weight for each row; weight [cols] or None.
-    sum: takes r (of residual's type; X's without one); rstd: float32 [rows], takes the root's inverse.  Y fp32,
+    sum: takes r (of residual's type; of any without one); rstd: float32 [rows], takes the root's inverse.  Y fp32,
     bf16 or fp16; or float8_e4m3fn codes [rows, Kp] with scales uint8 [rows, Ks] for typed_linear_fp8; or int8 codes
-    [rows, Kp] with scales float32 [rows] for typed_linear_int8.  Y may be X, sum may be residual."""
-    import torch
-    d = _same_device(X, weight, Y, residual, sum, scales, rstd, None if dropout is None else dropout.rng)
+    [rows, Kp] with scales float32 [rows] for typed_linear_int8.  Y may be X, sum may be residual.  A call's 16-bit tensors are of
+    one type."""
+    t = _torch()
+    floats = t.floats
+    d = _device_of(X, t)
     if X.dim() != 2:
         raise ValueError("X must be a matrix")
-    rows, cols = X.shape
-    xp, ldx = _rows(X, "X", rows, cols)
-    kept = residual if residual is not None else sum if sum is not None else X
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", rows, cols)
-    sp, lds = (None, 0) if sum is None else _rows(sum, "sum", rows, cols, kept.dtype)
-    if Y.dtype == torch.float8_e4m3fn or Y.dtype == torch.int8:
-        if scales is None:
-            raise ValueError("8-bit codes need scales")
-        code = F8_E4M3 if Y.dtype == torch.float8_e4m3fn else I8
-        _fp8_check(Y, scales, (rows,), (rows,), cols) if code == F8_E4M3 else _int8_check(Y, scales, (rows,), cols)
-        yp, ldy, scp = Y.data_ptr(), 0, scales.data_ptr()
-    else:
+    rows, cols = shape = X.shape
+    xp, ldx = _rows(X, "X", shape, d)
+    rp = ldr = sp = lds = wp = scp = sdp = 0
+    x_type = sum_type = floats[X.dtype]
+    if residual is not None:
+        rp, ldr = _rows(residual, "residual", shape, d)
+        sum_type = floats[residual.dtype]
+    if sum is not None:
+        sp, lds = _rows(sum, "sum", shape, d)
+        if residual is None:
+            sum_type = floats[sum.dtype]
+        elif sum.dtype != residual.dtype:
+            raise ValueError("sum must be of residual's type")
+    w_type = F32
+    if weight is not None:
+        wp, w_type = _flat(weight, "weight", (cols,), d), floats[weight.dtype]
+    if rstd is not None:
+        sdp = _flat(rstd, "rstd", (rows,), d, t.float32)
+    code = floats.get(Y.dtype)
+    if code is not None:
         if scales is not None:
             raise ValueError("scales are for 8-bit codes")
-        (yp, ldy), code, scp = _rows(Y, "Y", rows, cols), _dtype(Y), None
-    _check(_lib.rgnn_rms_norm(_dtype(X), xp, rows, ldx, cols, _drop(dropout), _dtype(kept), rp, ldr, sp, lds,
-                              F32 if weight is None else _dtype(weight), _vector(weight, "weight", cols), eps, code, yp, ldy,
-                              scp, _vector(rstd, "rstd", rows, torch.float32), _stream_on(stream, d)))
+        yp, ldy = _rows(Y, "Y", shape, d)
+    else:
+        if scales is None:
+            raise ValueError("Y must be fp32, bf16 or fp16, or 8-bit codes with scales")
+        Kp, Ks = fp8_widths(cols)
+        if Y.dtype == t.int8:
+            code, ldy, scp = I8, Kp, _flat(scales, "scales", (rows,), d, t.float32)
+        else:
+            code, ldy, scp = F8_E4M3, Kp, _flat(scales, "scales", (rows, Ks), d, t.uint8)
+        yp = _flat(Y, "codes", (rows, Kp), d, t.int8 if code == I8 else t.e4m3)
+    _check(_lib.rgnn_rms_norm(_NORM_PACK(xp, rp, sp, wp, yp, scp, sdp, rows, ldx, ldr, lds, ldy, eps,
+                                         *(_NO_DROPOUT if dropout is None else dropout._args(d)), cols, x_type, sum_type,
+                                         w_type, code), _stream_of(stream, d, t)))
 
 
 def rms_norm_backward_workspace_size(rows: int, cols: int) -> int:
@@ -752,21 +822,38 @@ def rms_norm_backward(dY, sum, rstd, weight, d_sum=None, d_residual=None, dX=Non
     """The gradients of rms_norm: sum and rstd as it wrote them (sum: X itself without residual and dropout), d_sum
     the gradient that reaches the sum by other ways.  d_residual (sum's type), dX and dW [cols] are written where
     given; dW needs the workspace ws.  d_residual may be d_sum, dX may be dY."""
-    import torch
-    d = _same_device(dY, sum, rstd, weight, d_sum, d_residual, dX, dW, ws, None if dropout is None else dropout.rng)
+    t = _torch()
+    floats = t.floats
+    d = _device_of(dY, t)
     if dY.dim() != 2:
         raise ValueError("dY must be a matrix")
-    rows, cols = dY.shape
-    yp, ldy = _rows(dY, "dY", rows, cols)
-    sp, lds = _rows(sum, "sum", rows, cols)
-    gp, ldg = (None, 0) if d_sum is None else _rows(d_sum, "d_sum", rows, cols, sum.dtype)
-    rp, ldr = (None, 0) if d_residual is None else _rows(d_residual, "d_residual", rows, cols, sum.dtype)
-    xp, ldx = (None, 0) if dX is None else _rows(dX, "dX", rows, cols)
+    rows, cols = shape = dY.shape
+    yp, ldy = _rows(dY, "dY", shape, d)
+    sp, lds = _rows(sum, "sum", shape, d)
+    gp = ldg = rp = ldr = xp = ldx = wp = dwp = wsp = ws_bytes = 0
+    w_type = x_type = dw_type = F32
+    if d_sum is not None:
+        if d_sum.dtype != sum.dtype:
+            raise ValueError("d_sum must be of sum's type")
+        gp, ldg = _rows(d_sum, "d_sum", shape, d)
+    if d_residual is not None:
+        if d_residual.dtype != sum.dtype:
+            raise ValueError("d_residual must be of sum's type")
+        rp, ldr = _rows(d_residual, "d_residual", shape, d)
+    if dX is not None:
+        (xp, ldx), x_type = _rows(dX, "dX", shape, d), floats[dX.dtype]
+    if weight is not None:
+        wp, w_type = _flat(weight, "weight", (cols,), d), floats[weight.dtype]
+    if dW is not None:
+        dwp, dw_type = _flat(dW, "dW", (cols,), d), floats[dW.dtype]
+    if ws is not None:
+        if ws.get_device() != d or not ws.is_contiguous():
+            raise ValueError("the workspace must be contiguous, on the tensors' device")
+        wsp, ws_bytes = ws.data_ptr(), ws.numel() * ws.element_size()
     _check(_lib.rgnn_rms_norm_backward(
-        _dtype(dY), yp, rows, ldy, cols, _dtype(sum), sp, lds, _vector(rstd, "rstd", rows, torch.float32),
-        F32 if weight is None else _dtype(weight), _vector(weight, "weight", cols), gp, ldg, _drop(dropout), rp, ldr,
-        F32 if dX is None else _dtype(dX), xp, ldx, F32 if dW is None else _dtype(dW), _vector(dW, "dW", cols), _ptr(ws),
-        0 if ws is None else ws.numel() * ws.element_size(), _stream_on(stream, d)))
+        _NORM_BACKWARD_PACK(yp, sp, _flat(rstd, "rstd", (rows,), d, t.float32), wp, gp, rp, xp, dwp, wsp, rows, ldy, lds, ldg,
+                            ldr, ldx, ws_bytes, *(_NO_DROPOUT if dropout is None else dropout._args(d)), cols, floats[dY.dtype],
+                            floats[sum.dtype], w_type, x_type, dw_type), _stream_of(stream, d, t)))
 
 
 class AdamwTensors:

@@ -16,9 +16,39 @@ def lib():
 P = 0x10000     # an address that no check dereferences
 
 
+class Drop(ctypes.Structure):
+    _fields_ = [("rng", ctypes.c_void_p), ("call", ctypes.c_int64), ("p", ctypes.c_double)]
+
+
+def fields(pointers, sizes, tail, ints):
+    """A structure's fields in the header's order."""
+    return [(n, ctypes.c_void_p) for n in pointers.split()] + [(n, ctypes.c_int64) for n in sizes.split()] + tail + \
+        [(n, ctypes.c_int32) for n in ints.split()]
+
+
+class DropoutRows(ctypes.Structure):
+    _fields_ = fields("X res Y", "rows ldx ldr ldy", [("drop", Drop)], "cols dtype y_dtype")
+
+
+class Norm(ctypes.Structure):
+    _fields_ = fields("X res sum w Y scales rstd", "rows ldx ldr lds ldy", [("eps", ctypes.c_double), ("drop", Drop)],
+                      "cols dtype sum_dtype w_dtype y_dtype")
+
+
+class NormBackward(ctypes.Structure):
+    _fields_ = fields("dY sum rstd w dsum dres dX dW ws", "rows lddy lds ldds lddr lddx ws_bytes", [("drop", Drop)],
+                      "cols dy_dtype sum_dtype w_dtype dx_dtype dw_dtype")
+
+
 def drop(p=0.5, rng=P, call=0):
-    rgnn, _ = lib()
-    return ctypes.byref(rgnn.DropoutArgs(rng, call, p))
+    return Drop(rng, call, p)
+
+
+def call(function, structure, a, kw):
+    assert set(kw) <= set(a)
+    a.update(kw)
+    a["drop"] = a["drop"] or Drop()
+    return function(bytes(structure(**a)), None)
 
 
 @pytest.mark.parametrize("counter,key,answer", [
@@ -35,10 +65,14 @@ def test_generator(counter, key, answer):
 def norm(**kw):
     _, l = lib()
     a = dict(dtype=1, X=P, rows=10, ldx=64, cols=64, drop=None, sum_dtype=1, res=P, ldr=64, sum=P, lds=64, w_dtype=1, w=P,
-             eps=1e-6, y_dtype=1, Y=P, ldy=64, scales=None, rstd=None, stream=None)
-    assert set(kw) <= set(a)
-    a.update(kw)
-    return l.rgnn_rms_norm(*a.values())
+             eps=1e-6, y_dtype=1, Y=P, ldy=64, scales=None, rstd=None)
+    return call(l.rgnn_rms_norm, Norm, a, kw)
+
+
+def dropout(**kw):
+    _, l = lib()
+    a = dict(dtype=1, X=P, rows=4, ldx=64, cols=64, drop=drop(), y_dtype=1, res=P, ldr=64, Y=P, ldy=64)
+    return call(l.rgnn_dropout, DropoutRows, a, kw)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -57,18 +91,17 @@ def test_norm_refusals(kw, status):
     assert l.rgnn_last_error()
 
 
-@pytest.mark.parametrize("kw", [dict(p=-0.1), dict(p=1.5), dict(p=float("nan")), dict(rng=None), dict(rng=P + 4)])
+@pytest.mark.parametrize("kw", [dict(p=-0.1), dict(p=1.5), dict(p=float("nan")), dict(rng=P + 4)])
 def test_dropout_arguments_are_refused(kw):
-    _, l = lib()
     assert norm(drop=drop(**kw)) == -1
-    assert l.rgnn_dropout(1, P, 4, 64, 64, drop(**kw), 1, None, 0, P, 64, None) == -1
+    assert dropout(drop=drop(**kw)) == -1
     assert backward(drop=drop(**kw)) == -1
 
 
 def test_no_rows_are_ok():
     _, l = lib()
     assert norm(rows=0, X=None, Y=None, res=None, sum=None) == 0
-    assert l.rgnn_dropout(1, None, 0, 64, 64, drop(), 1, None, 0, None, 64, None) == 0
+    assert dropout(rows=0, X=None, Y=None, res=None) == 0
     assert l.rgnn_int8_quantize_rows(1, None, 0, 64, 64, None, None, None) == 0
     assert backward(rows=0, dW=None, dY=None, sum=None, rstd=None) == 0
     assert backward(dW=None, dX=None, dres=None) == 0            # nothing wanted
@@ -77,10 +110,8 @@ def test_no_rows_are_ok():
 def backward(**kw):
     rgnn, l = lib()
     a = dict(dy_dtype=1, dY=P, rows=10, lddy=64, cols=64, sum_dtype=1, sum=P, lds=64, rstd=P, w_dtype=1, w=P, dsum=P, ldds=64,
-             drop=None, dres=P, lddr=64, dx_dtype=1, dX=P, lddx=64, dw_dtype=1, dW=P, ws=P, ws_bytes=1 << 20, stream=None)
-    assert set(kw) <= set(a)
-    a.update(kw)
-    return l.rgnn_rms_norm_backward(*a.values())
+             drop=None, dres=P, lddr=64, dx_dtype=1, dX=P, lddx=64, dw_dtype=1, dW=P, ws=P, ws_bytes=1 << 20)
+    return call(l.rgnn_rms_norm_backward, NormBackward, a, kw)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -112,12 +143,23 @@ def test_backward_workspace_size():
 
 @pytest.mark.parametrize("kw", [dict(dtype=3), dict(y_dtype=4), dict(dtype=2), dict(rows=-1), dict(cols=0), dict(X=None),
                                 dict(Y=None), dict(X=P + 1), dict(Y=P + 1), dict(res=P + 1), dict(ldx=63), dict(ldy=63),
-                                dict(ldr=63), dict(drop=None)])
+                                dict(ldr=63)])
 def test_dropout_refusals(kw):
+    assert dropout(**kw) == -1
+
+
+def test_no_arguments_are_refused():
     _, l = lib()
-    a = dict(dtype=1, X=P, rows=4, ldx=64, cols=64, drop=drop(), y_dtype=1, res=P, ldr=64, Y=P, ldy=64, stream=None)
-    a.update(kw)
-    assert l.rgnn_dropout(*a.values()) == -1
+    assert l.rgnn_dropout(None, None) == l.rgnn_rms_norm(None, None) == l.rgnn_rms_norm_backward(None, None) == -1
+
+
+def test_packed_arguments_are_the_structures():
+    rgnn, _ = lib()
+    assert rgnn._DROPOUT_PACK(*range(1, 9), -9, 0.5, 11, 12, 13) == bytes(DropoutRows(1, 2, 3, 4, 5, 6, 7, Drop(8, -9, 0.5), 11, 12, 13))
+    assert rgnn._NORM_PACK(*range(1, 13), 0.25, 14, -15, 0.5, 17, 18, 19, 20, 21) == bytes(
+        Norm(*range(1, 13), 0.25, Drop(14, -15, 0.5), 17, 18, 19, 20, 21))
+    assert rgnn._NORM_BACKWARD_PACK(*range(1, 18), -18, 0.5, *range(20, 26)) == bytes(
+        NormBackward(*range(1, 17), Drop(17, -18, 0.5), *range(20, 26)))
 
 
 @pytest.mark.parametrize("args", [
@@ -186,8 +228,8 @@ def test_norm_wrapper_checks_shapes(change, monkeypatch):
     """Shapes, types and strides are checked before the library is called (devices apart, which a CPU tensor fails first)."""
     import torch
     rgnn, _ = lib()
-    monkeypatch.setattr(rgnn, "_same_device", lambda *t: 0)
-    monkeypatch.setattr(rgnn, "_stream_on", lambda *t: None)
+    monkeypatch.setattr(rgnn, "_device_of", lambda t, _: t.get_device())
+    monkeypatch.setattr(rgnn, "_stream_of", lambda *t: None)
     kinds = {"f": torch.float32, "h": torch.bfloat16, "i": torch.int8, "8": torch.float8_e4m3fn}
 
     def make(spec):
