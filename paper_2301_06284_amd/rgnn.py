@@ -604,7 +604,8 @@ class _Torch:
         import torch
         self.current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        self.empty, self.int8, self.float32, self.uint8, self.e4m3 = torch.empty, torch.int8, torch.float32, torch.uint8, torch.float8_e4m3fn
+        self.empty, self.float32, self.e4m3 = torch.empty, torch.float32, torch.float8_e4m3fn
+        self.int8, self.uint8, self.int32, self.int64 = torch.int8, torch.uint8, torch.int32, torch.int64
 
         class Floats(dict):
             def __missing__(self, dtype):
@@ -662,9 +663,9 @@ def _int8_out(codes, scales, lead, K, device, stream):
         return _on_stream(stream, device, lambda: _int8_out(codes, scales, lead, K, device, None))
     t = _torch()
     if codes is None:
-        codes = t.empty((*lead, -(-K // 128) * 128), dtype=t.int8, device=device)
+        codes = t.empty(*lead, -(-K // 128) * 128, dtype=t.int8, device=device)
     if scales is None:
-        scales = t.empty(lead, dtype=t.float32, device=device)
+        scales = t.empty(*lead, dtype=t.float32, device=device)
     return codes, scales
 
 
@@ -710,14 +711,12 @@ def typed_linear_int8(X, x_scales, type_ptr, W, w_scales, Y, gather=None, scatte
     if K % 128:
         raise ValueError("codes lie in rows of whole blocks of 128")
     yp, ldy = _rows(Y, "Y", (y_rows, N), d)
-    for index in (gather, scatter):
-        if index is not None and index.get_device() != d:
-            raise ValueError("tensors must be on one device")
-    gp, sp = _index(gather), _index(scatter)
-    M = _positions(type_ptr, T, gather, scatter, rows)
+    M = gather.shape[0] if gather is not None else scatter.shape[0] if scatter is not None else rows
+    gp = None if gather is None else _flat(gather, "gather", (M,), d, t.int32)
+    sp = None if scatter is None else _flat(scatter, "scatter", (M,), d, t.int32)
     _check(_lib.rgnn_typed_linear_int8(
         _flat(X, "X", (rows, K), d, t.int8), _flat(x_scales, "x_scales", (rows,), d, t.float32), rows, gp,
-        _flat(type_ptr, "type_ptr", (T + 1,), d), T, M, _flat(W, "W", (T, N, K), d, t.int8),
+        _flat(type_ptr, "type_ptr", (T + 1,), d, t.int64), T, M, _flat(W, "W", (T, N, K), d, t.int8),
         _flat(w_scales, "w_scales", (T, N), d, t.float32), K, N, t.floats[Y.dtype], yp, y_rows, ldy, sp, _stream_of(stream, d, t)))
 
 

@@ -629,7 +629,7 @@ def test_int8_rows(dtype, K):
             assert scales[3] == 2.0 ** -126
 
 
-@pytest.mark.parametrize("K,N", [(1, 1), (8, 8), (100, 77), (64, 64), (128, 65), (130, 63), (500, 128), (2048, 136), (1000, 1)])
+@pytest.mark.parametrize("K,N", [(1, 1), (8, 8), (100, 77), (64, 64), (128, 65), (130, 63), (500, 128), (2048, 136), (1000, 1), (1030, 40), (2049, 33), (4096, 72), (4100, 72)])
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 def test_int8_weights(dtype, K, N):
     import torch
