@@ -293,8 +293,8 @@ struct Philox {
 #pragma unroll
         for (int i = 0; i < 10; ++i) {
             const uint64_t p = (uint64_t)a * 0xD2511F53u, q = (uint64_t)c * 0xCD9E8D57u;
-            a = (uint32_t)(q >> 32) ^ b ^ x;
-            c = (uint32_t)(p >> 32) ^ d ^ y;
+            a = (uint32_t)__builtin_amdgcn_bitop3_b32((int)(q >> 32), (int)b, (int)x, 0x96);      // exclusive or of three
+            c = (uint32_t)__builtin_amdgcn_bitop3_b32((int)(p >> 32), (int)d, (int)y, 0x96);
             b = (uint32_t)q;
             d = (uint32_t)p;
             x += 0x9E3779B9u;
