@@ -112,24 +112,27 @@ struct Eight {
             for (int i = 0; i < words; ++i) raw[i] = c < cols ? raw[i] : 0;
             return;
         }
-        const int by = c + 8 - cols;
-        if (by <= 0 || cols < 8) return;
+        if (c + 8 <= cols || cols < 8) return;
+        const int by = 8 - (cols & 7);            // the same for all lanes whose vector the row ends in: c is whole vectors
         if constexpr (sizeof(E) == 2) {
-            uint64_t lo = (uint64_t)raw[1] << 32 | raw[0], hi = (uint64_t)raw[3] << 32 | raw[2];
-            const int bits = (by & 3) * 16;
-            if (by & 4) { lo = hi; hi = 0; }
-            if (bits) { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
-            if (by >= 8) lo = hi = 0;
-            raw[0] = (uint32_t)lo; raw[1] = (uint32_t)(lo >> 32);
-            raw[2] = (uint32_t)hi; raw[3] = (uint32_t)(hi >> 32);
+            if (by & 2)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[i] = i < 3 ? raw[i + 1] : 0;
+            if (by & 4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[i] = i < 2 ? raw[i + 2] : 0;
+            if (by & 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw[i] = raw[i] >> 16 | (i < 3 ? raw[i + 1] << 16 : 0);
         } else {
 #pragma unroll
             for (int step = 1; step < 8; step *= 2)
+                if (by & step)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) raw[i] = by & step ? (i + step < 8 ? raw[i + step] : 0) : raw[i];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) raw[i] = by >= 8 ? 0 : raw[i];
+                    for (int i = 0; i < 8; ++i) raw[i] = i + step < 8 ? raw[i + step] : 0;
         }
+#pragma unroll
+        for (int i = 0; i < words; ++i) raw[i] = c < cols ? raw[i] : 0;
     }
     __device__ __forceinline__ float at(int i) const
     {
@@ -149,10 +152,10 @@ __device__ __forceinline__ void store8(void *base, int64_t row, const float (&x)
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (E)x[i];
     E *p = (E *)base + row + c;
-    const int left = cols - c;
-    if (left >= 8) {
+    const int left = cols & 7;                    // of the vector that the row ends in
+    if (c + 8 <= cols) {
         __builtin_memcpy(p, &v, sizeof(v));
-    } else if (!WHOLE && left > 0) {
+    } else if (!WHOLE && c < cols) {
         if constexpr (sizeof(E) == 2) {
             i32x4 w = __builtin_bit_cast(i32x4, v);
             if (left & 4) {
