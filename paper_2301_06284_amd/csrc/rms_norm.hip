@@ -56,12 +56,12 @@ __device__ __forceinline__ float inverse_rms(double squares, int cols, double ep
 
 // L threads hold a row, NV vectors of eight columns each.
 template <class H, bool X32, bool R32, bool WHOLE, int L, int NV>
-__global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_kernel(NormArgs a)
+__global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
 {
 #pragma clang fp contract(off)
     typedef typename std::conditional<X32, float, H>::type XT;
     typedef typename std::conditional<R32, float, H>::type RT;
-    constexpr int PER = L >= 256 ? 1 : 256 / L;      // rows of a workgroup
+    constexpr int PER = L > 64 ? 1 : 256 / L;       // rows of a workgroup
     __shared__ double sums[L > 64 ? L / 64 : 1];
     __shared__ uint32_t tops[L > 64 ? L / 64 : 1];
     const int64_t row = flat_block() * (int64_t)PER + (PER > 1 ? threadIdx.x / L : 0);
@@ -245,30 +245,41 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     if (a.out == kRowsE4m3 && (int)threadIdx.x < fp8_scales(a.cols) - (kp >> 7)) sc[(kp >> 7) + threadIdx.x] = 127;
 }
 
-template <class H, bool X32, bool R32, int L, int NV>
+template <class H, bool X32, bool R32, bool WHOLE, int L, int NV>
 void launch_rows(const NormArgs &a, hipStream_t s)
 {
-    constexpr int PER = L >= 256 ? 1 : 256 / L;
-    const dim3 g = flat_grid((a.rows + PER - 1) / PER), b(L > 256 ? L : 256);
-    if (whole_vectors(a.cols)) hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, true, L, NV>), g, b, 0, s, a);
-    else hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, false, L, NV>), g, b, 0, s, a);
+    constexpr int PER = L > 64 ? 1 : 256 / L;
+    hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, WHOLE, L, NV>), flat_grid((a.rows + PER - 1) / PER), dim3(L > 64 ? L : 256), 0, s, a);
+}
+
+// The threads of a row: as many as it has vectors of eight, a power of two, which measured faster than fewer threads with
+// several vectors (bf16, with residual and sum: 60 000 x 512 64 threads 39.2 us, 32 of two 43.2; 30 000 x 1000 128 threads
+// 41.4, 64 of two 42.8; 8000 x 4096 512 threads 41.9, 256 of two 43.4; 4000 x 8192 1024 threads 44.0, 256 of four 48.5; 8 x 1000
+// 2.6 and 3.2).  Two vectors a thread where rows end inside one (80 000 x 333 53.9 us, 64 threads 60.0; 30 000 x 1001
+// 50.4, 128 threads 54.7) and for long rows of codes (4000 x 8192 into int8 42.4, 1024 threads 44.6).
+template <class H, bool X32, bool R32, bool WHOLE>
+void launch_cols(const NormArgs &a, hipStream_t s)
+{
+    const bool codes = a.out > kRowsF32;
+    const int cols = codes ? fp8_width(a.cols) : a.cols;
+    if (cols <= 64) launch_rows<H, X32, R32, WHOLE, 8, 1>(a, s);
+    else if (cols <= 128) launch_rows<H, X32, R32, WHOLE, 16, 1>(a, s);
+    else if (cols <= 256) launch_rows<H, X32, R32, WHOLE, 32, 1>(a, s);
+    else if (cols <= 512) launch_rows<H, X32, R32, WHOLE, WHOLE ? 64 : 32, WHOLE ? 1 : 2>(a, s);
+    else if (cols <= 1024) launch_rows<H, X32, R32, WHOLE, WHOLE ? 128 : 64, WHOLE ? 1 : 2>(a, s);
+    else if (cols <= 2048) launch_rows<H, X32, R32, WHOLE, 256, 1>(a, s);
+    else if (cols <= 4096) launch_rows<H, X32, R32, WHOLE, 512, 1>(a, s);
+    else if (cols <= 8192 && !codes) launch_rows<H, X32, R32, WHOLE, 1024, 1>(a, s);
+    else if (cols <= 8192) launch_rows<H, X32, R32, WHOLE, 512, 2>(a, s);
+    else if (cols <= 16384) launch_rows<H, X32, R32, WHOLE, 1024, 2>(a, s);
+    else if (cols <= 32768) launch_rows<H, X32, R32, WHOLE, 1024, 4>(a, s);
+    else hipLaunchKernelGGL((rms_norm_long_kernel<H, X32, R32>), flat_grid(a.rows), dim3(1024), 0, s, a);
 }
 
 template <class H, bool X32, bool R32>
 void launch_types(const NormArgs &a, hipStream_t s)
 {
-    const int cols = a.out <= kRowsF32 ? a.cols : fp8_width(a.cols);
-    if (cols <= 64) launch_rows<H, X32, R32, 8, 1>(a, s);
-    else if (cols <= 128) launch_rows<H, X32, R32, 16, 1>(a, s);
-    else if (cols <= 256) launch_rows<H, X32, R32, 32, 1>(a, s);
-    else if (cols <= 512) launch_rows<H, X32, R32, 32, 2>(a, s);
-    else if (cols <= 1024) launch_rows<H, X32, R32, 64, 2>(a, s);
-    else if (cols <= 2048) launch_rows<H, X32, R32, 256, 1>(a, s);
-    else if (cols <= 4096) launch_rows<H, X32, R32, 256, 2>(a, s);
-    else if (cols <= 8192) launch_rows<H, X32, R32, 256, 4>(a, s);
-    else if (cols <= 16384) launch_rows<H, X32, R32, 1024, 2>(a, s);
-    else if (cols <= 32768) launch_rows<H, X32, R32, 1024, 4>(a, s);
-    else hipLaunchKernelGGL((rms_norm_long_kernel<H, X32, R32>), flat_grid(a.rows), dim3(1024), 0, s, a);
+    whole_vectors(a.cols) ? launch_cols<H, X32, R32, true>(a, s) : launch_cols<H, X32, R32, false>(a, s);
 }
 
 template <class H>
