@@ -236,6 +236,60 @@ def test_norm_without_a_kept_sum(cols, y_t):
     check_norm(33, cols, "bf16", "bf16", "bf16", y_t, p=0.1, keep_sum=False)
 
 
+@pytest.mark.parametrize("cols", [100, 1000, 1001, 2048, 8192, 33000])
+def test_norm_with_dropout_into_codes(cols):
+    check_norm(21, cols, "bf16", "bf16", "bf16", "e4m3", p=0.2)
+    check_norm(21, cols, "fp16", "fp32", "fp32", "int8", p=0.2)
+
+
+@pytest.mark.parametrize("cols", [64, 333, 2048, 33000])
+@pytest.mark.parametrize("x_t,sum_t", [("fp32", "bf16"), ("bf16", "fp32"), ("fp32", "fp16")])
+def test_norm_keeps_the_sum_in_another_type(cols, x_t, sum_t):
+    """Without a residual the sum may be of any type; y is of what is kept."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    print(f"sum of another type {cols} {x_t} {sum_t}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = matrix(g, 19, cols, types()[x_t])
+    total, rstd = torch.empty(19, cols, dtype=types()[sum_t], device="cuda"), torch.empty(19, device="cuda")
+    y = torch.empty(19, cols, device="cuda")
+    rgnn.rms_norm(x, None, y, sum=total, rstd=rstd)
+    assert torch.equal(total, x.to(types()[sum_t]))
+    s = 1 / torch.sqrt(total.double().square().mean(dim=1) + 1e-6)
+    assert ((rstd.double() - s).abs() <= SECOND * U * s).all()
+    ref = total.double() * rstd.double()[:, None]
+    close(y, ref, 2 * U * ref.abs() + 2.0 ** -148, "y")
+
+
+def test_two_graphs_share_a_workspace():
+    """Two captured backward passes with one workspace, replayed in turn with eager work in between."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    g = torch.Generator(device="cuda").manual_seed(6)
+    sets, graphs, wanted = [], [], []
+    ws = torch.empty(rgnn.rms_norm_backward_workspace_size(5000, 512), dtype=torch.uint8, device="cuda")
+    for rows, cols in ((5000, 512), (700, 100)):
+        x, dy = matrix(g, rows, cols, torch.float32), matrix(g, rows, cols, torch.float32)
+        sets.append((dy, x, torch.ones(rows, device="cuda"), torch.ones(cols, device="cuda"), torch.empty_like(x), torch.empty(cols, device="cuda")))
+    for dy, x, rstd, w, dx, dw in sets:
+        work = lambda: rgnn.rms_norm_backward(dy, x, rstd, w, dX=dx, dW=dw, ws=ws)  # noqa: E731,B023
+        work()
+        torch.cuda.synchronize()
+        wanted.append((dx.clone(), dw.clone()))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            work()
+        graphs.append(graph)
+    for turn in range(3):
+        for (dy, x, rstd, w, dx, dw), graph, want in zip(sets, graphs, wanted):
+            dx.zero_(), dw.zero_()
+            if turn == 1:
+                ws.fill_(0xFF)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(dx, want[0]) and torch.equal(dw, want[1])
+
+
 @pytest.mark.parametrize("cols", [64, 100, 2048, 33000])
 def test_norm_in_place(cols):
     """The sum over the residual, the output over x."""
@@ -823,7 +877,6 @@ def test_streams():
     torch.cuda.synchronize()
     for a, b in zip(*got):
         assert a.dtype == torch.uint8 or torch.equal(a, b)
-    s = rgnn.lib()
     with pytest.raises(ValueError):
         rgnn.int8_quantize_rows(x.cpu())
 
