@@ -21,7 +21,7 @@ struct Cut {
 };
 
 // RES: with a residual.  DROP: p is not 0.
-template <class H, bool X32, bool Y32, bool WHOLE, bool RES, bool DROP>
+template <class H, bool X32, bool Y32, Fit FIT, bool RES, bool DROP>
 __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, Cut cut)
 {
 #pragma clang fp contract(off)
@@ -31,8 +31,8 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, Cut cut)
     const int first = (int)(block - down * cut.across) * cut.wide;
     const int64_t row0 = (int64_t)down * cut.tall;
     // Every thread loads all its vectors, those outside from inside: no branch stands between the loads.
-    Eight<XT, WHOLE> x[kVectors];
-    Eight<YT, WHOLE> in[RES ? kVectors : 1];
+    Eight<XT, FIT> x[kVectors];
+    Eight<YT, FIT> in[RES ? kVectors : 1];
     int64_t row[kVectors];
     int col[kVectors];
 #pragma unroll
@@ -61,24 +61,27 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, Cut cut)
             const float kept = RES ? __builtin_fmaf(v, a.drop.factor, res) : v * a.drop.factor;
             y[i] = !DROP || word[i] > a.drop.below ? kept : res;
         }
-        store8<YT, WHOLE>(a.Y, row[u] * a.ldy, y, col[u], a.cols);
+        store8<YT, FIT>(a.Y, row[u] * a.ldy, y, col[u], a.cols);
     }
 }
 
 template <class H, bool X32, bool Y32>
 void launch_types(const DropoutArgs &a, const Cut &cut, dim3 grid, hipStream_t s)
 {
-    auto go = [&](auto whole, auto res, auto drop) {
-        hipLaunchKernelGGL((dropout_kernel<H, X32, Y32, decltype(whole)::value, decltype(res)::value, decltype(drop)::value>), grid, dim3(256),
+    auto go = [&](auto fit, auto res, auto drop) {
+        hipLaunchKernelGGL((dropout_kernel<H, X32, Y32, decltype(fit)::value, decltype(res)::value, decltype(drop)::value>), grid, dim3(256),
                            0, s, a, cut);
     };
     const std::true_type yes;
     const std::false_type no;
-    auto with = [&](auto whole) {
-        if (a.drop.rng) a.res ? go(whole, yes, yes) : go(whole, no, yes);
-        else a.res ? go(whole, yes, no) : go(whole, no, no);
+    auto with = [&](auto fit) {
+        if (a.drop.rng) a.res ? go(fit, yes, yes) : go(fit, no, yes);
+        else a.res ? go(fit, yes, no) : go(fit, no, no);
     };
-    whole_vectors(a.cols) ? with(yes) : with(no);
+    const Fit fit = fit_of(a.cols);
+    if (fit == kWhole) with(std::integral_constant<Fit, kWhole>());
+    else if (fit == kEnds) with(std::integral_constant<Fit, kEnds>());
+    else with(std::integral_constant<Fit, kTiny>());
 }
 
 template <class H>

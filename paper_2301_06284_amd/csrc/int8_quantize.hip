@@ -11,7 +11,7 @@ namespace rgnn {
 
 namespace {
 
-template <class E, bool WHOLE, int L, int NV>
+template <class E, Fit FIT, int L, int NV>
 __global__ __launch_bounds__(L > 64 ? L : 256) void int8_rows_kernel(const E *X, int64_t rows, int64_t ldx, int K, uint8_t *codes,
                                                                       float *scales)
 {
@@ -20,7 +20,7 @@ __global__ __launch_bounds__(L > 64 ? L : 256) void int8_rows_kernel(const E *X,
     const int64_t row = flat_block() * (int64_t)PER + (PER > 1 ? threadIdx.x / L : 0);
     if (row >= rows) return;
     const int lane = threadIdx.x % L, kp = fp8_width(K);
-    Eight<E, WHOLE> x[NV];
+    Eight<E, FIT> x[NV];
     uint32_t top = 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v) x[v].load(X + row * ldx, (v * L + lane) * 8, K);
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(1024) void int8_long_rows_kernel(const E *X, int64_
     const int kp = fp8_width(K);
     uint32_t top = 0;
     for (int c = threadIdx.x * 8; c < K; c += 8192) {
-        Eight<E, false> x;
+        Eight<E, kEnds> x;
         x.load(X + row * ldx, c, K);
         x.settle(c, K);
 #pragma unroll
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(1024) void int8_long_rows_kernel(const E *X, int64_
     const float scale = int8_scale(row_max<1024>(top, tops)), inverse = 1.0f / scale;
     if (threadIdx.x == 0) scales[row] = scale;
     for (int c = threadIdx.x * 8; c < kp; c += 8192) {
-        Eight<E, false> x;
+        Eight<E, kEnds> x;
         float f[8];
         x.load(X + row * ldx, c, K);
         x.settle(c, K);
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(1024) void int8_long_rows_kernel(const E *X, int64_
 // The largest magnitudes of eight columns so far, 16-bit ones two a word: bits of magnitudes order like whole numbers.
 template <class E>
 struct Tops {
-    static constexpr int words = Eight<E, true>::words;
+    static constexpr int words = Eight<E, kWhole>::words;
     typedef uint16_t pair __attribute__((ext_vector_type(2)));
     uint32_t raw[words];
     __device__ __forceinline__ void see(const uint32_t (&x)[words])
@@ -88,7 +88,7 @@ struct Tops {
     __device__ __forceinline__ uint32_t bits(int i) const      // as fp32
     {
         if constexpr (sizeof(E) == 4) return raw[i];
-        else return __float_as_uint(((const Eight<E, true> &)raw).at(i));
+        else return __float_as_uint(((const Eight<E, kWhole> &)raw).at(i));
     }
 };
 
@@ -96,7 +96,7 @@ struct Tops {
 // the codes: four threads across, P times four k a thread.  Loads have one base for all lanes and 32-bit offsets that the
 // P passes share (`k_bytes`: from one k to the next; KS of them stay below 2^32), and no more registers than let a second
 // workgroup of the CU load while this one computes.
-template <class E, bool WHOLE, int TH, int P>
+template <class E, Fit FIT, int TH, int P>
 __global__ __launch_bounds__(TH, sizeof(E) == 4 ? 2 : 4) void int8_weights_kernel(const char *W, int T, int K, int N, int kp, uint32_t k_bytes, uint8_t *codes,
                                                                                   float *scales)
 {
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(TH, sizeof(E) == 4 ? 2 : 4) void int8_weights_kerne
     if (t >= (uint32_t)T || n0 >= N) return;
     const char *w = W + t * K * (int64_t)k_bytes;
     const uint32_t at = (uint32_t)min(n, N - 8) * (uint32_t)sizeof(E);
-    Eight<E, WHOLE> x[P][4];
+    Eight<E, FIT> x[P][4];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const int first = min(p * KS, (K - 1) / 4 * 4), rows = K - first;      // behind K the last one again: no new maximum
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(TH, sizeof(E) == 4 ? 2 : 4) void int8_weights_kerne
     for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (!WHOLE) x[p][q].settle(n, N);
+            if (FIT != kWhole) x[p][q].settle(n, N);
             top.see(x[p][q].raw);
             opaque(x[p][q].raw);
         }
@@ -175,7 +175,7 @@ __global__ __launch_bounds__(TH, sizeof(E) == 4 ? 2 : 4) void int8_weights_kerne
 
 // Longer k are read twice.  A workgroup takes 64 outputs of one type: eight threads across, TH / 8 rows of k at a time for the maxima, then
 // four times as many for the codes, which turn over in LDS.  The second reading comes from L2 or the last-level cache.
-template <class E, bool WHOLE, int TH>
+template <class E, Fit FIT, int TH>
 __global__ __launch_bounds__(TH) void int8_long_weights_kernel(const E *W, int K, int N, int kp, uint8_t *codes, float *scales)
 {
     constexpr int DOWN = TH / 8, KS = DOWN * 4, ROW = KS + 16;      // k of a turn; bytes of an output's codes in LDS
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(TH) void int8_long_weights_kernel(const E *W, int K
     uint32_t top[8] = {};
 #pragma unroll 4
     for (int k = down; k < K; k += DOWN) {
-        Eight<E, WHOLE> x;
+        Eight<E, FIT> x;
         x.load(w + (int64_t)k * N, n, N);
         x.settle(n, N);
 #pragma unroll
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(TH) void int8_long_weights_kernel(const E *W, int K
     for (int i = 0; i < 8; ++i) inv[i] = inverse[across + i];
     for (int k0 = 0; k0 < kp; k0 += KS) {
         const int first = k0 + down * 4;
-        Eight<E, WHOLE> x[4];                    // four k side by side
+        Eight<E, FIT> x[4];                    // four k side by side
 #pragma unroll
         for (int q = 0; q < 4; ++q) x[q].load(w + (int64_t)min(first + q, K - 1) * N, n, N);
 #pragma unroll
@@ -242,8 +242,10 @@ void launch_shape(const E *X, int64_t rows, int64_t ldx, int K, uint8_t *codes, 
 {
     constexpr int PER = L > 64 ? 1 : 256 / L;
     const dim3 g = flat_grid((rows + PER - 1) / PER), b(L > 64 ? L : 256);
-    if (whole_vectors(K)) hipLaunchKernelGGL((int8_rows_kernel<E, true, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
-    else hipLaunchKernelGGL((int8_rows_kernel<E, false, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
+    const Fit fit = fit_of(K);
+    if (fit == kWhole) hipLaunchKernelGGL((int8_rows_kernel<E, kWhole, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
+    else if (fit == kEnds) hipLaunchKernelGGL((int8_rows_kernel<E, kEnds, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
+    else if constexpr (L == 16) hipLaunchKernelGGL((int8_rows_kernel<E, kTiny, L, NV>), g, b, 0, s, X, rows, ldx, K, codes, scales);
 }
 
 // Two vectors of eight a thread measured fastest, one up to 256 and of 1025 to 2048 columns (bf16: 80 000 x 264 12.9 us, one
@@ -264,7 +266,7 @@ void rows_of(const void *p, int64_t rows, int64_t ldx, int K, void *c, float *sc
     else hipLaunchKernelGGL((int8_long_rows_kernel<E>), flat_grid(rows), dim3(1024), 0, s, X, rows, ldx, K, codes, scales);
 }
 
-template <class E, bool WHOLE>
+template <class E, Fit FIT>
 void weights_of(const E *W, int T, int K, int N, uint8_t *codes, float *scales, hipStream_t s)
 {
     const int kp = fp8_width(K);
@@ -272,26 +274,24 @@ void weights_of(const E *W, int T, int K, int N, uint8_t *codes, float *scales, 
     const int64_t pairs = (int64_t)T * ((N + 63) / 64);
     const dim3 g64((uint32_t)((N + 63) / 64), (uint32_t)T);
     auto once = [&](auto kernel, int th) { hipLaunchKernelGGL(kernel, dim3((uint32_t)((pairs + 7) / 8 * 16)), dim3(th), 0, s, (const char *)W, T, K, N, kp, (uint32_t)k_bytes, codes, scales); };
-    if (N < 8 || kp > (sizeof(E) == 2 ? 4096 : 2048) || k_bytes * 1024 >= (uint64_t(1) << 32) || pairs >= (1 << 20)) {
-        hipLaunchKernelGGL((int8_long_weights_kernel<E, WHOLE, 1024>), g64, dim3(1024), 0, s, W, K, N, kp, codes, scales);
-    } else if (kp <= 256) {
-        once(int8_weights_kernel<E, WHOLE, 256, 1>, 256);
-    } else if (kp <= 512) {
-        once(int8_weights_kernel<E, WHOLE, 256, 2>, 256);
-    } else if (kp <= 1024) {
-        once(int8_weights_kernel<E, WHOLE, 512, 2>, 512);
-    } else if (kp <= 2048) {
-        once(int8_weights_kernel<E, WHOLE, 512, 4>, 512);
-    } else if constexpr (sizeof(E) == 2) {
-        once(int8_weights_kernel<E, WHOLE, 1024, 4>, 1024);
+    if (FIT == kTiny || kp > (sizeof(E) == 2 ? 4096 : 2048) || k_bytes * 1024 >= (uint64_t(1) << 32) || pairs >= (1 << 20)) {
+        hipLaunchKernelGGL((int8_long_weights_kernel<E, FIT, 1024>), g64, dim3(1024), 0, s, W, K, N, kp, codes, scales);
+    } else if constexpr (FIT != kTiny) {
+        if (kp <= 256) once(int8_weights_kernel<E, FIT, 256, 1>, 256);
+        else if (kp <= 512) once(int8_weights_kernel<E, FIT, 256, 2>, 256);
+        else if (kp <= 1024) once(int8_weights_kernel<E, FIT, 512, 2>, 512);
+        else if (kp <= 2048) once(int8_weights_kernel<E, FIT, 512, 4>, 512);
+        else if constexpr (sizeof(E) == 2) once(int8_weights_kernel<E, FIT, 1024, 4>, 1024);
     }
 }
 
 template <class E>
 void weights_any(const void *W, int T, int K, int N, void *codes, float *scales, hipStream_t s)
 {
-    if (whole_vectors(N)) weights_of<E, true>((const E *)W, T, K, N, (uint8_t *)codes, scales, s);
-    else weights_of<E, false>((const E *)W, T, K, N, (uint8_t *)codes, scales, s);
+    const Fit fit = fit_of(N);
+    if (fit == kWhole) weights_of<E, kWhole>((const E *)W, T, K, N, (uint8_t *)codes, scales, s);
+    else if (fit == kEnds) weights_of<E, kEnds>((const E *)W, T, K, N, (uint8_t *)codes, scales, s);
+    else weights_of<E, kTiny>((const E *)W, T, K, N, (uint8_t *)codes, scales, s);
 }
 
 }  // namespace

@@ -55,7 +55,7 @@ __device__ __forceinline__ float inverse_rms(double squares, int cols, double ep
 }
 
 // L threads hold a row, NV vectors of eight columns each.
-template <class H, bool X32, bool R32, bool WHOLE, int L, int NV>
+template <class H, bool X32, bool R32, Fit FIT, int L, int NV>
 __global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
 {
 #pragma clang fp contract(off)
@@ -68,8 +68,8 @@ __global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
     if (row >= a.rows) return;                       // all lanes of a row
     const int lane = threadIdx.x % L;
 
-    Eight<XT, WHOLE> x[NV];
-    Eight<RT, WHOLE> in[NV];
+    Eight<XT, FIT> x[NV];
+    Eight<RT, FIT> in[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int c = (v * L + lane) * 8;
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
     if (a.drop.rng) gen.init(a.drop);
     float r[NV][8], w[NV][8];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight<H, WHOLE>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
+    for (int v = 0; v < NV; ++v) load_weight<H, FIT>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
     double squares = 0;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
             res[i] = a.res ? in[v].at(i) : 0.0f;
         }
         sum8<RT>(a, gen, row, c, f, res, r[v]);
-        if (a.sum) store8<RT, WHOLE>(a.sum, row * a.lds, r[v], c, a.cols);
+        if (a.sum) store8<RT, FIT>(a.sum, row * a.lds, r[v], c, a.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)r[v][i], (double)r[v][i], squares);
     }
@@ -114,8 +114,8 @@ __global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * L + lane) * 8;
-            if (a.out == kRowsF32) store8<float, WHOLE>(a.Y, row * a.ldy, r[v], c, a.cols);
-            else store8<H, WHOLE>(a.Y, row * a.ldy, r[v], c, a.cols);
+            if (a.out == kRowsF32) store8<float, FIT>(a.Y, row * a.ldy, r[v], c, a.cols);
+            else store8<H, FIT>(a.Y, row * a.ldy, r[v], c, a.cols);
         }
         return;
     }
@@ -173,8 +173,8 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     Philox gen;
     if (a.drop.rng) gen.init(a.drop);
     auto sum = [&](int c, float (&r)[8]) {
-        Eight<XT, false> x;
-        Eight<RT, false> in;
+        Eight<XT, kEnds> x;
+        Eight<RT, kEnds> in;
         x.load((const XT *)a.X + row * a.ldx, c, a.cols);
         if (a.res) in.load((const RT *)a.res + row * a.ldr, c, a.cols);
         x.settle(c, a.cols);
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     auto again = [&](int c, float s, float (&y)[8]) {       // the norm's output in fp32, zero behind the columns
         float w[8];
         if (a.sum) {
-            Eight<RT, false> in;
+            Eight<RT, kEnds> in;
             in.load((const RT *)a.sum + row * a.lds, c, a.cols);
             in.settle(c, a.cols);
 #pragma unroll
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
         } else {
             sum(c, y);
         }
-        load_weight<H, false>(a.w, a.w32, c, a.cols, w);
+        load_weight<H, kEnds>(a.w, a.w32, c, a.cols, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = c + i < a.cols ? y[i] * s * w[i] : 0.0f;
     };
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
         float r[8];
         sum(c, r);
-        if (a.sum) store8<RT, false>(a.sum, row * a.lds, r, c, a.cols);
+        if (a.sum) store8<RT, kEnds>(a.sum, row * a.lds, r, c, a.cols);
 #pragma unroll
         for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)r[i], (double)r[i], squares);
     }
@@ -230,8 +230,8 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     for (int c = threadIdx.x * 8; c < kp; c += 8192) {
         float y[8];
         again(c, s, y);
-        if (a.out == kRowsHalf) store8<H, false>(a.Y, row * a.ldy, y, c, a.cols);
-        else if (a.out == kRowsF32) store8<float, false>(a.Y, row * a.ldy, y, c, a.cols);
+        if (a.out == kRowsHalf) store8<H, kEnds>(a.Y, row * a.ldy, y, c, a.cols);
+        else if (a.out == kRowsF32) store8<float, kEnds>(a.Y, row * a.ldy, y, c, a.cols);
         else if (a.out == kRowsInt8) store_int8(codes + c, y, inverse, scale != scale);
         else {      // kp is whole blocks: the 16 lanes of a block are here together
             uint32_t top = 0;
@@ -245,11 +245,11 @@ __global__ __launch_bounds__(1024) void rms_norm_long_kernel(NormArgs a)
     if (a.out == kRowsE4m3 && (int)threadIdx.x < fp8_scales(a.cols) - (kp >> 7)) sc[(kp >> 7) + threadIdx.x] = 127;
 }
 
-template <class H, bool X32, bool R32, bool WHOLE, int L, int NV>
+template <class H, bool X32, bool R32, Fit FIT, int L, int NV>
 void launch_rows(const NormArgs &a, hipStream_t s)
 {
     constexpr int PER = L > 64 ? 1 : 256 / L;
-    hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, WHOLE, L, NV>), flat_grid((a.rows + PER - 1) / PER), dim3(L > 64 ? L : 256), 0, s, a);
+    hipLaunchKernelGGL((rms_norm_kernel<H, X32, R32, FIT, L, NV>), flat_grid((a.rows + PER - 1) / PER), dim3(L > 64 ? L : 256), 0, s, a);
 }
 
 // The threads of a row: as many as it has vectors of eight, a power of two, which measured faster than fewer threads with
@@ -257,29 +257,33 @@ void launch_rows(const NormArgs &a, hipStream_t s)
 // 41.4, 64 of two 42.8; 8000 x 4096 512 threads 41.9, 256 of two 43.4; 4000 x 8192 1024 threads 44.0, 256 of four 48.5; 8 x 1000
 // 2.6 and 3.2).  Two vectors a thread where rows end inside one (80 000 x 333 53.9 us, 64 threads 60.0; 30 000 x 1001
 // 50.4, 128 threads 54.7) and for long rows of codes (4000 x 8192 into int8 42.4, 1024 threads 44.6).
-template <class H, bool X32, bool R32, bool WHOLE>
+template <class H, bool X32, bool R32, Fit FIT>
 void launch_cols(const NormArgs &a, hipStream_t s)
 {
     const bool codes = a.out > kRowsF32;
     const int cols = codes ? fp8_width(a.cols) : a.cols;
-    if (cols <= 64) launch_rows<H, X32, R32, WHOLE, 8, 1>(a, s);
-    else if (cols <= 128) launch_rows<H, X32, R32, WHOLE, 16, 1>(a, s);
-    else if (cols <= 256) launch_rows<H, X32, R32, WHOLE, 32, 1>(a, s);
-    else if (cols <= 512) launch_rows<H, X32, R32, WHOLE, WHOLE ? 64 : 32, WHOLE ? 1 : 2>(a, s);
-    else if (cols <= 1024) launch_rows<H, X32, R32, WHOLE, WHOLE ? 128 : 64, WHOLE ? 1 : 2>(a, s);
-    else if (cols <= 2048) launch_rows<H, X32, R32, WHOLE, 256, 1>(a, s);
-    else if (cols <= 4096) launch_rows<H, X32, R32, WHOLE, 512, 1>(a, s);
-    else if (cols <= 8192 && !codes) launch_rows<H, X32, R32, WHOLE, 1024, 1>(a, s);
-    else if (cols <= 8192) launch_rows<H, X32, R32, WHOLE, 512, 2>(a, s);
-    else if (cols <= 16384) launch_rows<H, X32, R32, WHOLE, 1024, 2>(a, s);
-    else if (cols <= 32768) launch_rows<H, X32, R32, WHOLE, 1024, 4>(a, s);
+    if (cols <= 64) launch_rows<H, X32, R32, FIT, 8, 1>(a, s);
+    else if (cols <= 128) launch_rows<H, X32, R32, FIT, 16, 1>(a, s);
+    else if (cols <= 256) launch_rows<H, X32, R32, FIT, 32, 1>(a, s);
+    else if (cols <= 512) launch_rows<H, X32, R32, FIT, FIT == kWhole ? 64 : 32, FIT == kWhole ? 1 : 2>(a, s);
+    else if (cols <= 1024) launch_rows<H, X32, R32, FIT, FIT == kWhole ? 128 : 64, FIT == kWhole ? 1 : 2>(a, s);
+    else if (cols <= 2048) launch_rows<H, X32, R32, FIT, 256, 1>(a, s);
+    else if (cols <= 4096) launch_rows<H, X32, R32, FIT, 512, 1>(a, s);
+    else if (cols <= 8192 && !codes) launch_rows<H, X32, R32, FIT, 1024, 1>(a, s);
+    else if (cols <= 8192) launch_rows<H, X32, R32, FIT, 512, 2>(a, s);
+    else if (cols <= 16384) launch_rows<H, X32, R32, FIT, 1024, 2>(a, s);
+    else if (cols <= 32768) launch_rows<H, X32, R32, FIT, 1024, 4>(a, s);
     else hipLaunchKernelGGL((rms_norm_long_kernel<H, X32, R32>), flat_grid(a.rows), dim3(1024), 0, s, a);
 }
 
 template <class H, bool X32, bool R32>
 void launch_types(const NormArgs &a, hipStream_t s)
 {
-    whole_vectors(a.cols) ? launch_cols<H, X32, R32, true>(a, s) : launch_cols<H, X32, R32, false>(a, s);
+    const Fit fit = fit_of(a.cols);
+    if (fit == kWhole) launch_cols<H, X32, R32, kWhole>(a, s);
+    else if (fit == kEnds) launch_cols<H, X32, R32, kEnds>(a, s);
+    else if (a.out <= kRowsF32) launch_rows<H, X32, R32, kTiny, 8, 1>(a, s);
+    else launch_rows<H, X32, R32, kTiny, 16, 1>(a, s);
 }
 
 template <class H>

@@ -25,18 +25,18 @@ int64_t groups_of(int64_t rows, int cols)
     return std::min<int64_t>((rows + per - 1) / per, cols <= 2048 ? 1024 : cols <= 4096 ? 512 : 256);
 }
 
-template <class H, bool WHOLE>
+template <class H, Fit FIT>
 __device__ __forceinline__ void store_typed(void *base, bool f32, int64_t row, const float (&x)[8], int c, int cols)
 {
-    if (f32) store8<float, WHOLE>(base, row, x, c, cols);
-    else store8<H, WHOLE>(base, row, x, c, cols);
+    if (f32) store8<float, FIT>(base, row, x, c, cols);
+    else store8<H, FIT>(base, row, x, c, cols);
 }
 
 // dX of eight columns from dr, and both stored.
-template <class H, class RT, bool WHOLE, bool DROP>
+template <class H, class RT, Fit FIT, bool DROP>
 __device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const Philox &gen, int64_t row, int c, float (&dr)[8])
 {
-    if (a.dres) store8<RT, WHOLE>(a.dres, row * a.lddr, dr, c, a.cols);
+    if (a.dres) store8<RT, FIT>(a.dres, row * a.lddr, dr, c, a.cols);
     if (!a.dX) return;
     if constexpr (DROP) {
         uint32_t word[8];
@@ -44,10 +44,10 @@ __device__ __forceinline__ void store_gradients(const NormBackwardArgs &a, const
 #pragma unroll
         for (int i = 0; i < 8; ++i) dr[i] = word[i] > a.drop.below ? dr[i] * a.drop.factor : 0.0f;
     }
-    store_typed<H, WHOLE>(a.dX, a.dx32, row * a.lddx, dr, c, a.cols);
+    store_typed<H, FIT>(a.dX, a.dx32, row * a.lddx, dr, c, a.cols);
 }
 
-template <class H, bool DY32, bool R32, bool WHOLE, bool DROP, int L, int NV>
+template <class H, bool DY32, bool R32, Fit FIT, bool DROP, int L, int NV>
 __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(NormBackwardArgs a)
 {
 #pragma clang fp contract(off)
@@ -61,11 +61,11 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
     if (DROP) gen.init(a.drop);
     float w[NV][8], dw[NV][8] = {};
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load_weight<H, WHOLE>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
+    for (int v = 0; v < NV; ++v) load_weight<H, FIT>(a.w, a.w32, (v * L + lane) * 8, a.cols, w[v]);
     int turn = 0;
     for (int64_t row = blockIdx.x * (int64_t)PER + group; row < a.rows; row += gridDim.x * (int64_t)PER, turn ^= 1) {
-        Eight<YT, WHOLE> dy[NV];
-        Eight<RT, WHOLE> r[NV], ds[NV];
+        Eight<YT, FIT> dy[NV];
+        Eight<RT, FIT> r[NV], ds[NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * L + lane) * 8;
@@ -108,14 +108,14 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
                 dr[i] = s * (g - n * mean);
                 if (a.dsum) dr[i] += ds[v].at(i);
             }
-            store_gradients<H, RT, WHOLE, DROP>(a, gen, row, c, dr);
+            store_gradients<H, RT, FIT, DROP>(a, gen, row, c, dr);
         }
     }
     if (!a.dW) return;
     float *out = a.ws + blockIdx.x * (int64_t)a.cols;
     if constexpr (PER == 1) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) store8<float, WHOLE>(out, 0, dw[v], (v * L + lane) * 8, a.cols);
+        for (int v = 0; v < NV; ++v) store8<float, FIT>(out, 0, dw[v], (v * L + lane) * 8, a.cols);
     } else {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -151,12 +151,12 @@ __global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwa
         const float s = a.rstd[row];
         double dot = 0;
         for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
-            Eight<YT, false> dy;
-            Eight<RT, false> r;
+            Eight<YT, kEnds> dy;
+            Eight<RT, kEnds> r;
             float w[8], dw[8];
             dy.load((const YT *)a.dY + row * a.lddy, c, a.cols);
             r.load((const RT *)a.r + row * a.ldr, c, a.cols);
-            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
+            load_weight<H, kEnds>(a.w, a.w32, c, a.cols, w);
             dy.settle(c, a.cols);
             r.settle(c, a.cols);
             if (IN_LDS) {
@@ -176,18 +176,18 @@ __global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwa
                 *(f32x4 *)(held + c) = *(const f32x4 *)dw;
                 *(f32x4 *)(held + c + 4) = *(const f32x4 *)(dw + 4);
             } else if (out) {
-                store8<float, false>(out, 0, dw, c, a.cols);
+                store8<float, kEnds>(out, 0, dw, c, a.cols);
             }
         }
         const float mean = (float)(row_sum<1024>(dot, sums[turn]) / a.cols);
         for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
-            Eight<YT, false> dy;
-            Eight<RT, false> r, ds;
+            Eight<YT, kEnds> dy;
+            Eight<RT, kEnds> r, ds;
             float w[8], dr[8];
             dy.load((const YT *)a.dY + row * a.lddy, c, a.cols);
             r.load((const RT *)a.r + row * a.ldr, c, a.cols);
             if (a.dsum) ds.load((const RT *)a.dsum + row * a.ldds, c, a.cols);
-            load_weight<H, false>(a.w, a.w32, c, a.cols, w);
+            load_weight<H, kEnds>(a.w, a.w32, c, a.cols, w);
             dy.settle(c, a.cols);
             r.settle(c, a.cols);
             if (a.dsum) ds.settle(c, a.cols);
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(1024) void rms_norm_backward_long_kernel(NormBackwa
                 dr[i] = s * (g - n * mean);
                 if (a.dsum) dr[i] += ds.at(i);
             }
-            store_gradients<H, RT, false, DROP>(a, gen, row, c, dr);
+            store_gradients<H, RT, kEnds, DROP>(a, gen, row, c, dr);
         }
     }
 }
@@ -229,8 +229,10 @@ template <class H, bool DY32, bool R32, bool DROP, int L, int NV>
 void launch_shape(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
 {
     const dim3 g((uint32_t)groups), b(L > 256 ? L : 256);
-    if (whole_vectors(a.cols)) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, true, DROP, L, NV>), g, b, 0, s, a);
-    else hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, false, DROP, L, NV>), g, b, 0, s, a);
+    const Fit fit = fit_of(a.cols);
+    if (fit == kWhole) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kWhole, DROP, L, NV>), g, b, 0, s, a);
+    else if (fit == kEnds) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kEnds, DROP, L, NV>), g, b, 0, s, a);
+    else if constexpr (L == 8) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kTiny, DROP, L, NV>), g, b, 0, s, a);
 }
 
 template <class H, bool DY32, bool R32, bool DROP>
