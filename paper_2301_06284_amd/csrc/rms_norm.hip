@@ -255,18 +255,21 @@ void launch_rows(const NormArgs &a, hipStream_t s)
 // The threads of a row: as many as it has vectors of eight, a power of two, which measured faster than fewer threads with
 // several vectors (bf16, with residual and sum: 60 000 x 512 64 threads 39.2 us, 32 of two 43.2; 30 000 x 1000 128 threads
 // 41.4, 64 of two 42.8; 8000 x 4096 512 threads 41.9, 256 of two 43.4; 4000 x 8192 1024 threads 44.0, 256 of four 48.5; 8 x 1000
-// 2.6 and 3.2).  Two vectors a thread where rows end inside one (80 000 x 333 53.9 us, 64 threads 60.0; 30 000 x 1001
-// 50.4, 128 threads 54.7) and for long rows of codes (4000 x 8192 into int8 42.4, 1024 threads 44.6).
+// 2.6 and 3.2).  Two vectors a thread for many rows that end inside one (80 000 x 333 45.2 us, 64 threads 46.3; 30 000 x 1001
+// 40.5, 128 threads 46.7; but 1000 x 333 3.6 and 2.8) and for long rows of codes (4000 x 8192 into int8 42.4, 1024 threads 44.6).
 template <class H, bool X32, bool R32, Fit FIT>
 void launch_cols(const NormArgs &a, hipStream_t s)
 {
     const bool codes = a.out > kRowsF32;
     const int cols = codes ? fp8_width(a.cols) : a.cols;
+    if constexpr (FIT == kEnds)
+        if (a.rows > 4096 && cols > 256 && cols <= 1024)
+            return cols <= 512 ? launch_rows<H, X32, R32, FIT, 32, 2>(a, s) : launch_rows<H, X32, R32, FIT, 64, 2>(a, s);
     if (cols <= 64) launch_rows<H, X32, R32, FIT, 8, 1>(a, s);
     else if (cols <= 128) launch_rows<H, X32, R32, FIT, 16, 1>(a, s);
     else if (cols <= 256) launch_rows<H, X32, R32, FIT, 32, 1>(a, s);
-    else if (cols <= 512) launch_rows<H, X32, R32, FIT, FIT == kWhole ? 64 : 32, FIT == kWhole ? 1 : 2>(a, s);
-    else if (cols <= 1024) launch_rows<H, X32, R32, FIT, FIT == kWhole ? 128 : 64, FIT == kWhole ? 1 : 2>(a, s);
+    else if (cols <= 512) launch_rows<H, X32, R32, FIT, 64, 1>(a, s);
+    else if (cols <= 1024) launch_rows<H, X32, R32, FIT, 128, 1>(a, s);
     else if (cols <= 2048) launch_rows<H, X32, R32, FIT, 256, 1>(a, s);
     else if (cols <= 4096) launch_rows<H, X32, R32, FIT, 512, 1>(a, s);
     else if (cols <= 8192 && !codes) launch_rows<H, X32, R32, FIT, 1024, 1>(a, s);

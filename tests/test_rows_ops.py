@@ -202,6 +202,12 @@ def test_norm(cols, x_t, res_t, w_t, y_t):
         check_norm(rows, cols, x_t, res_t, w_t, y_t)
 
 
+@pytest.mark.parametrize("cols", [257, 333, 511, 513, 1001, 1023])
+@pytest.mark.parametrize("x_t,res_t,w_t,y_t", [("bf16", "bf16", "bf16", "bf16"), ("fp16", "fp32", "fp32", "e4m3"), ("fp32", "fp32", "fp32", "int8")])
+def test_norm_of_many_rows_that_end_inside_a_vector(cols, x_t, res_t, w_t, y_t):
+    check_norm(4099, cols, x_t, res_t, w_t, y_t, p=0.1 if y_t == "bf16" else 0.0)
+
+
 @pytest.mark.parametrize("x_t,res_t,w_t,y_t", [("bf16", "", "bf16", "bf16"), ("fp16", "", "", "fp32"), ("fp32", "bf16", "bf16", "bf16"),
                                                ("fp32", "", "fp16", "fp16"), ("bf16", "bf16", "fp32", "fp32"),
                                                ("fp32", "fp16", "fp32", "fp32"), ("bf16", "fp32", "", "fp32"),
