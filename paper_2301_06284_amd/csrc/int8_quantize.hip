@@ -1,8 +1,11 @@
 // int8_quantize.hip -- rows and weights as 8-bit integers, with a scale for each row (token) and for each
 // output of a type's weight (channel): scale = max |x| / 127, code = round(x (1 / scale)).
 //
-// A row stays in registers between its maximum and its codes.  A weight's columns are read twice, for
-// their maxima and for the codes, which turn over in LDS to rows of k.
+// A row stays in registers between its maximum and its codes, and so do a weight's columns up to 4096 k in 16 bits (2048 in
+// fp32); longer ones are read twice.  The weights' codes turn over in LDS to rows of k.
+//
+// Bound by memory.  Measured, bf16: rows 8192 x 4096 17 us (5.8 TB/s), 8 rows of 2048 2.6; weights 16 x 2048 x 1536
+// 39 us (3.8 TB/s: every workgroup loads first and stores last), 4096 x 4096 18, 4 x 5000 x 3000 (read twice) 74.
 #include <algorithm>
 
 #include "rows.h"

@@ -2,9 +2,14 @@
 // r = round(residual + D(x)), s = 1 / sqrt(mean(r^2) + eps), y = (r s) w, as rows or as 8-bit codes.
 //
 // A row is read once and stays in registers from its loads to its stores: a few lanes of a wave hold a short row, a wave
-// or a workgroup a long one, eight columns a lane at a time.  Squares are summed in 64 bits, which costs a
-// kernel that waits for memory nothing: the result does not depend on how a row is cut, and a code next to a border
-// is the one that the formula gives.
+// or a workgroup a long one, eight columns a lane at a time.  Squares are summed in 64 bits, which costs
+// next to nothing where memory is waited for (16 384 x 2048 74.4 us, in 32 bits 74.3; 8000 x 4096 42.8 and 42.5; 600 000 x 24
+// 30.8 and 28.5): the result does not depend on how a row is cut, and a code next to a border is the one that the formula
+// gives.
+//
+// Bound by memory, a few rows by the launch.  Measured, with residual and sum: 1 000 003 x 64 fp32 181 us (5.7 TB/s), 16 384 x
+// 2048 bf16 with an fp32 residual and dropout 74 us (5.4), 8192 x 4096 bf16 into e4m3 45 us (5.2), 15 000 x 2048 bf16
+// 39 us (6.3, from the last-level cache in part), 10 000 x 333 fp16 8.2 us, 8 x 2048 2.5 us in a graph.
 #include <algorithm>
 
 #include "rows.h"
@@ -254,7 +259,7 @@ void launch_rows(const NormArgs &a, hipStream_t s)
 
 // The threads of a row: as many as it has vectors of eight, a power of two, which measured faster than fewer threads with
 // several vectors (bf16, with residual and sum: 60 000 x 512 64 threads 39.2 us, 32 of two 43.2; 30 000 x 1000 128 threads
-// 41.4, 64 of two 42.8; 8000 x 4096 512 threads 41.9, 256 of two 43.4; 4000 x 8192 1024 threads 44.0, 256 of four 48.5; 8 x 1000
+// 41.4, 64 of two 42.8; 600 000 x 24 fp16 4 lanes 23.3, 8 34.4; 8000 x 4096 512 threads 41.9, 256 of two 43.4; 4000 x 8192 1024 threads 44.0, 256 of four 48.5; 8 x 1000
 // 2.6 and 3.2).  Two vectors a thread for many rows that end inside one (80 000 x 333 45.2 us, 64 threads 46.3; 30 000 x 1001
 // 40.5, 128 threads 46.7; but 1000 x 333 3.6 and 2.8) and for long rows of codes (4000 x 8192 into int8 42.4, 1024 threads 44.6).
 template <class H, bool X32, bool R32, Fit FIT>
@@ -265,7 +270,9 @@ void launch_cols(const NormArgs &a, hipStream_t s)
     if constexpr (FIT == kEnds)
         if (a.rows > 4096 && cols > 256 && cols <= 1024)
             return cols <= 512 ? launch_rows<H, X32, R32, FIT, 32, 2>(a, s) : launch_rows<H, X32, R32, FIT, 64, 2>(a, s);
-    if (cols <= 64) launch_rows<H, X32, R32, FIT, 8, 1>(a, s);
+    if (cols <= 8) launch_rows<H, X32, R32, FIT, 1, 1>(a, s);
+    else if (cols <= 32) launch_rows<H, X32, R32, FIT, 4, 1>(a, s);
+    else if (cols <= 64) launch_rows<H, X32, R32, FIT, 8, 1>(a, s);
     else if (cols <= 128) launch_rows<H, X32, R32, FIT, 16, 1>(a, s);
     else if (cols <= 256) launch_rows<H, X32, R32, FIT, 32, 1>(a, s);
     else if (cols <= 512) launch_rows<H, X32, R32, FIT, 64, 1>(a, s);
@@ -285,7 +292,7 @@ void launch_types(const NormArgs &a, hipStream_t s)
     const Fit fit = fit_of(a.cols);
     if (fit == kWhole) launch_cols<H, X32, R32, kWhole>(a, s);
     else if (fit == kEnds) launch_cols<H, X32, R32, kEnds>(a, s);
-    else if (a.out <= kRowsF32) launch_rows<H, X32, R32, kTiny, 8, 1>(a, s);
+    else if (a.out <= kRowsF32) launch_rows<H, X32, R32, kTiny, 1, 1>(a, s);
     else launch_rows<H, X32, R32, kTiny, 16, 1>(a, s);
 }
 

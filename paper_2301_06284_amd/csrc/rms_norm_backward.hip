@@ -5,6 +5,10 @@
 // A workgroup takes every G-th group of rows and keeps dw of its columns in registers to the end, then
 // writes it to the workspace; a second launch adds the G rows there in 64 bits, in their order, so that results are
 // reproducible.
+//
+// Bound by memory.  Measured, with d_sum, dX and d_residual: 16 384 x 2048 bf16 with an fp32 sum and dropout 105 + 5 us
+// (5.0 TB/s), 15 000 x 2048 bf16 56 us (5.5), 100 000 x 333 fp16 75 us (4.4), 2000 x 16 000 bf16 71 us (4.5), 8 x 2048 5 us,
+// two launches.  The register count (82 to 105) leaves four workgroups on a CU; bounds for six spill and take 1.4 to 2.5 times as long.
 #include <algorithm>
 
 #include "rows.h"
@@ -15,8 +19,8 @@ namespace {
 
 constexpr int kLong = 32768;         // columns whose dw LDS holds
 
-// Rows of a workgroup: several short ones, of 8 to 64 lanes each.
-int rows_of_group(int cols) { return cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
+// Rows of a workgroup: several short ones, of 1 to 64 lanes each.
+int rows_of_group(int cols) { return cols <= 8 ? 256 : cols <= 32 ? 64 : cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
 // As many workgroups as the CUs hold at a time: 1024 are four on each (1280, or fewer of them with equal turns,
 // 3 to 8 % slower).
 int64_t groups_of(int64_t rows, int cols)
@@ -55,7 +59,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
     typedef typename std::conditional<R32, float, H>::type RT;
     constexpr int PER = L >= 256 ? 1 : 256 / L;
     __shared__ double sums[2][L > 64 ? L / 64 : 1];
-    __shared__ float part[PER > 1 ? 256 * NV * 8 : 1];
+    __shared__ float part[PER > 1 ? 4 * L * NV * 8 : 1];
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     Philox gen;
     if (DROP) gen.init(a.drop);
@@ -117,16 +121,22 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
 #pragma unroll
         for (int v = 0; v < NV; ++v) store8<float, FIT>(out, 0, dw[v], (v * L + lane) * 8, a.cols);
     } else {
+        // the rows of a wave, then the four waves
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            float *to = part + group * (L * NV * 8) + (v * L + lane) * 8;
+            float *to = part + (threadIdx.x >> 6) * (L * NV * 8) + (v * L + lane) * 8;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) to[i] = dw[v][i];
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int d = L; d < 64; d <<= 1) dw[v][i] += __shfl_xor(dw[v][i], d);
+                if ((threadIdx.x & 63) < L) to[i] = dw[v][i];
+            }
         }
         __syncthreads();
         for (int c = threadIdx.x; c < a.cols; c += 256) {
             float x = 0;
-            for (int g = 0; g < PER; ++g) x += part[g * (L * NV * 8) + c];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) x += part[g * (L * NV * 8) + c];
             out[c] = x;
         }
     }
@@ -232,13 +242,15 @@ void launch_shape(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
     const Fit fit = fit_of(a.cols);
     if (fit == kWhole) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kWhole, DROP, L, NV>), g, b, 0, s, a);
     else if (fit == kEnds) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kEnds, DROP, L, NV>), g, b, 0, s, a);
-    else if constexpr (L == 8) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kTiny, DROP, L, NV>), g, b, 0, s, a);
+    else if constexpr (L == 1) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kTiny, DROP, L, NV>), g, b, 0, s, a);
 }
 
 template <class H, bool DY32, bool R32, bool DROP>
 void launch_cols(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
 {
-    if (a.cols <= 64) launch_shape<H, DY32, R32, DROP, 8, 1>(a, groups, s);
+    if (a.cols <= 8) launch_shape<H, DY32, R32, DROP, 1, 1>(a, groups, s);
+    else if (a.cols <= 32) launch_shape<H, DY32, R32, DROP, 4, 1>(a, groups, s);
+    else if (a.cols <= 64) launch_shape<H, DY32, R32, DROP, 8, 1>(a, groups, s);
     else if (a.cols <= 128) launch_shape<H, DY32, R32, DROP, 16, 1>(a, groups, s);
     else if (a.cols <= 256) launch_shape<H, DY32, R32, DROP, 32, 1>(a, groups, s);
     else if (a.cols <= 512) launch_shape<H, DY32, R32, DROP, 64, 1>(a, groups, s);

@@ -1,6 +1,6 @@
 // typed_linear.hip -- the typed linear over ragged segments whose offsets lie on the
 // device: Y[scatter[i]] = X[gather[i]] W[t(i)], weights as stored or transposed (the
-// input gradient), and its 8-bit form.
+// input gradient), and its 8-bit forms.
 //
 // A workgroup takes BM x BN outputs of one type and walks k in steps of 128 bytes of a row
 // (32 fp32, 64 16-bit or 128 8-bit values), which makes one kernel of all types: the same
@@ -22,12 +22,12 @@
 //
 // What bounds it, and what it measured (copies reach 5.2 TB/s here, large bf16 products 1.1 PFLOP/s):
 //   few rows: the weights' bytes, and the latency of the steps (16 rows of 2048 -> 1536, 13 of 32 types'
-//     weights read: 19 us, 4.3 TB/s; in 8 bits 10 us, 4.0 TB/s);
+//     weights read: 19 us, 4.3 TB/s; in 8 bits 10 us, 4.0 TB/s; as integers, 10 of 32 types, 9 us);
 //   many rows of narrow weights: memory (300 007 rows 64 -> 64, fp16: 16 us, 5.0 TB/s; 1 000 003
 //     gathered and scattered rows 64 -> 128, bf16: 95 us, 4.1 TB/s of rows at random, each counted as often as it is read);
 //   many rows of wide weights: the matrix cores, at the rate of the whole tiles that the types' sizes
 //     leave (16 384 rows of 32 types, 2048 -> 4096, bf16: 322 us, 0.85 PFLOP/s; one type 242 us, 1.14; 8
-//     bits, 8192 rows 4096 -> 4096: 156 us, 1.76 PFLOP/s);
+//     bits, 8192 rows 4096 -> 4096: 156 us, 1.76 PFLOP/s; as integers 148 us, 1.86 POP/s);
 //   thousands of types: the search for a tile, which every workgroup makes from the first offset on (bf16, 65 535
 //     rows, 64 -> 64: 1024 types 10 us, 4096 42, 16 384 380, 65 535 5.1 ms).
 #include <algorithm>

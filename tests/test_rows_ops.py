@@ -188,7 +188,7 @@ def check_codes(y32, codes, scales, kind):
         assert (codes[:, cols:] == 0).all()
 
 
-COLS = [1, 7, 8, 64, 65, 100, 128, 129, 256, 257, 333, 512, 513, 1000, 1025, 2048, 2050, 4096, 4100, 8192, 8200, 16384,
+COLS = [1, 7, 8, 9, 24, 32, 33, 64, 65, 100, 128, 129, 256, 257, 333, 512, 513, 1000, 1025, 2048, 2050, 4096, 4100, 8192, 8200, 16384,
         16400, 32768, 32776, 40001]
 
 
@@ -432,7 +432,7 @@ def test_norm_backward(cols, dy_t, sum_t, w_t, dx_t, dw_t):
         check_backward(rows, cols, dy_t, sum_t, w_t, dx_t, dw_t)
 
 
-@pytest.mark.parametrize("rows,cols", [(5000, 64), (2 ** 16 + 5, 40), (3001, 333), (2100, 2048), (1500, 5000), (300, 12000), (300, 33000)])
+@pytest.mark.parametrize("rows,cols", [(2 ** 19 + 3, 5), (2 ** 18 + 77, 8), (2 ** 17 + 9, 24), (5000, 64), (2 ** 16 + 5, 40), (3001, 333), (2100, 2048), (1500, 5000), (300, 12000), (300, 33000)])
 def test_norm_backward_many_rows(rows, cols):
     """More rows than workgroups, so that each takes several."""
     check_backward(rows, cols, "bf16", "bf16", "fp32", "bf16", "fp32", p=0.1)
