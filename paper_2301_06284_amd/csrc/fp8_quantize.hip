@@ -18,28 +18,6 @@ namespace rgnn {
 
 namespace {
 
-// scale byte of a block whose largest magnitude has these bits
-__device__ __forceinline__ int scale_byte(uint32_t top)
-{
-    if (top >= 0x7F800000u) return 255;
-    const int e = (int)((top + 0x1FFFFFu) >> 23) - 8;
-    return e < 1 ? 1 : e;
-}
-// 1 / scale, exact; NaN for byte 255
-__device__ __forceinline__ float scale_inverse(int byte)
-{
-    return byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(254 - byte) << 23);
-}
-
-// four codes of four values (|x| <= 448, or NaN)
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
-{
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
-}
-
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
-
 // Eight values of a row from column k on, zero behind K.
 template <class E, bool VEC>
 __device__ __forceinline__ void load8(const E *row, int64_t k, int K, float x[8])
@@ -72,15 +50,15 @@ __global__ __launch_bounds__(256) void fp8_rows_kernel(const E *X, int64_t rows,
     load8<E, VEC>(X + row * ldx, k, K, x);
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, magnitude(x[i]));
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude_bits(x[i]));
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    const int byte = k < Kp ? scale_byte(top) : 127;
+    const int byte = k < Kp ? e4m3_scale_byte(top) : 127;
     if (k < Kp) {
-        const float inv = scale_inverse(byte);
+        const float inv = e4m3_scale_inverse(byte);
         uint2 q;
-        q.x = codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
-        q.y = codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
+        q.x = e4m3_codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+        q.y = e4m3_codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
         if (byte == 255) q = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
         *(uint2 *)(codes + row * Kp + k) = q;
     }
@@ -112,21 +90,21 @@ __global__ __launch_bounds__(256) void fp8_weights_kernel(const E *W, int K, int
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[i][j] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, magnitude(x[i][j]));
+        for (int j = 0; j < 8; ++j) top = max(top, magnitude_bits(x[i][j]));
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     if ((tid & 63) == 0) tops[tid >> 6] = top;
     __syncthreads();
     top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
-    const int byte = scale_byte(top);
-    const float inv = scale_inverse(byte);
+    const int byte = e4m3_scale_byte(top);
+    const float inv = e4m3_scale_inverse(byte);
     if (tid == 0) sc[kb] = (uint8_t)byte;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         uint2 q;
-        q.x = codes4(x[0][j] * inv, x[1][j] * inv, x[2][j] * inv, x[3][j] * inv);
-        q.y = codes4(x[4][j] * inv, x[5][j] * inv, x[6][j] * inv, x[7][j] * inv);
+        q.x = e4m3_codes4(x[0][j] * inv, x[1][j] * inv, x[2][j] * inv, x[3][j] * inv);
+        q.y = e4m3_codes4(x[4][j] * inv, x[5][j] * inv, x[6][j] * inv, x[7][j] * inv);
         if (byte == 255) q = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
         *(uint2 *)(turn + ((tid & 15) * 8 + j) * 144 + (tid >> 4) * 8) = q;
     }

@@ -139,6 +139,30 @@ __device__ __forceinline__ f32x4 mma16<F32>(i32x4 a, i32x4 b, f32x4 c)
     return c;
 }
 
+// ---------------------------------------------------------------- 8-bit codes with block scales
+
+// Scale byte of a block whose largest magnitude has these bits
+__device__ __forceinline__ int e4m3_scale_byte(uint32_t top)
+{
+    if (top >= 0x7F800000u) return 255;
+    const int e = (int)((top + 0x1FFFFFu) >> 23) - 8;
+    return e < 1 ? 1 : e;
+}
+// 1 / scale, exact; NaN for byte 255
+__device__ __forceinline__ float e4m3_scale_inverse(int byte)
+{
+    return byte == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(254 - byte) << 23);
+}
+
+// Four codes of four values (|x| <= 448, or NaN)
+__device__ __forceinline__ uint32_t e4m3_codes4(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+__device__ __forceinline__ uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
 // ---------------------------------------------------------------- tiles
 
 struct Piece {          // a workgroup's share: number `index` of type `type`'s pieces

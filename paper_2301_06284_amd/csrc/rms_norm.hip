@@ -18,24 +18,6 @@ namespace rgnn {
 
 namespace {
 
-// scale byte of a block whose largest magnitude has these bits (see rgnn_fp8_quantize_rows)
-__device__ __forceinline__ int e4m3_scale_byte(uint32_t top)
-{
-    if (top >= 0x7F800000u) return 255;
-    const int e = (int)((top + 0x1FFFFFu) >> 23) - 8;
-    return e < 1 ? 1 : e;
-}
-
-__device__ __forceinline__ void store_e4m3(uint8_t *codes, const float (&x)[8], int byte)
-{
-    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
-    uint2 q;
-    q.x = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[2] * inv, x[3] * inv, __builtin_amdgcn_cvt_pk_fp8_f32(x[0] * inv, x[1] * inv, 0, false), true);
-    q.y = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[6] * inv, x[7] * inv, __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * inv, x[5] * inv, 0, false), true);
-    if (byte == 255) q = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
-    *(uint2 *)codes = q;
-}
-
 // r of eight columns: the sum in fp32, the kept value's product not rounded before it, rounded to r's type.
 template <class RT>
 __device__ __forceinline__ void sum8(const NormArgs &a, const Philox &gen, int64_t row, int col, const float (&x)[8], const float (&res)[8],

@@ -322,7 +322,13 @@ struct Philox {
 
 // ---------------------------------------------------------------- 8-bit codes
 
-__device__ __forceinline__ uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+__device__ __forceinline__ void store_e4m3(uint8_t *codes, const float (&x)[8], int byte)
+{
+    const float inv = e4m3_scale_inverse(byte);
+    uint2 q = make_uint2(e4m3_codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv), e4m3_codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+    if (byte == 255) q = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+    *(uint2 *)codes = q;
+}
 
 // The scale of 8-bit integers whose largest magnitude has these bits: top / 127, at least 2^-126 (so that its inverse
 // is finite); NaN for an infinity or a NaN.

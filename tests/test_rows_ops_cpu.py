@@ -240,6 +240,34 @@ def test_norm_wrapper_checks_shapes(change, monkeypatch):
         rgnn.rms_norm(**args)
 
 
+def test_other_devices_are_refused():
+    """A stream of another device than the tensors', and tensors of another device than the current one."""
+    rgnn, _ = lib()
+
+    class Stream:
+        device_index, cuda_stream = 1, 0
+
+    class Tensor:
+        device = 0
+
+        def get_device(self):
+            return self.device
+
+    class Torch:
+        raw_stream = None
+
+        @staticmethod
+        def current():
+            return 0
+    with pytest.raises(ValueError):
+        rgnn._stream_of(Stream(), 0, Torch)
+    x = Tensor()
+    assert rgnn._device_of(x, Torch) == 0
+    for x.device in (1, -1):
+        with pytest.raises(ValueError):
+            rgnn._device_of(x, Torch)
+
+
 def test_tile_of_int8():
     """The 8-bit forms share their tiles."""
     rgnn, l = lib()
