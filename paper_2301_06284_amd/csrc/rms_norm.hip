@@ -106,40 +106,41 @@ __global__ __launch_bounds__(L > 64 ? L : 256) void rms_norm_kernel(NormArgs a)
         }
         return;
     }
-    // codes: what lies behind the columns is zero up to whole blocks of 128
-    const int kp = fp8_width(a.cols);
-    uint8_t *codes = (uint8_t *)a.Y + row * kp;
-    if (a.out == kRowsE4m3) {
-        const int ks = fp8_scales(a.cols);
-        uint8_t *sc = (uint8_t *)a.scales + row * ks;
+    if constexpr (L >= 16) {      // codes: what lies behind the columns is zero up to whole blocks of 128, 16 lanes or more
+        const int kp = fp8_width(a.cols);
+        uint8_t *codes = (uint8_t *)a.Y + row * kp;
+        if (a.out == kRowsE4m3) {
+            const int ks = fp8_scales(a.cols);
+            uint8_t *sc = (uint8_t *)a.scales + row * ks;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int c = (v * L + lane) * 8;
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max(top, c + i < a.cols ? magnitude_bits(r[v][i]) : 0);
+                const int byte = e4m3_scale_byte(lanes_max<16>(top));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[v][i] = c + i < a.cols ? r[v][i] : 0.0f;
+                if (c < kp) store_e4m3(codes + c, r[v], byte);
+                if (c < kp && (lane & 15) == 0) sc[c >> 7] = (uint8_t)byte;
+            }
+            if (lane < ks - (kp >> 7)) sc[(kp >> 7) + lane] = 127;
+            return;
+        }
+        uint32_t top = 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, (v * L + lane) * 8 + i < a.cols ? magnitude_bits(r[v][i]) : 0);
+        const float scale = int8_scale(row_max<L>(top, tops)), inverse = 1.0f / scale;
+        if (lane == 0) ((float *)a.scales)[row] = scale;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * L + lane) * 8;
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, c + i < a.cols ? magnitude_bits(r[v][i]) : 0);
-            const int byte = e4m3_scale_byte(lanes_max<16>(top));
 #pragma unroll
             for (int i = 0; i < 8; ++i) r[v][i] = c + i < a.cols ? r[v][i] : 0.0f;
-            if (c < kp) store_e4m3(codes + c, r[v], byte);
-            if (c < kp && (lane & 15) == 0) sc[c >> 7] = (uint8_t)byte;
+            if (c < kp) store_int8(codes + c, r[v], inverse, scale != scale);
         }
-        if (lane < ks - (kp >> 7)) sc[(kp >> 7) + lane] = 127;
-        return;
-    }
-    uint32_t top = 0;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, (v * L + lane) * 8 + i < a.cols ? magnitude_bits(r[v][i]) : 0);
-    const float scale = int8_scale(row_max<L>(top, tops)), inverse = 1.0f / scale;
-    if (lane == 0) ((float *)a.scales)[row] = scale;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = (v * L + lane) * 8;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[v][i] = c + i < a.cols ? r[v][i] : 0.0f;
-        if (c < kp) store_int8(codes + c, r[v], inverse, scale != scale);
     }
 }
 
