@@ -219,6 +219,18 @@ __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear
     }
     f32x4 acc[FM][FN] = {};
 
+    // int8: the scales of this lane's rows and outputs, on their way before the steps
+    float xf[INT8 ? FM : 1], wf[INT8 ? FN : 1][4];
+    if constexpr (INT8) {
+#pragma unroll
+        for (int m = 0; m < FM; ++m) {
+            const int row = from[(wm * FM + m) * 16 + r16];
+            xf[m] = *(const float *)(row >= 0 ? (const char *)(a.xf + row) : zeros);
+        }
+#pragma unroll
+        for (int f = 0; f < FN; ++f) output_scales(a, p.type, j0 + (wn * FN + f) * 16 + g * 4, wf[f]);
+    }
+
     // fp8: the scale bytes of this lane's rows and of the weights, whose columns of a wave lie in one
     // block of 128.  A word is four steps; the next one is read a word ahead.
     const char *xs[FP8 ? FM : 1];
@@ -380,18 +392,12 @@ __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear
     const int *out = to + wm * FM * 16;
     const int j1 = j0 + wn * FN * 16;               // this wave's first column
     if constexpr (INT8) {                           // whole numbers to fp32, times the scales
-        float wf[FN][4];
 #pragma unroll
-        for (int f = 0; f < FN; ++f) output_scales(a, p.type, j1 + f * 16 + g * 4, wf[f]);
-#pragma unroll
-        for (int m = 0; m < FM; ++m) {
-            const int row = from[(wm * FM + m) * 16 + r16];
-            const float xf = row >= 0 ? a.xf[row] : 0.0f;
+        for (int m = 0; m < FM; ++m)
 #pragma unroll
             for (int f = 0; f < FN; ++f)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][f][i] = (float)__float_as_int(acc[m][f][i]) * xf * wf[f][i];
-        }
+                for (int i = 0; i < 4; ++i) acc[m][f][i] = (float)__float_as_int(acc[m][f][i]) * xf[m] * wf[f][i];
     }
     if (sizeof(E) == 4 || a.y_f32) {
 #pragma unroll
