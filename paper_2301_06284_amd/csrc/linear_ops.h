@@ -92,10 +92,10 @@ inline int64_t row_tiles_bound(int64_t M, int64_t T, int64_t rows)
 
 #ifdef __HIPCC__
 
-// A launch holds fewer than 2^32 threads along x: `groups` workgroups (fewer than 2^31) in rows of 2^22.
+// A launch holds fewer than 2^32 threads along x: `groups` workgroups (fewer than 2^31) of up to 1024 in rows of 2^21.
 inline dim3 flat_grid(int64_t groups)
 {
-    constexpr int64_t row = int64_t(1) << 22;
+    constexpr int64_t row = int64_t(1) << 21;
     return groups <= row ? dim3((uint32_t)groups) : dim3((uint32_t)row, (uint32_t)((groups + row - 1) / row));
 }
 __device__ __forceinline__ uint32_t flat_block() { return blockIdx.y * gridDim.x + blockIdx.x; }

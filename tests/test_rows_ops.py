@@ -860,6 +860,23 @@ def test_rows_beyond_32_bits():
     assert torch.equal(y, small)
 
 
+def test_more_workgroups_than_a_launch_is_wide():
+    """2^22 rows and more of 1024 threads each, which along one axis were 2^32 threads.  All rows repeat the first 64."""
+    import torch
+    from paper_2301_06284_amd import rgnn
+    rows, cols = 2 ** 22 + 64, 4104
+    print("more workgroups than a launch is wide", flush=True)
+    first = matrix(torch.Generator(device="cuda").manual_seed(6), 64, cols, torch.bfloat16)
+    w, small = torch.ones(cols, dtype=torch.bfloat16, device="cuda"), torch.empty_like(first)
+    x = first.repeat(rows // 64, 1)
+    rgnn.rms_norm(first, w, small)
+    rgnn.rms_norm(x, w, x)
+    for part in x.view(-1, 64, cols).split(4096):
+        assert (part == small).all()
+    del x, part
+    torch.cuda.empty_cache()
+
+
 def test_streams():
     """Two calls at once on two streams, with workspaces of their own; outputs made in the stream's memory."""
     import torch
