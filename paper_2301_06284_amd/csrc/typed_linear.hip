@@ -219,17 +219,23 @@ __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear
     }
     f32x4 acc[FM][FN] = {};
 
-    // int8: the scales of this lane's rows and outputs, on their way before the steps
+    // int8: the scales of this lane's rows and outputs, on their way before the steps.  The one-step 128 x 128 tile, whose
+    // bound on registers leaves no room for them beside its sums, reads them afterwards (before, 20 registers spilled: 1 000 003 rows
+    // 64 -> 128 113 us, 85 now; 300 007 rows of 96 types 128 -> 128 35 and 26; but 64 -> 64, 128 x 64 tiles, 16.8 before, 18.2 after).
+    constexpr bool BEFORE = STAGES > 1 || FM * FN < 16;
     float xf[INT8 ? FM : 1], wf[INT8 ? FN : 1][4];
-    if constexpr (INT8) {
+    auto factors = [&] {
+        if constexpr (INT8) {
 #pragma unroll
-        for (int m = 0; m < FM; ++m) {
-            const int row = from[(wm * FM + m) * 16 + r16];
-            xf[m] = *(const float *)(row >= 0 ? (const char *)(a.xf + row) : zeros);
+            for (int m = 0; m < FM; ++m) {
+                const int row = from[(wm * FM + m) * 16 + r16];
+                xf[m] = *(const float *)(row >= 0 ? (const char *)(a.xf + row) : zeros);
+            }
+#pragma unroll
+            for (int f = 0; f < FN; ++f) output_scales(a, p.type, j0 + (wn * FN + f) * 16 + g * 4, wf[f]);
         }
-#pragma unroll
-        for (int f = 0; f < FN; ++f) output_scales(a, p.type, j0 + (wn * FN + f) * 16 + g * 4, wf[f]);
-    }
+    };
+    if (BEFORE) factors();
 
     // fp8: the scale bytes of this lane's rows and of the weights, whose columns of a wave lie in one
     // block of 128.  A word is four steps; the next one is read a word ahead.
@@ -392,6 +398,7 @@ __global__ __launch_bounds__(WM *WN * 64, STAGES == 1 ? 4 : 2) void typed_linear
     const int *out = to + wm * FM * 16;
     const int j1 = j0 + wn * FN * 16;               // this wave's first column
     if constexpr (INT8) {                           // whole numbers to fp32, times the scales
+        if (!BEFORE) factors();
 #pragma unroll
         for (int m = 0; m < FM; ++m)
 #pragma unroll
