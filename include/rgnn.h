@@ -532,7 +532,8 @@ rgnn_status rgnn_dropout(const rgnn_dropout_rows_t *args, void *stream);
  *   y_dtype: fp32 or 16-bit, scales then unused; or RGNN_F8_E4M3: Y codes [rows, Kp] and scales uint8 [rows, Ks] as
  *   rgnn_fp8_quantize_rows makes them of y in fp32; or RGNN_I8: Y codes [rows, Kp] and scales fp32 [rows] as
  *   rgnn_int8_quantize_rows does (codes on a 16-byte address, scales on a 4-byte one; ldy unused).
- * A NaN or an infinity in a row spoils that row alone; a row of zeros gives zeros where eps > 0. */
+ * A NaN or an infinity in a row spoils that row alone.  s beyond fp32 (mean(r^2) + eps below about 2^-256) counts as the largest
+ * fp32 number, so that a row of zeros gives zeros for any eps > 0; with eps = 0 it gives s = infinity and NaN. */
 typedef struct {
     const void *X;             /* [rows, cols] of dtype                       */
     const void *residual;      /* [rows, cols] of sum_dtype, or NULL          */

@@ -36,9 +36,12 @@ __device__ __forceinline__ void sum8(const NormArgs &a, const Philox &gen, int64
     for (int i = 0; i < 8; ++i) r[i] = (float)(RT)r[i];
 }
 
+// What lies beyond fp32 counts as its largest number, so that zeros times it are zeros for any eps > 0; of a row of zeros
+// without eps it is infinite.
 __device__ __forceinline__ float inverse_rms(double squares, int cols, double eps)
 {
-    return (float)(1.0 / sqrt(squares / cols + eps));
+    const double s = 1.0 / sqrt(squares / cols + eps);
+    return s < __builtin_inf() ? (float)fmin(s, 0x1.fffffep+127) : (float)s;
 }
 
 // L threads hold a row, NV vectors of eight columns each.
