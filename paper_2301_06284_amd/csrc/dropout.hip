@@ -15,7 +15,6 @@ namespace {
 constexpr int kVectors = 4;
 
 struct Cut {
-    int chunks;          // vectors of a row
     int wide, tall;      // a workgroup's: vectors of a row, rows
     int across;          // workgroups side by side
     uint32_t inverse;    // ceil(2^32 / wide)
@@ -85,10 +84,11 @@ void launch_types(const DropoutArgs &a, const Cut &cut, dim3 grid, hipStream_t s
     else with(std::integral_constant<Fit, kTiny>());
 }
 
+// Of calls with a 16-bit type.
 template <class H>
 void launch_half(const DropoutArgs &a, const Cut &cut, dim3 grid, hipStream_t s)
 {
-    if (a.x32) a.y32 ? launch_types<H, true, true>(a, cut, grid, s) : launch_types<H, true, false>(a, cut, grid, s);
+    if (a.x32) launch_types<H, true, false>(a, cut, grid, s);
     else a.y32 ? launch_types<H, false, true>(a, cut, grid, s) : launch_types<H, false, false>(a, cut, grid, s);
 }
 
@@ -97,19 +97,20 @@ void launch_half(const DropoutArgs &a, const Cut &cut, dim3 grid, hipStream_t s)
 rgnn_status launch_dropout(const DropoutArgs &a, hipStream_t s)
 {
     constexpr int most = 256 * kVectors;
+    const int chunks = (a.cols + 7) / 8;          // vectors of a row
     Cut cut;
-    cut.chunks = (a.cols + 7) / 8;
-    cut.across = (cut.chunks + most - 1) / most;
-    cut.wide = (cut.chunks + cut.across - 1) / cut.across;
+    cut.across = (chunks + most - 1) / most;
+    cut.wide = (chunks + cut.across - 1) / cut.across;
     // small matrices: one vector a thread
-    const int share = (int64_t)a.rows * cut.chunks <= 256 * 1024 ? 256 : most;
+    const int share = (int64_t)a.rows * chunks <= 256 * 1024 ? 256 : most;
     cut.tall = std::max(1, share / cut.wide);
     cut.inverse = cut.wide == 1 ? 0 : (uint32_t)(((uint64_t(1) << 32) + cut.wide - 1) / cut.wide);
     const int64_t groups = (a.rows + cut.tall - 1) / cut.tall * cut.across;
     if (groups >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many rows");
     {
         LaunchScope ls("dropout", s);
-        if (a.half == RGNN_F16) launch_half<_Float16>(a, cut, flat_grid(groups), s);
+        if (a.x32 && a.y32) launch_types<__bf16, true, true>(a, cut, flat_grid(groups), s);
+        else if (a.half == RGNN_F16) launch_half<_Float16>(a, cut, flat_grid(groups), s);
         else launch_half<__bf16>(a, cut, flat_grid(groups), s);
     }
     hipError_t e = hipGetLastError();

@@ -256,8 +256,9 @@ void launch_cols(const NormArgs &a, hipStream_t s)
     if constexpr (FIT == kEnds)
         if (a.rows > 4096 && cols > 256 && cols <= 1024)
             return cols <= 512 ? launch_rows<H, X32, R32, FIT, 32, 2>(a, s) : launch_rows<H, X32, R32, FIT, 64, 2>(a, s);
-    if (cols <= 8) launch_rows<H, X32, R32, FIT, 1, 1>(a, s);
-    else if (cols <= 32) launch_rows<H, X32, R32, FIT, 4, 1>(a, s);
+    if constexpr (FIT == kWhole)      // rows that end inside a vector have more than eight columns
+        if (cols <= 8) return launch_rows<H, X32, R32, FIT, 1, 1>(a, s);
+    if (cols <= 32) launch_rows<H, X32, R32, FIT, 4, 1>(a, s);
     else if (cols <= 64) launch_rows<H, X32, R32, FIT, 8, 1>(a, s);
     else if (cols <= 128) launch_rows<H, X32, R32, FIT, 16, 1>(a, s);
     else if (cols <= 256) launch_rows<H, X32, R32, FIT, 32, 1>(a, s);

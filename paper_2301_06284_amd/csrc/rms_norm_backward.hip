@@ -240,9 +240,13 @@ void launch_shape(const NormBackwardArgs &a, int64_t groups, hipStream_t s)
 {
     const dim3 g((uint32_t)groups), b(L > 256 ? L : 256);
     const Fit fit = fit_of(a.cols);
-    if (fit == kWhole) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kWhole, DROP, L, NV>), g, b, 0, s, a);
-    else if (fit == kEnds) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kEnds, DROP, L, NV>), g, b, 0, s, a);
-    else if constexpr (L == 1) hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kTiny, DROP, L, NV>), g, b, 0, s, a);
+    if (fit == kWhole) {
+        hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kWhole, DROP, L, NV>), g, b, 0, s, a);
+    } else if constexpr (L == 1) {       // rows that end inside a vector have more than eight columns
+        hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kTiny, DROP, L, NV>), g, b, 0, s, a);
+    } else {
+        hipLaunchKernelGGL((rms_norm_backward_kernel<H, DY32, R32, kEnds, DROP, L, NV>), g, b, 0, s, a);
+    }
 }
 
 template <class H, bool DY32, bool R32, bool DROP>

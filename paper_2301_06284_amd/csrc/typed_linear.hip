@@ -620,10 +620,12 @@ rgnn_status launch_tile(TileArgs k, hipStream_t s)
     const int64_t grid = xcd_grid(tiles, k.window);
     if (grid >= (int64_t(1) << 31)) return fail(RGNN_ERANGE, "too many tiles");
     const dim3 g = flat_grid(grid), b(WM * WN * 64);
-    if (k.K * (int)sizeof(typename T::elem) <= 128)
+    if constexpr (DEEP)              // of many steps
+        hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, 4>), g, b, 0, s, k);
+    else if (k.K * (int)sizeof(typename T::elem) <= 128)
         hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, 1>), g, b, 0, s, k);
     else
-        hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, DEEP ? 4 : 2>), g, b, 0, s, k);
+        hipLaunchKernelGGL((typed_linear_kernel<T, BM, BN, WM, WN, TRANS, ANY, 2>), g, b, 0, s, k);
     return RGNN_OK;
 }
 

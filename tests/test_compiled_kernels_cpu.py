@@ -50,3 +50,15 @@ def test_integer_tiles_keep_their_sums_in_registers(compiled):
     assert len(tiles) >= 6
     for name, k in tiles.items():
         assert k["vgpr_spill_count"] == 0 and k["private_segment_fixed_size"] == 0, name
+
+
+@pytest.mark.parametrize("pattern", [
+    r"rms_norm_kernelI.*LNS_3FitE1ELi1ELi1E",                 # one lane a row, rows that end inside a vector: those have nine columns or more
+    r"rms_norm_backward_kernelI.*LNS_3FitE1ELb[01]ELi1ELi1E",
+    r"dropout_kernelIDF16_Lb1ELb1E",                          # all of fp32, compiled for a second 16-bit type
+    r"typed_linear_kernelI.*(BF16|F16|F8|I8)ELi(32|64)ELi64E.*Lb0ELi1EEE",      # four-stage tiles where k is one step
+])
+def test_nothing_is_compiled_that_no_call_reaches(compiled, pattern):
+    kept = re.sub(r"LNS_3FitE1", "LNS_3FitE0", pattern).replace("Lb1ELb1E", "Lb1ELb0E").replace("Lb0ELi1EEE", "Lb0ELi4EEE")
+    assert any(re.search(kept, n) for n in compiled), "the names have changed"
+    assert [n for n in compiled if re.search(pattern, n)] == []
