@@ -70,7 +70,7 @@ extern "C" rgnn_status rgnn_rms_norm(const rgnn_rms_norm_t *args, void *stream)
     const int32_t dtype = p.dtype, sum_dtype = p.sum_dtype, w_dtype = p.w_dtype, y_dtype = p.y_dtype, cols = p.cols;
     const int64_t rows = p.rows;
     const bool codes = dtype_eight(y_dtype);
-    if (!float_type(dtype) || !float_type(sum_dtype)) return fail(RGNN_EINVAL, "X and p.sum must be fp32, bf16 or fp16");
+    if (!float_type(dtype) || !float_type(sum_dtype)) return fail(RGNN_EINVAL, "X and sum must be fp32, bf16 or fp16");
     if (!codes && !float_type(y_dtype)) return fail(RGNN_EINVAL, "Y must be fp32, bf16, fp16, e4m3 or int8");
     if (p.weight && !float_type(w_dtype)) return fail(RGNN_EINVAL, "weight must be fp32, bf16 or fp16");
     Half half;

@@ -278,3 +278,10 @@ def test_tile_of_int8():
             assert l.rgnn_typed_linear_select_tile(dtype, P, rows, K, None, types, rows, P, K, N, 1, ctypes.byref(t)) == 0
             got.append((t.rows, t.cols, t.stages, t.any))
         assert got[0] == got[1]
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=3), dict(sum_dtype=3)])
+def test_messages_name_the_arguments_as_documented(kw):
+    _, l = lib()
+    assert norm(**kw) == -1
+    assert l.rgnn_last_error() == b"X and sum must be fp32, bf16 or fp16"
