@@ -498,7 +498,7 @@ rgnn_status rgnn_typed_linear_int8(const void *X, const float *x_scales, int64_t
  *   - An output may be one of the inputs if it has its address, type and leading dimension (Y on X, sum on
  *     residual); otherwise outputs overlap nothing.
  *   - Results are reproducible: no atomics, sums in a fixed order, whatever the launch.
- *   - A row stays in registers up to 32768 columns (in the backward pass 16384); longer ones are read twice or, into
+ *   - A row is read once up to 32768 columns (in the backward pass 16384); longer ones twice or, into
  *     8-bit integers, three times, by one workgroup.
  */
 

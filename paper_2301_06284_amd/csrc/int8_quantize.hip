@@ -2,7 +2,7 @@
 // output of a type's weight (channel): scale = max |x| / 127, code = round(x (1 / scale)).
 //
 // A row stays in registers between its maximum and its codes, and so do a weight's columns up to 4096 k in 16 bits (2048 in
-// fp32); longer ones are read twice.  The weights' codes turn over in LDS to rows of k.
+// fp32; of the longest, 16-bit outputs that end inside a vector spill three registers); longer ones are read twice.  The weights' codes turn over in LDS to rows of k.
 //
 // Bound by memory.  Measured, bf16: rows 8192 x 4096 17 us (5.8 TB/s), 8 rows of 2048 2.6; weights 16 x 2048 x 1536
 // 39 us (3.8 TB/s: every workgroup loads first and stores last), 4096 x 4096 18, 4 x 5000 x 3000 (read twice) 74.

@@ -4,12 +4,12 @@
 // A row is read once and stays in registers from its loads to its stores: a few lanes of a wave hold a short row, a wave
 // or a workgroup a long one, eight columns a lane at a time.  Squares are summed in 64 bits, which costs
 // next to nothing where memory is waited for (16 384 x 2048 74.4 us, in 32 bits 74.3; 8000 x 4096 42.8 and 42.5; 600 000 x 24
-// 30.8 and 28.5): the result does not depend on how a row is cut, and a code next to a border is the one that the formula
-// gives.
+// 30.8 and 28.5).  A sum is off by some 2^-53 of itself, so that 1 / rms is the formula's to half a step of fp32, and rows
+// that are cut in another way differ only where theirs lies next to a border of that rounding.
 //
 // Bound by memory, a few rows by the launch.  Measured, with residual and sum: 1 000 003 x 64 fp32 181 us (5.7 TB/s), 16 384 x
 // 2048 bf16 with an fp32 residual and dropout 74 us (5.4), 8192 x 4096 bf16 into e4m3 45 us (5.2), 15 000 x 2048 bf16
-// 39 us (6.3, from the last-level cache in part), 10 000 x 333 fp16 8.2 us, 8 x 2048 2.5 us in a graph.
+// 37 to 39 us (6.3, from the last-level cache in part), 10 007 x 333 fp16 9.4 us (8.7 in a graph), 8 x 2048 2.9 us in a graph.
 #include <algorithm>
 
 #include "rows.h"

@@ -1,14 +1,19 @@
 // rms_norm_backward.hip -- gradients of the root-mean-square norm with residual and dropout.
 //
 // With n = r s and g = dY w: dr = s (g - n mean(g n)) + dsum, the residual's gradient; dX = D'(dr), whose kept
-// values the generator tells again; dw = sum over the rows of dY n.  A row is read once and stays in registers.
+// values the generator tells again; dw = sum over the rows of dY n.  A row is read once and stays in registers, up to 16 384 columns.
 // A workgroup takes every G-th group of rows and keeps dw of its columns in registers to the end, then
 // writes it to the workspace; a second launch adds the G rows there in 64 bits, in their order, so that results are
 // reproducible.
 //
-// Bound by memory.  Measured, with d_sum, dX and d_residual: 16 384 x 2048 bf16 with an fp32 sum and dropout 105 + 5 us
-// (5.0 TB/s), 15 000 x 2048 bf16 56 us (5.5), 100 000 x 333 fp16 75 us (4.4), 2000 x 16 000 bf16 71 us (4.5), 8 x 2048 5 us,
-// two launches.  The register count (82 to 105) leaves four workgroups on a CU; bounds for six spill and take 1.4 to 2.5 times as long.
+// Bound by memory.  Measured, with d_sum, dX and d_residual, both launches: 16 384 x 2048 bf16 with an fp32 sum and dropout 110 us
+// (4.9 TB/s), 15 000 x 2048 bf16 58 (5.3), 8000 x 4096 65 (5.0), 100 000 x 333 fp16 77 (4.3), 8 x 2048 6.  One vector a lane takes 70 to
+// 105 registers up to 2048 columns (to 116 beyond), which leaves four workgroups of 256 threads or more on a CU; bounds for six spill and
+// take 1.4 to 2.5 times as long.  Two vectors a lane (513 to 1024 columns) take 128 to 173, which leaves two to four;
+// memory is busy all the same (20 000 x 768 bf16 with an fp32 sum and dropout 45 to 48 us, 5.1 TB/s; 30 000 x 1024 100, 4.9, all bf16
+// 55, 5.5; 30 000 x 1001 fp16 63, 4.7).  1024 threads of two vectors (8193 to 16 384 columns) have 128 at most: 16-bit dY and
+// sum fit (2000 x 16 000 bf16 75 us, 4.2 TB/s); both fp32, or one of them with dropout, spill up to 52 (fp32 sum and
+// dropout 122 us, 4.2; all fp32 145, 4.4, with dropout 169, 3.8, and 16 001 columns 183, 3.5).
 #include <algorithm>
 
 #include "rows.h"
@@ -22,7 +27,7 @@ constexpr int kLong = 32768;         // columns whose dw LDS holds
 // Rows of a workgroup: several short ones, of 1 to 64 lanes each.
 int rows_of_group(int cols) { return cols <= 8 ? 256 : cols <= 32 ? 64 : cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
 // As many workgroups as the CUs hold at a time: 1024 are four on each (1280, or fewer of them with equal turns,
-// 3 to 8 % slower).
+// 3 to 8 % slower).  At 513 to 1024 columns the registers let 512 or more of the 1024 run at a time, and the others follow.
 int64_t groups_of(int64_t rows, int cols)
 {
     const int per = rows_of_group(cols);
@@ -93,7 +98,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void rms_norm_backward_kernel(No
                 dot += (double)(d * w[v][i] * n);
             }
             // Where registers are short, the words are kept as they came over the sum (16 bits: 8 registers in place
-            // of 24), and dw is done with them (2000 rows of 16 000, bf16: 71 us, 131 from LDS and L2).
+            // of 24), and dw is done with them (2000 rows of 16 000, bf16: 75 us, 131 from LDS and L2).
             if constexpr (L * NV > 1024) {
                 opaque(dw[v]);
                 opaque(dy[v].raw);

@@ -24,10 +24,11 @@
 //   few rows: the weights' bytes, and the latency of the steps (16 rows of 2048 -> 1536, 13 of 32 types'
 //     weights read: 19 us, 4.3 TB/s; in 8 bits 10 us, 4.0 TB/s; as integers, 10 of 32 types, 9 us);
 //   many rows of narrow weights: memory (300 007 rows 64 -> 64, fp16: 16 us, 5.0 TB/s; 1 000 003
-//     gathered and scattered rows 64 -> 128, bf16: 95 us, 4.1 TB/s of rows at random, each counted as often as it is read);
+//     gathered and scattered rows 64 -> 128, bf16: 95 us, 4.1 TB/s of rows at random, each counted as often as it is read; rows of
+//     8-bit integers in order, codes of 128 bytes, 85 us, 4.6 TB/s);
 //   many rows of wide weights: the matrix cores, at the rate of the whole tiles that the types' sizes
 //     leave (16 384 rows of 32 types, 2048 -> 4096, bf16: 322 us, 0.85 PFLOP/s; one type 242 us, 1.14; 8
-//     bits, 8192 rows 4096 -> 4096: 156 us, 1.76 PFLOP/s; as integers 148 us, 1.86 POP/s);
+//     bits, 8192 rows 4096 -> 4096: 156 us, 1.76 PFLOP/s; as integers 151 us, 139 in a graph, 1.8 to 2.0 POP/s);
 //   thousands of types: the search for a tile, which every workgroup makes from the first offset on (bf16, 65 535
 //     rows, 64 -> 64: 1024 types 10 us, 4096 42, 16 384 380, 65 535 5.1 ms).
 #include <algorithm>
